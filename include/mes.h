@@ -69,7 +69,8 @@ typedef enum {
   MES_ERR_SEGMENTS = 5,  /* seg_offsets not 0 = o[0] <= ... <= o[E] = T              */
   MES_ERR_ALIGN = 6,     /* a pointer is not 16-byte aligned                         */
   MES_ERR_WORKSPACE = 7, /* workspace missing or too small                           */
-  MES_ERR_DEVICE = 8     /* a HIP call failed (message carries the HIP error string) */
+  MES_ERR_DEVICE = 8,    /* a HIP call failed (message carries the HIP error string) */
+  MES_ERR_PAGES = 9      /* not enough free pages, or page pairs that cannot be copied */
 } mes_status;
 
 /* Quantisation grid (Eq. 1 and its symmetric variant). */
@@ -304,6 +305,111 @@ mes_status mes_step_grad(const float* delta, int d_in, int d_out, const int32_t*
  * number of this update.  step, grad, m, v: DEVICE fp32 [n]; m and v start at 0. */
 mes_status mes_step_adamw(float* step, const float* grad, float* m, float* v, int n, int t, float lr, float beta1,
                           float beta2, float eps, float weight_decay, void* stream);
+
+/* ---- attention between the projections of a block: a paged cache of keys and values, what writes it, the attention
+ * that reads it, and the movement of its pages ------------------------------------------------------------------
+ * The blocks that the linears above belong to (Section 5: Mistral-7B, LLaMA-2-13B) compute, per query head h of
+ * n_heads and its key / value head g = h / (n_heads / n_kv_heads), for the token at position p of its sequence
+ *     out[h] = sum_{j <= p} softmax_j(scale * <q[h], k_j[g]>) v_j[g]                    (causal; scale usually head_dim^-1/2)
+ * Queries, fresh keys / values and outputs are bf16 [T][heads][head_dim], head_dim contiguous, heads head_dim apart,
+ * rows ld_* elements apart (ld_* >= heads * head_dim, a multiple of 8: views of one fused q/k/v buffer are fine), 16-byte
+ * aligned.  head_dim is 64 or 128; n_heads is a multiple of n_kv_heads, at most 64 times as many.
+ * Numerics: scores, softmax statistics and sums are fp32; the softmax weights are rounded to bf16 for the product with
+ * V, the output is rounded once.  A row that sees no token is 0.  Tokens that a row does not see do not touch it, whatever
+ * their keys and values hold (infinities and NaN included).
+ *
+ * The cache: k and v are [n_layers][n_pages][n_kv_heads][page_tokens][head_dim], page_tokens 16, 32, 64, 128 or 256, 16-byte
+ * aligned.  MES_KV_BF16: bf16.  MES_KV_E4M3: 8-bit floating point (4 exponent, 3 mantissa bits, largest value 448), value =
+ * code * scale with one fp32 scale per layer and head, k_scale and v_scale [n_layers][n_kv_heads] (NULL for bf16). */
+enum { MES_KV_BF16 = 0, MES_KV_E4M3 = 1 };
+#define MES_MAX_SEQS 4096
+typedef struct {           /* HOST struct; pointers DEVICE, caller-owned */
+  int32_t n_layers, n_pages, page_tokens, n_kv_heads, head_dim, dtype;
+  void* k;
+  void* v;
+  const float* k_scale;
+  const float* v_scale;
+} mes_kv;
+
+/* The sequences of a call (HOST struct; pointers DEVICE, so that a captured graph can be replayed while they grow).
+ * Sequence s holds kv_len[s] tokens (the call's own included); token j stands in slot j % page_tokens of page
+ * page_table[s * table_pages + j / page_tokens].  The rows q_offsets[s] .. q_offsets[s+1] of the call are its LAST tokens
+ * (q_offsets NULL: one row per sequence, row s).  0 <= n_seqs <= MES_MAX_SEQS; calls of no
+ * sequences or no rows return MES_OK without touching anything.
+ * Values that the host cannot see are checked where they are used: a token past the table's room or on a page outside
+ * [0, n_pages) counts as absent (never read or written), a negative kv_len as 0. */
+typedef struct {
+  int32_t n_seqs, table_pages;
+  const int32_t* q_offsets;    /* [n_seqs + 1], 0 = o[0] <= o[1] <= ...; rows behind o[n_seqs] are left as they are */
+  const int32_t* kv_len;       /* [n_seqs] */
+  const int32_t* page_table;   /* [n_seqs][table_pages] */
+} mes_seqs;
+
+/* Rotary embedding of new queries and keys, and writing keys and values to the cache's pages (layer `layer`).
+ * q (may be NULL with q_out), k, v: T new rows; row t of sequence s has position kv_len[s] - (q_offsets[s+1] - t).
+ * rotary: fp32 [n_positions][2][head_dim / 2], cosines then sines, n_positions >= table_pages * page_tokens; element i of
+ * the first half turns with element i of the second: (a c - b s, b c + a s), every product and sum rounded to fp32, the
+ * result once to bf16 (q_out; may be q) or to the cache's type (e4m3: after division by the scale, to nearest even,
+ * clamped to +-448).  rotary NULL: keys are written as they are and q must be NULL.
+ * Rows without a place (see mes_seqs) are left out.  Two rows of one call must not share a place. */
+mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                         int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
+                         int ld_q_out, void* stream);
+
+/* Attention over whole prompts: n_seqs sequences packed one after the other, rows seq_offsets[s] .. seq_offsets[s+1]
+ * (DEVICE int32 [n_seqs + 1], 0 = o[0] <= ... <= o[n_seqs] <= T; rows behind are left as they are), every row sees the
+ * rows of its own sequence up to itself.  out: [T][n_heads][head_dim], rows ld_out apart. */
+mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, int n_seqs, const int32_t* seq_offsets,
+                           int n_heads, int n_kv_heads, int head_dim, int ld_q, int ld_k, int ld_v, float scale, void* out,
+                           int ld_out, void* stream);
+
+/* The same with keys and values in the cache (a prompt behind a cached system prompt, the next piece of a long prompt):
+ * the T rows are the last tokens of their sequences and their keys / values have been appended.  q_offsets not NULL. */
+mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, int T, int n_heads, int ld_q,
+                           float scale, void* out, int ld_out, void* stream);
+
+/* One token per sequence (q_offsets is not read): row s attends to the kv_len[s] cached tokens of sequence s.
+ * Sequences that share a prefix: rows are sorted by expert as for mes_delta_linear, seg_offsets HOST [n_experts + 1]
+ * with o[n_experts] = n_seqs, and those sequences of expert e that have prefix_len[e] tokens or more hold the same
+ * tokens in their first prefix_len[e] positions (HOST [n_experts], >= 0; for instance the expert's system prompt).  These are
+ * read once for all of them, through the page table of the first such sequence; they need not be shared pages.  A
+ * shorter sequence (a row that only pads the batch: kv_len 0) is read by itself.
+ * seg_offsets and prefix_len NULL (n_experts ignored): nothing is shared.  1 <= n_experts <= MES_MAX_EXPERTS.
+ * workspace: >= mes_attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim), 16-byte aligned, contents
+ * irrelevant; calls sharing a workspace must be stream-ordered.  Results do not depend on other calls, and are the same
+ * from run to run. */
+size_t mes_attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim);
+mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, int n_heads, int ld_q,
+                           int n_experts, const int32_t* seg_offsets, const int32_t* prefix_len, float scale, void* out,
+                           int ld_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies n pages, page src[i] to page dst[i], in all layers of keys and values.  src, dst: HOST int32 [n], inside [0,
+ * n_pages); no page may be written twice, or both read and written (MES_ERR_PAGES). */
+mes_status mes_kv_copy_pages(const mes_kv* kv, const int32_t* src, const int32_t* dst, int n, void* stream);
+
+/* Which pages hold which sequence: bookkeeping on the HOST only (no GPU call), for max_seqs sequences, numbered from 0,
+ * of at most max_seq_pages pages each.  Pages are counted: forked sequences share pages until one of them writes.  The
+ * lowest free page is taken first.  Not thread-safe.
+ *  grow     sequences seqs[n] (distinct) get n_tokens[i] >= 0 more tokens each.  Where the first of them falls into a page
+ *           that others hold too, the sequence gets a page of its own and the pair (page to copy, its page) is added to
+ *           copy_src / copy_dst (room for n each): mes_kv_copy_pages them before the tokens are appended.  All or
+ *           nothing: MES_ERR_PAGES if pages run out, MES_ERR_SHAPE if a sequence outgrows max_seq_pages.
+ *  fork     child (empty) shares the first n_tokens <= length(parent) tokens of parent.
+ *  free     the sequence is empty again; pages nobody else holds become free.
+ *  compact  moves the pages in use to the lowest ids; pairs to copy in copy_src / copy_dst (room for n_pages / 2 each).
+ *           No page is both read and written by them.  Tables written before are out of date.
+ *  table    fills table[n][table_pages] (unused entries 0) and len[n] (may be NULL) for the sequences seqs[n]. */
+typedef struct mes_pages mes_pages;
+mes_status mes_pages_create(int n_pages, int page_tokens, int max_seqs, int max_seq_pages, mes_pages** out);
+void mes_pages_destroy(mes_pages* pages);
+mes_status mes_pages_grow(mes_pages* pages, const int32_t* seqs, const int32_t* n_tokens, int n, int32_t* copy_src,
+                          int32_t* copy_dst, int* n_copies);
+mes_status mes_pages_fork(mes_pages* pages, int parent, int child, int n_tokens);
+mes_status mes_pages_free(mes_pages* pages, int seq);
+mes_status mes_pages_compact(mes_pages* pages, int32_t* copy_src, int32_t* copy_dst, int* n_copies);
+mes_status mes_pages_table(const mes_pages* pages, const int32_t* seqs, int n, int32_t* table, int table_pages, int32_t* len);
+int mes_pages_length(const mes_pages* pages, int seq);   /* tokens of a sequence, or -1 */
+int mes_pages_unused(const mes_pages* pages);            /* free pages, or -1 */
 
 #ifdef __cplusplus
 }

@@ -21,8 +21,11 @@ GRID_SYM, GRID_EQ1 = 0, 1
 STEP_GIVEN, STEP_MAXABS, STEP_MEANABS = 0, 1, 2
 MAX_EXPERTS = 64
 
+KV_BF16, KV_E4M3 = 0, 1
+MAX_SEQS = 4096
+
 STATUS_NAMES = {0: "MES_OK", 1: "MES_ERR_NULL", 2: "MES_ERR_SHAPE", 3: "MES_ERR_BITS", 4: "MES_ERR_SALIENT",
-                5: "MES_ERR_SEGMENTS", 6: "MES_ERR_ALIGN", 7: "MES_ERR_WORKSPACE", 8: "MES_ERR_DEVICE"}
+                5: "MES_ERR_SEGMENTS", 6: "MES_ERR_ALIGN", 7: "MES_ERR_WORKSPACE", 8: "MES_ERR_DEVICE", 9: "MES_ERR_PAGES"}
 
 EXPORTS = ["mes_base_bytes", "mes_codes_bytes", "mes_salient_bytes", "mes_pack_workspace_bytes",
            "mes_select_workspace_bytes", "mes_linear_workspace_bytes", "mes_last_error", "mes_layout_version",
@@ -34,7 +37,10 @@ EXPORTS = ["mes_base_bytes", "mes_codes_bytes", "mes_salient_bytes", "mes_pack_w
            "mes_pool_register_blob", "mes_pool_acquire_multi", "mes_pool_prefetch", "mes_pool_prefetched",
            "mes_gated_workspace_bytes", "mes_delta_linear_gated",
            "mes_step_grad_workspace_bytes", "mes_step_grad", "mes_step_adamw", "mes_noalloc_scratch_bytes",
-           "mes_delta_linear_noalloc", "mes_long_segment_tokens"]
+           "mes_delta_linear_noalloc", "mes_long_segment_tokens",
+           "mes_kv_append", "mes_attn_prompt", "mes_attn_extend", "mes_attn_decode_workspace_bytes", "mes_attn_decode",
+           "mes_kv_copy_pages", "mes_pages_create", "mes_pages_destroy", "mes_pages_grow", "mes_pages_fork", "mes_pages_free",
+           "mes_pages_compact", "mes_pages_table", "mes_pages_length", "mes_pages_unused"]
 
 
 class MesError(RuntimeError):
@@ -52,6 +58,16 @@ class mes_delta(ctypes.Structure):
 
 class mes_linear(ctypes.Structure):
     _fields_ = [("w_base_tiled", ctypes.c_void_p), ("experts", ctypes.POINTER(mes_delta)), ("y", ctypes.c_void_p)]
+
+
+class mes_kv(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_pages", "page_tokens", "n_kv_heads", "head_dim", "dtype")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class mes_seqs(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("table_pages", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("q_offsets", "kv_len", "page_table")]
 
 
 def _load() -> ctypes.CDLL:
@@ -147,6 +163,37 @@ def _load() -> ctypes.CDLL:
     lib.mes_pool_prefetched.argtypes = [vp]
     lib.mes_pool_stats.restype = c_int
     lib.mes_pool_stats.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
+    kvp, sqp, fl = ctypes.POINTER(mes_kv), ctypes.POINTER(mes_seqs), ctypes.c_float
+    lib.mes_kv_append.restype = c_int
+    lib.mes_kv_append.argtypes = [kvp, c_int, sqp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, c_int, vp, c_int, vp]
+    lib.mes_attn_prompt.restype = c_int
+    lib.mes_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, c_int, c_int, c_int, c_int, c_int, fl, vp, c_int, vp]
+    lib.mes_attn_extend.restype = c_int
+    lib.mes_attn_extend.argtypes = [kvp, c_int, sqp, vp, c_int, c_int, c_int, fl, vp, c_int, vp]
+    lib.mes_attn_decode_workspace_bytes.restype = c_sz
+    lib.mes_attn_decode_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
+    lib.mes_attn_decode.restype = c_int
+    lib.mes_attn_decode.argtypes = [kvp, c_int, sqp, vp, c_int, c_int, c_int, i32p, i32p, fl, vp, c_int, vp, c_sz, vp]
+    lib.mes_kv_copy_pages.restype = c_int
+    lib.mes_kv_copy_pages.argtypes = [kvp, i32p, i32p, c_int, vp]
+    lib.mes_pages_create.restype = c_int
+    lib.mes_pages_create.argtypes = [c_int, c_int, c_int, c_int, ctypes.POINTER(vp)]
+    lib.mes_pages_destroy.restype = None
+    lib.mes_pages_destroy.argtypes = [vp]
+    lib.mes_pages_grow.restype = c_int
+    lib.mes_pages_grow.argtypes = [vp, i32p, i32p, c_int, i32p, i32p, ctypes.POINTER(c_int)]
+    lib.mes_pages_fork.restype = c_int
+    lib.mes_pages_fork.argtypes = [vp, c_int, c_int, c_int]
+    lib.mes_pages_free.restype = c_int
+    lib.mes_pages_free.argtypes = [vp, c_int]
+    lib.mes_pages_compact.restype = c_int
+    lib.mes_pages_compact.argtypes = [vp, i32p, i32p, ctypes.POINTER(c_int)]
+    lib.mes_pages_table.restype = c_int
+    lib.mes_pages_table.argtypes = [vp, i32p, c_int, vp, c_int, vp]
+    lib.mes_pages_length.restype = c_int
+    lib.mes_pages_length.argtypes = [vp, c_int]
+    lib.mes_pages_unused.restype = c_int
+    lib.mes_pages_unused.argtypes = [vp]
     return lib
 
 
@@ -521,6 +568,225 @@ class ExpertPool:
     def __del__(self):
         if getattr(self, "handle", None):
             lib.mes_pool_destroy(self.handle)
+            self.handle = None
+
+
+# ---------------------------------------------------------------------------------------- attention and its paged cache
+
+def _call_on(device: torch.device, entry, *args) -> None:
+    """entry(*args, stream) on the device's current stream, with that device current during the call."""
+    if torch.cuda.current_device() == device.index:
+        _check(entry(*args, torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(entry(*args, torch.cuda.current_stream(device).cuda_stream))
+
+
+def _heads_of(name: str, t: torch.Tensor, device: torch.device) -> int:
+    """Checks rows [T, heads, head_dim] of bf16 whose heads lie one behind the other; returns how far rows are apart."""
+    assert t.dtype == torch.bfloat16 and t.dim() == 3 and t.device == device, f"{name}: bf16 [T, heads, head_dim] on {device}"
+    heads, dim = t.shape[1], t.shape[2]
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), f"{name}: the heads of a row lie one behind the other"
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def _int32_on(name: str, t: torch.Tensor, device: torch.device) -> None:
+    assert t.dtype == torch.int32 and t.is_contiguous() and t.device == device, f"{name}: contiguous int32 on {device}"
+
+
+class KvCache:
+    """A paged cache of keys and values for all layers of a model (mes_kv in mes.h): k and v are
+    [n_layers, n_pages, n_kv_heads, page_tokens, head_dim], bf16, or float8_e4m3fn with one fp32 scale per layer and head."""
+
+    def __init__(self, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, dtype: int = KV_BF16,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda:0"):
+        shape = (n_layers, n_pages, n_kv_heads, page_tokens, head_dim)
+        kind = torch.float8_e4m3fn if dtype == KV_E4M3 else torch.bfloat16
+        self._set(torch.zeros(shape, dtype=torch.uint8 if dtype == KV_E4M3 else kind, device=device).view(kind),
+                  torch.zeros(shape, dtype=torch.uint8 if dtype == KV_E4M3 else kind, device=device).view(kind), k_scale, v_scale)
+
+    @classmethod
+    def over(cls, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        """A cache over tensors that are there already."""
+        self = cls.__new__(cls)
+        self._set(k, v, k_scale, v_scale)
+        return self
+
+    def _set(self, k, v, k_scale, v_scale):
+        assert k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous() and k.is_cuda and k.device == v.device
+        assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn), "a cache is bf16 or float8_e4m3fn"
+        fp8 = k.dtype == torch.float8_e4m3fn
+        for t in (k_scale, v_scale):
+            assert (t is not None) == fp8, "scales belong to an e4m3 cache"
+            assert t is None or (t.dtype == torch.float32 and t.shape == (k.shape[0], k.shape[2]) and t.is_contiguous() and t.device == k.device)
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.desc = mes_kv(self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, KV_E4M3 if fp8 else KV_BF16,
+                           k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if fp8 else None, v_scale.data_ptr() if fp8 else None)
+        self.ref = ctypes.byref(self.desc)
+
+
+class SeqBatch:
+    """The sequences of a call (mes_seqs in mes.h): kv_len int32 [n], page_table int32 [n, pages], q_offsets int32 [n + 1] or
+    None (one row per sequence), all on the GPU; their contents may change between calls."""
+
+    def __init__(self, kv_len: torch.Tensor, page_table: torch.Tensor, q_offsets: Optional[torch.Tensor] = None):
+        self.device = kv_len.device
+        n = kv_len.shape[0]
+        _int32_on("kv_len", kv_len, self.device)
+        _int32_on("page_table", page_table, self.device)
+        assert kv_len.is_cuda and kv_len.dim() == 1 and page_table.dim() == 2 and page_table.shape[0] == n
+        if q_offsets is not None:
+            _int32_on("q_offsets", q_offsets, self.device)
+            assert q_offsets.shape == (n + 1,)
+        self.kv_len, self.page_table, self.q_offsets, self.n = kv_len, page_table, q_offsets, n
+        self.desc = mes_seqs(n, page_table.shape[1], None if q_offsets is None else q_offsets.data_ptr(), kv_len.data_ptr(), page_table.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+
+def rotary_table(n_positions: int, head_dim: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
+    """Cosines and sines [n_positions, 2, head_dim / 2] for mes_kv_append; angles in fp64 (they pass what fp32 resolves)."""
+    angle = torch.arange(n_positions, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, head_dim, 2, dtype=torch.float64) / head_dim)
+    return torch.stack([angle.cos(), angle.sin()], 1).to(device=device, dtype=torch.float32)
+
+
+def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                  rotary: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Rotates the new rows' queries (returned; q_out may be q) and keys and puts keys and values into the cache's pages."""
+    dev, T = cache.device, k.shape[0]
+    assert batch.device == dev and v.shape == k.shape and k.shape[1:] == (cache.n_kv_heads, cache.head_dim)
+    ld_k, ld_v = _heads_of("k", k, dev), _heads_of("v", v, dev)
+    heads = ld_q = ld_o = n_pos = 0
+    if rotary is not None:
+        assert rotary.dtype == torch.float32 and rotary.is_contiguous() and rotary.device == dev and rotary.shape[1:] == (2, cache.head_dim // 2)
+        n_pos = rotary.shape[0]
+    if q is not None:
+        assert q.shape[0] == T and q.shape[2] == cache.head_dim
+        heads, ld_q = q.shape[1], _heads_of("q", q, dev)
+        if q_out is None:
+            q_out = torch.empty((T, heads, cache.head_dim), dtype=torch.bfloat16, device=dev)
+        assert q_out.shape == q.shape
+        ld_o = _heads_of("q_out", q_out, dev)
+    _call_on(dev, lib.mes_kv_append, cache.ref, layer, batch.ref, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), T, heads,
+             ld_q, ld_k, ld_v, None if rotary is None else rotary.data_ptr(), n_pos, None if q is None else q_out.data_ptr(), ld_o)
+    return q_out if q is not None else None
+
+
+def mes_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None) -> torch.Tensor:
+    """Causal attention over packed prompts: q [T, heads, d], k and v [T, kv heads, d] (views of one buffer are fine),
+    seq_offsets int32 [n + 1] on the GPU.  Returns [T, heads, d]; rows behind the last sequence are left as they are."""
+    dev = q.device
+    T, heads, dim = q.shape
+    assert q.is_cuda and k.shape == v.shape and k.shape[0] == T and k.shape[2] == dim
+    _int32_on("seq_offsets", seq_offsets, dev)
+    if out is None:
+        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
+    assert out.shape == q.shape
+    _call_on(dev, lib.mes_attn_prompt, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, seq_offsets.shape[0] - 1, seq_offsets.data_ptr(),
+             heads, k.shape[1], dim, _heads_of("q", q, dev), _heads_of("k", k, dev), _heads_of("v", v, dev),
+             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev))
+    return out
+
+
+def mes_attn_extend(cache: KvCache, layer: int, batch: SeqBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None) -> torch.Tensor:
+    """Causal attention of the batch's new rows (its last tokens, already appended) over the cache."""
+    dev = cache.device
+    T, heads, dim = q.shape
+    assert batch.device == dev and dim == cache.head_dim
+    if out is None:
+        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
+    assert out.shape == q.shape
+    _call_on(dev, lib.mes_attn_extend, cache.ref, layer, batch.ref, q.data_ptr(), T, heads, _heads_of("q", q, dev),
+             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev))
+    return out
+
+
+class AttnDecode:
+    """mes_attn_decode with its workspace, for up to max_seqs sequences; all layers of a model can share one."""
+
+    def __init__(self, cache: KvCache, n_heads: int, max_seqs: int = 64, workspace: Optional[torch.Tensor] = None):
+        self.cache, self.n_heads = cache, n_heads
+        n = max(lib.mes_attn_decode_workspace_bytes(max_seqs, n_heads, cache.n_kv_heads, cache.head_dim), 16)
+        self.ws = workspace if workspace is not None else torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+    def __call__(self, layer: int, batch: SeqBatch, q: torch.Tensor, seg_offsets: Optional[Sequence[int]] = None,
+                 prefix_len: Optional[Sequence[int]] = None, out: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
+        """q [n, heads, d], one row per sequence.  seg_offsets [E + 1] and prefix_len [E] (host): rows are sorted by expert and
+        the sequences of expert e share their first prefix_len[e] tokens, which are then read once."""
+        dev = self.cache.device
+        n, heads, dim = q.shape
+        assert batch.device == dev and n == batch.n and heads == self.n_heads and dim == self.cache.head_dim
+        if out is None:
+            out = torch.empty((n, heads, dim), dtype=torch.bfloat16, device=dev)
+        assert out.shape == q.shape
+        E, seg, pre = 0, None, None
+        if seg_offsets is not None:
+            E = len(prefix_len)
+            assert len(seg_offsets) == E + 1
+            seg, pre = (ctypes.c_int32 * (E + 1))(*seg_offsets), (ctypes.c_int32 * E)(*prefix_len)
+        _call_on(dev, lib.mes_attn_decode, self.cache.ref, layer, batch.ref, q.data_ptr(), heads, _heads_of("q", q, dev), E, seg, pre,
+                 dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev), self.ws.data_ptr(), self.ws.numel())
+        return out
+
+
+def mes_kv_copy_pages(cache: KvCache, src: Sequence[int], dst: Sequence[int]) -> None:
+    """Copies page src[i] to page dst[i] in all layers of keys and values (what PagePool.grow and .compact ask for)."""
+    n = len(src)
+    assert len(dst) == n
+    _call_on(cache.device, lib.mes_kv_copy_pages, cache.ref, (ctypes.c_int32 * n)(*src), (ctypes.c_int32 * n)(*dst), n)
+
+
+class PagePool:
+    """Which pages of a cache hold which sequence (mes_pages_* in mes.h; host bookkeeping only)."""
+
+    def __init__(self, n_pages: int, page_tokens: int, max_seqs: int, max_seq_pages: Optional[int] = None):
+        self.n_pages, self.page_tokens, self.max_seqs = n_pages, page_tokens, max_seqs
+        self.max_seq_pages = n_pages if max_seq_pages is None else max_seq_pages
+        h = ctypes.c_void_p()
+        _check(lib.mes_pages_create(n_pages, page_tokens, max_seqs, self.max_seq_pages, ctypes.byref(h)))
+        self.handle = h
+
+    def grow(self, seqs: Sequence[int], n_tokens: Sequence[int]):
+        """More tokens for each of the sequences; returns (src, dst): pages to copy before the tokens are appended."""
+        n = len(seqs)
+        assert len(n_tokens) == n
+        arr, count = ctypes.c_int32 * max(n, 1), ctypes.c_int(0)
+        src, dst = arr(), arr()
+        _check(lib.mes_pages_grow(self.handle, arr(*seqs), arr(*n_tokens), n, src, dst, ctypes.byref(count)))
+        return src[: count.value], dst[: count.value]
+
+    def fork(self, parent: int, child: int, n_tokens: Optional[int] = None) -> None:
+        _check(lib.mes_pages_fork(self.handle, parent, child, self.length(parent) if n_tokens is None else n_tokens))
+
+    def free(self, seq: int) -> None:
+        _check(lib.mes_pages_free(self.handle, seq))
+
+    def compact(self):
+        """Moves the pages in use to the lowest ids; returns (src, dst) to copy.  Tables taken before are out of date."""
+        arr, count = ctypes.c_int32 * max(self.n_pages // 2, 1), ctypes.c_int(0)
+        src, dst = arr(), arr()
+        _check(lib.mes_pages_compact(self.handle, src, dst, ctypes.byref(count)))
+        return src[: count.value], dst[: count.value]
+
+    def table(self, seqs: Sequence[int], table_pages: Optional[int] = None):
+        """Host tensors (page_table [n, table_pages], kv_len [n]) of the sequences."""
+        n = len(seqs)
+        table = torch.empty((n, self.max_seq_pages if table_pages is None else table_pages), dtype=torch.int32)
+        length = torch.empty(n, dtype=torch.int32)
+        _check(lib.mes_pages_table(self.handle, (ctypes.c_int32 * max(n, 1))(*seqs), n, table.data_ptr() or None, table.shape[1], length.data_ptr() or None))
+        return table, length
+
+    def length(self, seq: int) -> int:
+        return lib.mes_pages_length(self.handle, seq)
+
+    def unused(self) -> int:
+        return lib.mes_pages_unused(self.handle)
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            lib.mes_pages_destroy(self.handle)
             self.handle = None
 
 

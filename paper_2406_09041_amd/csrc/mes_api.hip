@@ -1,9 +1,10 @@
 // extern "C" entry points: argument validation on the host (before any HIP call), then launch.
-#include "mes_internal.h"
+#include "mes_attn.h"
 #include "mes_bench.h"
 
 #include <cstdarg>
 #include <cstdio>
+#include <vector>
 
 namespace mes {
 
@@ -284,6 +285,204 @@ mes_status mes_copy_probe(void* dst, const void* src, size_t bytes, void* stream
   if (!dst || !src) return fail(MES_ERR_NULL, "mes_copy_probe: null buffer");
   if (bytes % 16 || ((uintptr_t)dst | (uintptr_t)src) % 16) return fail(MES_ERR_ALIGN, "mes_copy_probe: buffers and size must be multiples of 16 bytes");
   return check_hip(launch_copy_probe(dst, src, bytes, (hipStream_t)stream), "mes_copy_probe");
+}
+
+// ---- attention and its cache ---------------------------------------------------------------------------------
+
+static mes_status check_heads(const char* who, int n_heads, int n_kv_heads, int head_dim) {
+  if (head_dim != 64 && head_dim != 128) return fail(MES_ERR_SHAPE, "%s: head_dim must be 64 or 128 (got %d)", who, head_dim);
+  if (n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads != 0 || n_heads / n_kv_heads > 64 || n_heads > 65535)
+    return fail(MES_ERR_SHAPE, "%s: n_heads = %d must be 1 to 64 times n_kv_heads = %d", who, n_heads, n_kv_heads);
+  return MES_OK;
+}
+
+static mes_status check_rows(const char* who, const char* what, const void* p, int ld, int heads, int head_dim) {
+  if (!p) return fail(MES_ERR_NULL, "%s: %s is null", who, what);
+  if (!aligned16(p)) return fail(MES_ERR_ALIGN, "%s: %s must be 16-byte aligned", who, what);
+  if (ld < (int64_t)heads * head_dim || ld % 8 != 0) return fail(MES_ERR_SHAPE, "%s: rows of %s are %d apart: a multiple of 8, %d or more", who, what, ld, heads * head_dim);
+  return MES_OK;
+}
+
+static mes_status check_kv(const char* who, const mes_kv* kv, int layer) {
+  if (!kv) return fail(MES_ERR_NULL, "%s: kv is null", who);
+  if (kv->dtype != MES_KV_BF16 && kv->dtype != MES_KV_E4M3) return fail(MES_ERR_BITS, "%s: unknown cache type %d", who, kv->dtype);
+  if (kv->n_layers < 1 || kv->n_pages < 1) return fail(MES_ERR_SHAPE, "%s: n_layers = %d, n_pages = %d must be positive", who, kv->n_layers, kv->n_pages);
+  if (kv->page_tokens < 16 || kv->page_tokens > 256 || (kv->page_tokens & (kv->page_tokens - 1)))
+    return fail(MES_ERR_SHAPE, "%s: page_tokens must be 16, 32, 64, 128 or 256 (got %d)", who, kv->page_tokens);
+  if (mes_status st = check_heads(who, kv->n_kv_heads, kv->n_kv_heads, kv->head_dim)) return st;
+  if (!kv->k || !kv->v) return fail(MES_ERR_NULL, "%s: the cache's k / v is null", who);
+  if (!aligned16(kv->k) || !aligned16(kv->v)) return fail(MES_ERR_ALIGN, "%s: the cache must be 16-byte aligned", who);
+  if (kv->dtype == MES_KV_E4M3 && (!kv->k_scale || !kv->v_scale)) return fail(MES_ERR_NULL, "%s: an e4m3 cache needs k_scale and v_scale", who);
+  if (layer < 0 || layer >= kv->n_layers) return fail(MES_ERR_SHAPE, "%s: layer %d outside [0, %d)", who, layer, kv->n_layers);
+  return MES_OK;
+}
+
+static mes_status check_seqs(const char* who, const mes_kv* kv, const mes_seqs* s, bool offsets) {
+  if (!s) return fail(MES_ERR_NULL, "%s: seqs is null", who);
+  if (s->n_seqs < 0 || s->n_seqs > MES_MAX_SEQS) return fail(MES_ERR_SHAPE, "%s: n_seqs = %d outside [0, %d]", who, s->n_seqs, MES_MAX_SEQS);
+  if (s->n_seqs == 0) return MES_OK;
+  if (!s->kv_len || !s->page_table || (offsets && !s->q_offsets)) return fail(MES_ERR_NULL, "%s: a pointer in seqs is null", who);
+  if (s->table_pages < 1 || (int64_t)s->table_pages * kv->page_tokens > 0x7fffff00)
+    return fail(MES_ERR_SHAPE, "%s: table_pages = %d of %d tokens", who, s->table_pages, kv->page_tokens);
+  return MES_OK;
+}
+
+static size_t kv_layer_bytes(const mes_kv& kv) {
+  return (size_t)kv.n_pages * kv.n_kv_heads * kv.page_tokens * kv.head_dim * (kv.dtype == MES_KV_E4M3 ? 1 : 2);
+}
+static int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
+
+mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                         int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
+                         int ld_q_out, void* stream) {
+  static const char who[] = "mes_kv_append";
+  if (mes_status st = check_kv(who, kv, layer)) return st;
+  if (mes_status st = check_seqs(who, kv, seqs, false)) return st;
+  if (T < 0) return fail(MES_ERR_SHAPE, "%s: T = %d is negative", who, T);
+  if (!seqs->q_offsets && T > seqs->n_seqs) return fail(MES_ERR_SEGMENTS, "%s: %d rows of %d sequences without q_offsets", who, T, seqs->n_seqs);
+  if (T == 0 || seqs->n_seqs == 0) return MES_OK;
+  if ((q == nullptr) != (q_out == nullptr)) return fail(MES_ERR_NULL, "%s: give both of q and q_out or neither", who);
+  if (q && !rotary) return fail(MES_ERR_NULL, "%s: q needs rotary", who);
+  if (mes_status st = check_rows(who, "k", k, ld_k, kv->n_kv_heads, kv->head_dim)) return st;
+  if (mes_status st = check_rows(who, "v", v, ld_v, kv->n_kv_heads, kv->head_dim)) return st;
+  if (q) {
+    if (n_heads < 1 || n_heads > 65535) return fail(MES_ERR_SHAPE, "%s: n_heads = %d", who, n_heads);
+    if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, kv->head_dim)) return st;
+    if (mes_status st = check_rows(who, "q_out", q_out, ld_q_out, n_heads, kv->head_dim)) return st;
+    if (q == q_out && ld_q != ld_q_out) return fail(MES_ERR_SHAPE, "%s: q_out is q with rows %d apart instead of %d", who, ld_q_out, ld_q);
+  }
+  const int capacity = seqs->table_pages * kv->page_tokens;
+  if (rotary) {
+    if (!aligned16(rotary)) return fail(MES_ERR_ALIGN, "%s: rotary must be 16-byte aligned", who);
+    if (n_positions < capacity) return fail(MES_ERR_SHAPE, "%s: rotary has %d positions, the page table has room for %d", who, n_positions, capacity);
+  }
+  AppendArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, rotary, (uint16_t*)q_out, kv->k, kv->v, kv->k_scale, kv->v_scale,
+               seqs->q_offsets, seqs->kv_len, seqs->page_table, layer, kv->n_pages, log2_of(kv->page_tokens), n_heads, kv->n_kv_heads,
+               kv->head_dim, seqs->n_seqs, seqs->table_pages, capacity, ld_q, ld_k, ld_v, ld_q_out};
+  return check_hip(launch_append(a, T, kv->dtype == MES_KV_E4M3, (hipStream_t)stream), who);
+}
+
+mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, int n_seqs, const int32_t* seq_offsets,
+                           int n_heads, int n_kv_heads, int head_dim, int ld_q, int ld_k, int ld_v, float scale, void* out,
+                           int ld_out, void* stream) {
+  static const char who[] = "mes_attn_prompt";
+  if (mes_status st = check_heads(who, n_heads, n_kv_heads, head_dim)) return st;
+  if (n_seqs < 0 || n_seqs > MES_MAX_SEQS) return fail(MES_ERR_SHAPE, "%s: n_seqs = %d outside [0, %d]", who, n_seqs, MES_MAX_SEQS);
+  if (T < 0) return fail(MES_ERR_SHAPE, "%s: T = %d is negative", who, T);
+  if (!(scale > 0.0f) || scale > 1e30f) return fail(MES_ERR_SHAPE, "%s: scale must be positive and finite", who);
+  if (T == 0 || n_seqs == 0) return MES_OK;
+  if (!seq_offsets) return fail(MES_ERR_NULL, "%s: seq_offsets is null", who);
+  if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, head_dim)) return st;
+  if (mes_status st = check_rows(who, "k", k, ld_k, n_kv_heads, head_dim)) return st;
+  if (mes_status st = check_rows(who, "v", v, ld_v, n_kv_heads, head_dim)) return st;
+  if (mes_status st = check_rows(who, "out", out, ld_out, n_heads, head_dim)) return st;
+  PromptArgs a{};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.out = (uint16_t*)out;
+  a.q_offsets = seq_offsets;
+  a.T = T; a.n_seqs = n_seqs; a.n_heads = n_heads; a.n_kv_heads = n_kv_heads; a.head_dim = head_dim;
+  a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out; a.scale = scale;
+  return check_hip(launch_attn_prompt(a, KV_PACKED, (hipStream_t)stream), who);
+}
+
+mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, int T, int n_heads, int ld_q,
+                           float scale, void* out, int ld_out, void* stream) {
+  static const char who[] = "mes_attn_extend";
+  if (mes_status st = check_kv(who, kv, layer)) return st;
+  if (mes_status st = check_seqs(who, kv, seqs, true)) return st;
+  if (mes_status st = check_heads(who, n_heads, kv->n_kv_heads, kv->head_dim)) return st;
+  if (T < 0) return fail(MES_ERR_SHAPE, "%s: T = %d is negative", who, T);
+  if (!(scale > 0.0f) || scale > 1e30f) return fail(MES_ERR_SHAPE, "%s: scale must be positive and finite", who);
+  if (T == 0 || seqs->n_seqs == 0) return MES_OK;
+  if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, kv->head_dim)) return st;
+  if (mes_status st = check_rows(who, "out", out, ld_out, n_heads, kv->head_dim)) return st;
+  const bool fp8 = kv->dtype == MES_KV_E4M3;
+  PromptArgs a{};
+  a.q = (const uint16_t*)q; a.out = (uint16_t*)out;
+  a.k = (const uint16_t*)((const char*)kv->k + layer * kv_layer_bytes(*kv));
+  a.v = (const uint16_t*)((const char*)kv->v + layer * kv_layer_bytes(*kv));
+  if (fp8) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  a.q_offsets = seqs->q_offsets; a.kv_len = seqs->kv_len; a.page_table = seqs->page_table;
+  a.T = T; a.n_seqs = seqs->n_seqs; a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads; a.head_dim = kv->head_dim;
+  a.n_pages = kv->n_pages; a.page_shift = log2_of(kv->page_tokens); a.table_pages = seqs->table_pages;
+  a.capacity = seqs->table_pages * kv->page_tokens;
+  a.ld_q = ld_q; a.ld_out = ld_out; a.scale = scale;
+  return check_hip(launch_attn_prompt(a, fp8 ? KV_PAGED_E4M3 : KV_PAGED, (hipStream_t)stream), who);
+}
+
+size_t mes_attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
+  if (n_seqs < 1 || n_seqs > MES_MAX_SEQS || n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || n_heads / n_kv_heads > 64 ||
+      n_heads > 65535 || (head_dim != 64 && head_dim != 128))
+    return 0;
+  return attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim);
+}
+
+mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, int n_heads, int ld_q,
+                           int n_experts, const int32_t* seg_offsets, const int32_t* prefix_len, float scale, void* out,
+                           int ld_out, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char who[] = "mes_attn_decode";
+  if (mes_status st = check_kv(who, kv, layer)) return st;
+  if (mes_status st = check_seqs(who, kv, seqs, false)) return st;
+  if (mes_status st = check_heads(who, n_heads, kv->n_kv_heads, kv->head_dim)) return st;
+  if (!(scale > 0.0f) || scale > 1e30f) return fail(MES_ERR_SHAPE, "%s: scale must be positive and finite", who);
+  if (seqs->n_seqs == 0) return MES_OK;
+  if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, kv->head_dim)) return st;
+  if (mes_status st = check_rows(who, "out", out, ld_out, n_heads, kv->head_dim)) return st;
+  if ((seg_offsets == nullptr) != (prefix_len == nullptr)) return fail(MES_ERR_NULL, "%s: give both of seg_offsets and prefix_len or neither", who);
+  DecodeArgs a{};
+  if (seg_offsets) {
+    if (n_experts < 1 || n_experts > MES_MAX_EXPERTS) return fail(MES_ERR_SHAPE, "%s: n_experts = %d outside [1, %d]", who, n_experts, MES_MAX_EXPERTS);
+    if (seg_offsets[0] != 0) return fail(MES_ERR_SEGMENTS, "%s: seg_offsets[0] must be 0 (got %d)", who, seg_offsets[0]);
+    for (int e = 0; e < n_experts; ++e) {
+      if (seg_offsets[e + 1] < seg_offsets[e]) return fail(MES_ERR_SEGMENTS, "%s: seg_offsets decreases at %d", who, e + 1);
+      if (prefix_len[e] < 0) return fail(MES_ERR_SEGMENTS, "%s: prefix_len[%d] = %d is negative", who, e, prefix_len[e]);
+    }
+    if (seg_offsets[n_experts] != seqs->n_seqs)
+      return fail(MES_ERR_SEGMENTS, "%s: seg_offsets[%d] = %d, expected n_seqs = %d", who, n_experts, seg_offsets[n_experts], seqs->n_seqs);
+    // an expert with one sequence or without a prefix shares nothing: only the others are handed on
+    for (int e = 0; e < n_experts; ++e) {
+      if (seg_offsets[e + 1] - seg_offsets[e] < 2 || prefix_len[e] == 0) continue;
+      a.first[a.n_groups] = seg_offsets[e];
+      a.behind[a.n_groups] = seg_offsets[e + 1];
+      a.prefix[a.n_groups++] = prefix_len[e];
+    }
+  }
+  // units of work are numbered in 32 bits (an expert's shared prefix has at most two passes per sequence)
+  if ((int64_t)3 * seqs->n_seqs * kv->n_kv_heads * (seqs->table_pages * kv->page_tokens / 128 + 2) > 0x40000000)
+    return fail(MES_ERR_SHAPE, "%s: %d page tables of %d pages are more than one call takes", who, seqs->n_seqs, seqs->table_pages);
+  const size_t need = attn_decode_workspace_bytes(seqs->n_seqs, n_heads, kv->n_kv_heads, kv->head_dim);
+  if (!workspace || workspace_bytes < need) return fail(MES_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, need);
+  if (!aligned16(workspace)) return fail(MES_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+  const bool fp8 = kv->dtype == MES_KV_E4M3;
+  a.q = (const uint16_t*)q; a.out = (uint16_t*)out;
+  a.k = (const char*)kv->k + layer * kv_layer_bytes(*kv);
+  a.v = (const char*)kv->v + layer * kv_layer_bytes(*kv);
+  if (fp8) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  a.kv_len = seqs->kv_len; a.page_table = seqs->page_table; a.ws = workspace;
+  a.n_seqs = seqs->n_seqs; a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads; a.head_dim = kv->head_dim; a.n_pages = kv->n_pages;
+  a.page_shift = log2_of(kv->page_tokens); a.table_pages = seqs->table_pages; a.capacity = seqs->table_pages * kv->page_tokens;
+  a.ld_q = ld_q; a.ld_out = ld_out; a.scale = scale;
+  return check_hip(launch_attn_decode(a, fp8, (hipStream_t)stream), who);
+}
+
+mes_status mes_kv_copy_pages(const mes_kv* kv, const int32_t* src, const int32_t* dst, int n, void* stream) {
+  static const char who[] = "mes_kv_copy_pages";
+  if (mes_status st = check_kv(who, kv, 0)) return st;
+  if (n < 0 || n > kv->n_pages) return fail(MES_ERR_SHAPE, "%s: n = %d outside [0, %d]", who, n, kv->n_pages);
+  if (n == 0) return MES_OK;
+  if (!src || !dst) return fail(MES_ERR_NULL, "%s: src / dst is null", who);
+  try {
+    std::vector<int32_t> written(dst, dst + n);
+    std::sort(written.begin(), written.end());
+    for (int i = 0; i < n; ++i) {
+      if (src[i] < 0 || src[i] >= kv->n_pages || dst[i] < 0 || dst[i] >= kv->n_pages)
+        return fail(MES_ERR_PAGES, "%s: pair %d is page %d to page %d of %d", who, i, src[i], dst[i], kv->n_pages);
+      if (i && written[i] == written[i - 1]) return fail(MES_ERR_PAGES, "%s: page %d is written twice", who, written[i]);
+      if (std::binary_search(written.begin(), written.end(), src[i])) return fail(MES_ERR_PAGES, "%s: page %d is read and written", who, src[i]);
+    }
+  } catch (...) {
+    return fail(MES_ERR_DEVICE, "%s: out of host memory", who);
+  }
+  return check_hip(launch_copy_pages(*kv, src, dst, n, (hipStream_t)stream), who);
 }
 
 }  // extern "C"

@@ -1,0 +1,554 @@
+// One token of every sequence against the paged cache, prefixes that an expert's sequences share read once.  Bound by HBM:
+// every distinct cached token is read once, 2 head_dim values per key / value head, for 4 head_dim n_heads operations.
+//
+// Work is a flat line of units (kUnit = 128 tokens of one key / value head): per key / value head first the shared
+// prefixes (once per pass of up to 64 query rows), then what every sequence has of its own.  The line is cut into equal
+// chunks, one per workgroup, wherever that falls: the workgroups are equally busy however the lengths are spread, also for one long
+// sequence, and the launch does not depend on the lengths, which stay on the device (every workgroup adds them up for itself).  A
+// piece of the line that does not cover a sequence alone leaves (max, sum, weighted values) in the workspace, and k_join
+// adds the pieces of a row in their order.
+//
+// A wavefront takes 32 tokens at a time with all query rows of the unit (up to 4 tiles of 16).  Scores are formed transposed,
+// S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K's operand is 16 tokens x 8 dimensions per lane straight from memory, and the
+// result holds one query row (lane & 15) and tokens 4 g + (0..3) per lane (g = lane / 16), which rounded to bf16 IS the operand P^T of
+// O^T = V^T P^T over the 32 tokens in the order (4 g + i, 16 + 4 g + i).  V is read by rows, 16 lanes a row, lane r the
+// dimensions VD r .. VD r + VD - 1 of its 8 tokens: product j of VD then yields the dimensions VD m + j, and its operand is pairs of
+// 16-bit halves put together, one v_perm each.  So neither keys nor values pass through LDS.  Of the 16 columns of a tile 4
+// (n_heads / n_kv_heads) are used where nothing is shared: the matrix cores are idle most of the time anyway.
+#include "mes_attn_common.h"
+
+namespace mes {
+namespace {
+
+constexpr int kThreads = 256, kUnit = 128, kRowsPass = 64, kWorkgroups = 512;
+
+struct Shape {                       // what host and device derive alike
+  int group, per_pass, n_passes;     // query heads per key / value head, sequences per pass, passes of all groups
+};
+
+// partial results: [slot][rows][D] floats, then [slot][rows] (max, sum)
+struct Partials {
+  float* o;
+  float2* ml;
+};
+
+struct Layout {
+  size_t prefix_o, prefix_ml, own_o, own_ml, meta, total;
+};
+
+__host__ __device__ inline Layout layout(int n_seqs, int n_kv_heads, int group, int n_passes, int head_dim) {
+  const size_t pre = (size_t)(n_passes ? kWorkgroups + n_kv_heads * n_passes : 0) * kRowsPass;
+  const size_t own = (size_t)(kWorkgroups + n_kv_heads * n_seqs) * group;
+  Layout y;
+  y.prefix_o = 0;
+  y.own_o = y.prefix_o + pre * head_dim * 4;
+  y.prefix_ml = y.own_o + own * head_dim * 4;
+  y.own_ml = y.prefix_ml + pre * 8;
+  y.meta = (y.own_ml + own * 8 + 15) & ~(size_t)15;
+  y.total = y.meta + (size_t)n_kv_heads * n_seqs * sizeof(int4);
+  return y;
+}
+
+// where a (key / value head, sequence) finds its pieces: x first slot of its own part, y their number (-1: the row is
+// written already), z first slot of the shared prefix, w number of those | row in the pass << 16
+typedef int4 Meta;
+
+struct DecodeCall {
+  DecodeArgs a;
+  Shape sh;
+  int pass_base[MES_MAX_EXPERTS];
+};
+
+template <int D, bool FP8>
+struct Raw {                                        // 32 tokens of keys and values on their way
+  static constexpr int VD = D / 16, KC = FP8 ? D / 64 : D / 32, VW = VD * (FP8 ? 1 : 2) / 4;
+  u32x4 k[2][KC];
+  uint32_t v[8][VW];
+};
+
+// first dimension of the 8 that a lane holds in product c of K Q^T
+template <int D, bool FP8>
+__device__ __forceinline__ int dim_of(int c, int g) {
+  return FP8 ? 64 * (c / 2) + 16 * g + 8 * (c % 2) : 32 * c + 8 * g;
+}
+
+struct Segment {                                    // a piece of the line
+  int seq, seq0, rows;                              // page table; sequence of row 0; query rows
+  int from, to, t0, t1;                             // tokens of [from, to) in the steps [t0, t1), t0 a multiple of 32
+};
+
+template <int D, bool FP8>
+struct Shared {
+  float merge[4][16][D + 4];
+  u32x4 q[4][D / 32][64];
+  float2 ml[4][kRowsPass];
+  int cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
+  int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: fewer than two are
+  int part[4];
+};
+
+// The weighted sum over one piece, all query rows, into o / ml (or out where the piece is all that its rows see).
+template <int D, bool FP8, int NT>
+__device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D, FP8>& sh, bool direct, float* o, float2* ml_out) {
+  constexpr int VD = D / 16, KS = D / 32;
+  typedef Raw<D, FP8> R;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+
+  // Q^T operands: one tile in registers, more in LDS
+  u32x4 q1[KS];
+  __syncthreads();                                  // the last piece's reads of LDS are over
+  for (int nt = NT == 1 ? 0 : wave; nt < NT; nt += NT == 1 ? 1 : 4) {
+    const int row = 16 * nt + col;
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      u32x4 w = {0, 0, 0, 0};
+      if (row < g.rows)
+        w = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + row / group) * a.ld_q + (size_t)(kvh * group + row % group) * D + dim_of<D, FP8>(c, quad));
+      if constexpr (NT == 1) q1[c] = w; else sh.q[nt][c][lane] = w;
+    }
+  }
+  if constexpr (NT > 1) __syncthreads();
+
+  const float scale = a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f);
+  const int32_t* table = a.page_table + (size_t)g.seq * a.table_pages;
+  f32x4 acc[NT][VD];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt] = -INFINITY;
+    l[nt] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < VD; ++j) acc[nt][j] = f32x4{0, 0, 0, 0};
+  }
+
+  // the pages of this wavefront's next 64 steps, one step per lane
+  const int n_steps = (g.t1 - g.t0 + 31) / 32, mine = (n_steps - wave + 3) / 4;   // steps wave, wave + 4, ...
+  int pages[2] = {-1, -1};
+  auto look_up = [&](int first) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int t = g.t0 + (4 * (first + lane) + wave) * 32 + 16 * h;
+      pages[h] = first + lane < mine && t < g.to ? table[t >> a.page_shift] : -1;
+    }
+  };
+  R raw;
+  int there[2];                                     // pages of the step in `raw`
+  auto request_k = [&](int i, int (&pg)[2]) {
+    const int t = g.t0 + (4 * i + wave) * 32;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      pg[h] = __builtin_amdgcn_readlane(pages[h], i & 63);
+      const int page = (unsigned)pg[h] < (unsigned)a.n_pages ? pg[h] : 0;
+      const size_t at = ((((size_t)page * a.n_kv_heads + kvh) << a.page_shift) + ((t + 16 * h) & ((1 << a.page_shift) - 1)) + col) * D;
+#pragma unroll
+      for (int c = 0; c < R::KC; ++c) {
+        if constexpr (FP8) raw.k[h][c] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.k) + at + 64 * c + 16 * quad);
+        else raw.k[h][c] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.k) + at + 32 * c + 8 * quad);
+      }
+    }
+  };
+  auto request_v = [&](int i, const int (&pg)[2]) {
+    const int t = g.t0 + (4 * i + wave) * 32;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int page = (unsigned)pg[h] < (unsigned)a.n_pages ? pg[h] : 0;
+      const size_t at = ((((size_t)page * a.n_kv_heads + kvh) << a.page_shift) + ((t + 16 * h) & ((1 << a.page_shift) - 1)) + 4 * quad) * D + VD * col;
+      typedef uint32_t words __attribute__((ext_vector_type(R::VW)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const void* p = FP8 ? (const void*)(static_cast<const uint8_t*>(a.v) + at + e * D) : (const void*)(static_cast<const uint16_t*>(a.v) + at + e * D);
+        if constexpr (R::VW == 1) raw.v[4 * h + e][0] = *reinterpret_cast<const uint32_t*>(p);
+        else {
+          const words w = *reinterpret_cast<const words*>(p);
+#pragma unroll
+          for (int x = 0; x < R::VW; ++x) raw.v[4 * h + e][x] = w[x];
+        }
+      }
+    }
+  };
+
+  if (mine > 0) {
+    look_up(0);
+    request_k(0, there);
+    request_v(0, there);
+  }
+  for (int i = 0; i < mine; ++i) {
+    const int t = g.t0 + (4 * i + wave) * 32;
+    const bool ok0 = (unsigned)there[0] < (unsigned)a.n_pages, ok1 = (unsigned)there[1] < (unsigned)a.n_pages;
+    const bool whole = ok0 && ok1 && t >= g.from && t + 32 <= g.to;
+    auto seen = [&](int h, int e) {                 // token e of the lane's four in half h
+      const int tok = t + 16 * h + 4 * quad + e;
+      return (h ? ok1 : ok0) && tok >= g.from && tok < g.to;
+    };
+    u32x4 p[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+#pragma unroll
+      for (int c = 0; c < KS; ++c) {
+        u32x4 qc;
+        if constexpr (NT == 1) qc = q1[c]; else qc = sh.q[nt][c][lane];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 kc;
+          if constexpr (FP8) {
+            const u32x2 x = widen4(raw.k[h][c / 2][2 * (c % 2)]), y = widen4(raw.k[h][c / 2][2 * (c % 2) + 1]);
+            kc = u32x4{x[0], x[1], y[0], y[1]};
+          } else kc = raw.k[h][c];
+          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc), __builtin_bit_cast(bf16x8, qc), s[h], 0, 0, 0);
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!seen(h, e)) s[h][e] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * scale;
+      if (__any(top > m[nt] + kSlack)) {
+        top = fmaxf(top, other_row16(top));
+        top = fmaxf(top, other_half(top));
+        const float raised = fmaxf(m[nt], top);
+        const float shrink = exp2_fast(m[nt] - (raised == -INFINITY ? 0.0f : raised));
+        l[nt] *= shrink;
+#pragma unroll
+        for (int j = 0; j < VD; ++j) acc[nt][j] *= shrink;
+        m[nt] = raised;
+      }
+      const float from = m[nt] == -INFINITY ? 0.0f : m[nt];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        p[nt][x] = pack2(exp2_fast(s[x / 2][2 * (x % 2)] * scale - from), exp2_fast(s[x / 2][2 * (x % 2) + 1] * scale - from));
+        l[nt] = add_pair(p[nt][x], l[nt]);          // the sum of what is multiplied with V
+      }
+    }
+    int next[2] = {-1, -1};
+    const bool more = i + 1 < mine;
+    if (more) {
+      if (((i + 1) & 63) == 0) look_up(i + 1);
+      request_k(i + 1, next);
+    }
+    if (!whole) {                                   // what no row sees must not turn a weight of 0 into NaN
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int x = 0; x < R::VW; ++x)
+          if (!seen(e / 4, e % 4)) raw.v[e][x] = 0;
+    }
+#pragma unroll
+    for (int jw = 0; jw < VD / 2; ++jw) {           // dimensions VD m + 2 jw and + 1
+      uint32_t pair[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (FP8) pair[e] = widen4(raw.v[e][jw / 2])[jw % 2];
+        else pair[e] = raw.v[e][jw];
+      }
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        u32x4 v;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], odd ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          acc[nt][2 * jw + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p[nt]), acc[nt][2 * jw + odd], 0, 0, 0);
+      }
+    }
+    if (more) request_v(i + 1, next);
+    there[0] = next[0];
+    there[1] = next[1];
+  }
+
+  // ---- the four wavefronts' results on one maximum, added in their order
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] += other_row16(l[nt]);
+    l[nt] += other_half(l[nt]);
+    if (lane < 16) sh.ml[wave][16 * nt + lane] = make_float2(m[nt], l[nt]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, sh.ml[w][16 * nt + col].x);
+    const float shrink = exp2_fast(m[nt] - (top == -INFINITY ? 0.0f : top));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float* to = &sh.merge[wave][col][VD * (4 * quad + i)];
+#pragma unroll
+      for (int j = 0; j < VD; j += 4)
+        *reinterpret_cast<f32x4*>(to + j) = f32x4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * shrink;
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 4, row = 16 * nt + r, d0 = (threadIdx.x & 15) * VD;
+    if (row < g.rows) {
+      float lr = 0.0f, mr = -INFINITY, x[VD];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) mr = fmaxf(mr, sh.ml[w][row].x);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) lr += sh.ml[w][row].y * exp2_fast(sh.ml[w][row].x - (mr == -INFINITY ? 0.0f : mr));
+#pragma unroll
+      for (int j = 0; j < VD; ++j) x[j] = sh.merge[0][r][d0 + j] + sh.merge[1][r][d0 + j] + sh.merge[2][r][d0 + j] + sh.merge[3][r][d0 + j];
+      if (direct) {
+        const float inv = lr == 0.0f ? 0.0f : (FP8 ? a.v_scale[kvh] : 1.0f) / lr;
+        uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(kvh * group + row % group) * D + d0;
+#pragma unroll
+        for (int j = 0; j < VD; j += 4)
+          *reinterpret_cast<u32x2*>(dst + j) = u32x2{pack2(x[j] * inv, x[j + 1] * inv), pack2(x[j + 2] * inv, x[j + 3] * inv)};
+      } else {
+#pragma unroll
+        for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(o + (size_t)row * D + d0 + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+        if (d0 == 0) ml_out[row] = make_float2(mr, lr);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <int D, bool FP8>
+__device__ void run_tiles(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D, FP8>& sh, bool direct, float* o, float2* ml) {
+  if (g.rows <= 16) run_segment<D, FP8, 1>(a, group, kvh, g, sh, direct, o, ml);
+  else if (g.rows <= 32) run_segment<D, FP8, 2>(a, group, kvh, g, sh, direct, o, ml);
+  else run_segment<D, FP8, 4>(a, group, kvh, g, sh, direct, o, ml);
+}
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
+  __shared__ Shared<D, FP8> sh;
+  const DecodeArgs& a = c.a;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int n_items = a.n_groups + a.n_seqs;
+  auto length = [&](int s) { return min(max(a.kv_len[s], 0), a.capacity); };
+  auto units = [](int from, int to) { return to > from ? (to - (from & ~31) + kUnit - 1) / kUnit : 0; };
+
+  // ---- units of every item, groups first
+  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[a.n_groups + s] = units(0, length(s));
+  __syncthreads();
+  for (int g = wave; g < a.n_groups; g += 4) {
+    const int first = a.first[g], behind = a.behind[g], prefix = a.prefix[g];
+    int count = 0, src = -1;
+    for (int s0 = first; s0 < behind; s0 += 64) {
+      const uint64_t who = __ballot(s0 + lane < behind && length(min(s0 + lane, a.n_seqs - 1)) >= prefix);
+      if (src < 0 && who) src = s0 + __builtin_ctzll(who);
+      count += __popcll(who);
+    }
+    const bool active = count >= 2;
+    if (active)
+      for (int s = first + lane; s < behind; s += 64)
+        if (length(s) >= prefix) sh.cum[a.n_groups + s] = units(prefix, length(s));
+    if (lane == 0) {
+      sh.group_src[g] = active ? src : -1;
+      sh.cum[g] = active ? (prefix + kUnit - 1) / kUnit * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
+    }
+  }
+  __syncthreads();
+  // ---- exclusive sums, in place
+  {
+    const int per = (n_items + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * per, n_items), hi = min(lo + per, n_items);
+    int sum = 0;
+    for (int i = lo; i < hi; ++i) sum += sh.cum[i];
+    int run = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(run, o);
+      if (lane >= o) run += up;
+    }
+    if (lane == 63) sh.part[wave] = run;
+    __syncthreads();
+    int at = run - sum;
+    for (int w = 0; w < wave; ++w) at += sh.part[w];
+    for (int i = lo; i < hi; ++i) {
+      const int v = sh.cum[i];
+      sh.cum[i] = at;
+      at += v;
+    }
+    if (threadIdx.x == kThreads - 1) sh.cum[n_items] = sh.part[0] + sh.part[1] + sh.part[2] + sh.part[3];
+    __syncthreads();
+  }
+  const int per_head = uniform(sh.cum[n_items]), all = per_head * a.n_kv_heads;
+  const int chunk = max((all + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+
+  // ---- where the join finds every row's pieces
+  const Layout y = layout(a.n_seqs, a.n_kv_heads, c.sh.group, c.sh.n_passes, D);
+  char* ws = static_cast<char*>(a.ws);
+  Meta* meta = reinterpret_cast<Meta*>(ws + y.meta);
+  for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_kv_heads * a.n_seqs; i += gridDim.x * kThreads) {
+    const int h = i / a.n_seqs, s = i % a.n_seqs, it = a.n_groups + s;
+    Meta w = make_int4(0, 0, 0, 0);
+    for (int g = 0; g < a.n_groups; ++g) {
+      if (s < a.first[g] || s >= a.behind[g]) continue;
+      if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
+        const int n = (a.prefix[g] + kUnit - 1) / kUnit, pass = (s - a.first[g]) / c.sh.per_pass;
+        const int u0 = h * per_head + sh.cum[g] + pass * n, w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
+        w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
+        w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
+      }
+      break;
+    }
+    const int u0 = h * per_head + sh.cum[it], n = sh.cum[it + 1] - sh.cum[it];
+    if (n > 0) {
+      const int w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
+      w.x = w0 + i;
+      w.y = w0 == w1 && w.w == 0 ? -1 : w1 - w0 + 1;
+    }
+    meta[i] = w;
+  }
+
+  // ---- this workgroup's chunk, piece by piece
+  int u = (int)blockIdx.x * chunk;                  // at most `all` + grid, which fits
+  const int end = min(u + chunk, all);
+  while (u < end) {
+    const int h = u / per_head, in_head = u % per_head;
+    int lo = 0, hi = n_items - 1;                   // last item that begins at or before the unit (those of no units come before it)
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sh.cum[mid] <= in_head) lo = mid; else hi = mid - 1;
+    }
+    const int it = uniform(lo), first = uniform(sh.cum[it]), n = uniform(sh.cum[it + 1]) - first;
+    int from_unit = in_head - first, to_unit = min(from_unit + end - u, n);
+    Segment g;
+    if (it < a.n_groups) {
+      const int tiles = (a.prefix[it] + kUnit - 1) / kUnit, pass = from_unit / tiles;
+      from_unit -= pass * tiles;
+      to_unit = min(to_unit - pass * tiles, tiles);
+      g.seq = uniform(sh.group_src[it]);
+      g.seq0 = a.first[it] + pass * c.sh.per_pass;
+      g.rows = min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group;
+      g.from = 0;
+      g.to = a.prefix[it];
+      g.t0 = from_unit * kUnit;
+      g.t1 = min(to_unit * kUnit, g.to);
+      const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
+      run_tiles<D, FP8>(a, c.sh.group, h, g, sh, false, reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D,
+                        reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass);
+    } else {
+      const int s = it - a.n_groups;
+      g.seq = g.seq0 = s;
+      g.rows = c.sh.group;
+      g.from = 0;
+      for (int k = 0; k < a.n_groups; ++k)
+        if (s >= a.first[k] && s < a.behind[k] && sh.group_src[k] >= 0 && length(s) >= a.prefix[k]) g.from = a.prefix[k];
+      g.from = uniform(g.from);
+      g.to = uniform(length(s));
+      g.t0 = (g.from & ~31) + from_unit * kUnit;
+      g.t1 = min((g.from & ~31) + to_unit * kUnit, g.to);
+      const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
+      const bool direct = g.from == 0 && from_unit == 0 && to_unit == n;
+      if (c.sh.group <= 16) run_segment<D, FP8, 1>(a, c.sh.group, h, g, sh, direct, reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D, reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group);
+      else run_tiles<D, FP8>(a, c.sh.group, h, g, sh, direct, reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D, reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group);
+    }
+    u += to_unit - from_unit;
+  }
+}
+
+// One wavefront (W = 4: four, sharing out the pieces) per query row: the pieces of its prefix and its own, on one maximum.
+template <int D, int W>
+__global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
+  constexpr int E = D / 64;                          // dimensions per lane
+  __shared__ float part[4][D];
+  __shared__ float2 part_ml[4];
+  const DecodeArgs& a = c.a;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), group = c.sh.group;
+  const int row = W == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
+  if (row >= a.n_seqs * a.n_heads) return;
+  const int s = row / a.n_heads, head = row % a.n_heads, h = head / group, r = head % group;
+  const Layout y = layout(a.n_seqs, a.n_kv_heads, group, c.sh.n_passes, D);
+  const char* ws = static_cast<const char*>(a.ws);
+  const Meta w = reinterpret_cast<const Meta*>(ws + y.meta)[h * a.n_seqs + s];
+  if (w.y < 0) return;
+  const int n_pre = w.w & 0xffff, n = n_pre + w.y;
+  const float* pre_o = reinterpret_cast<const float*>(ws + y.prefix_o) + ((size_t)w.z * kRowsPass + (w.w >> 16) + r) * D;
+  const float2* pre_ml = reinterpret_cast<const float2*>(ws + y.prefix_ml) + (size_t)w.z * kRowsPass + (w.w >> 16) + r;
+  const float* own_o = reinterpret_cast<const float*>(ws + y.own_o) + ((size_t)w.x * group + r) * D;
+  const float2* own_ml = reinterpret_cast<const float2*>(ws + y.own_ml) + (size_t)w.x * group + r;
+  float m = -INFINITY, l = 0.0f, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.0f;
+  // up to 64 pieces at a time: lane i weighs piece i
+  for (int i0 = W == 4 ? wave * 64 : 0; i0 < n; i0 += 64 * W) {
+    const int i = i0 + lane, count = min(64, n - i0);
+    float2 ml = make_float2(-INFINITY, 0.0f);
+    if (i < n) ml = i < n_pre ? pre_ml[(size_t)i * kRowsPass] : own_ml[(size_t)(i - n_pre) * group];
+    float top = ml.x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float raised = fmaxf(m, top), to = raised == -INFINITY ? 0.0f : raised, shrink = exp2_fast(m - to);
+    const float weight = exp2_fast(ml.x - to);
+    float sum = ml.y * weight;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    l = l * shrink + sum;
+    m = raised;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= shrink;
+#pragma unroll 4
+    for (int k = 0; k < count; ++k) {
+      const int p = i0 + k;
+      const float f = __shfl(weight, k);
+      const float* o = p < n_pre ? pre_o + (size_t)p * kRowsPass * D : own_o + (size_t)(p - n_pre) * group * D;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(f, o[E * lane + e], x[e]);
+    }
+  }
+  if constexpr (W == 4) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) part[wave][E * lane + e] = x[e];
+    if (lane == 0) part_ml[wave] = make_float2(m, l);
+    __syncthreads();
+    if (wave) return;
+    float top = -INFINITY;
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, part_ml[k].x);
+    l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.0f;
+    for (int k = 0; k < 4; ++k) {
+      const float f = exp2_fast(part_ml[k].x - (top == -INFINITY ? 0.0f : top));
+      l += part_ml[k].y * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(f, part[k][E * lane + e], x[e]);
+    }
+  }
+  const float inv = l == 0.0f ? 0.0f : (fp8 ? a.v_scale[h] : 1.0f) / l;
+  uint16_t* dst = a.out + (size_t)s * a.ld_out + (size_t)head * D + E * lane;
+  if constexpr (E == 2) *reinterpret_cast<uint32_t*>(dst) = pack2(x[0] * inv, x[1] * inv);
+  else *dst = (uint16_t)pack2(x[0] * inv, 0.0f);
+}
+
+template <int D>
+hipError_t launch(const DecodeCall& c, bool fp8, hipStream_t s) {
+  // never more workgroups than units there can be
+  const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kUnit - 1) / kUnit + 1);
+  const unsigned grid = (unsigned)std::min<int64_t>(kWorkgroups, most);
+  if (fp8) k_attn_decode<D, true><<<grid, kThreads, 0, s>>>(c);
+  else k_attn_decode<D, false><<<grid, kThreads, 0, s>>>(c);
+  if (hipError_t e = hipGetLastError()) return e;
+  const int rows = c.a.n_seqs * c.a.n_heads;
+  if (rows <= 1024) k_join<D, 4><<<rows, kThreads, 0, s>>>(c, fp8);
+  else k_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(c, fp8);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
+  const int group = n_heads / n_kv_heads, per_pass = kRowsPass / group;
+  // passes of any way to share: a group has two sequences or more
+  const int most = n_seqs < 2 ? 0 : n_seqs / per_pass + std::min(MES_MAX_EXPERTS, n_seqs / 2);
+  return layout(n_seqs, n_kv_heads, group, most, head_dim).total;
+}
+
+hipError_t launch_attn_decode(const DecodeArgs& a, bool fp8, hipStream_t s) {
+  DecodeCall c;
+  c.a = a;
+  c.sh.group = a.n_heads / a.n_kv_heads;
+  c.sh.per_pass = kRowsPass / c.sh.group;
+  c.sh.n_passes = 0;
+  for (int g = 0; g < a.n_groups; ++g) {
+    c.pass_base[g] = c.sh.n_passes;
+    c.sh.n_passes += (a.behind[g] - a.first[g] + c.sh.per_pass - 1) / c.sh.per_pass;
+  }
+  return a.head_dim == 128 ? launch<128>(c, fp8, s) : launch<64>(c, fp8, s);
+}
+
+}  // namespace mes

@@ -1,0 +1,364 @@
+"""Attention over prompts and the paged cache, writing to the cache and copying its pages (through the C ABI) against row-by-row
+fp64 references, at the sizes, masks and layouts where they can go wrong.  Tolerances: oracle/attn_oracle.py."""
+import math
+import random
+
+import pytest
+import torch
+
+import paper_2406_09041_amd as mes
+from oracle import attn_oracle as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+INF, NAN = float("inf"), float("nan")
+
+
+def _ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def _rows(g, n, heads, dim, std=1.0):
+    return (torch.randn(n, heads, dim, generator=g) * std).to(torch.bfloat16)
+
+
+def _check(got, want, tol, what=""):
+    got = got.double().cpu()
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {((got - want).abs() / tol.clamp_min(1e-30)).max():.3g} times the tolerance, first at {bad.nonzero()[0].tolist()}"
+
+
+# ---------------------------------------------------------------------------------------------------------- prompts
+
+PROMPTS = [
+    ([1], 4, 2, 64), ([2], 4, 2, 128), ([31], 2, 1, 64), ([63], 2, 2, 128), ([64], 1, 1, 128), ([65], 3, 1, 64), ([127, 1, 128, 129], 2, 1, 128),
+    ([0, 5, 0, 0, 200, 1, 0], 4, 2, 64), ([333], 5, 5, 128), ([300, 17], 7, 1, 64), ([1] * 5, 8, 8, 128),
+    ([3] * 63 + [130], 2, 1, 64), ([0, 140] + [2] * 70 + [0], 2, 1, 64), ([1] * 64 + [129], 1, 1, 128),     # 64 sequences, and more
+]
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("lens,heads,kvh,dim", PROMPTS)
+def test_prompts(lens, heads, kvh, dim, fused):
+    g = torch.Generator().manual_seed(sum(lens) * 31 + heads)
+    T, behind = sum(lens), 3
+    q, k, v = _rows(g, T + behind, heads, dim, 2.0), _rows(g, T + behind, kvh, dim), _rows(g, T + behind, kvh, dim)
+    off = [0]
+    for n in lens:
+        off.append(off[-1] + n)
+    dq, dk, dv = q.to(DEV), k.to(DEV), v.to(DEV)
+    out = torch.full((T + behind, heads, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    if fused:                                                   # views of one buffer, rows further apart than they are long
+        row = torch.cat([dq, dk, dv, dk], 1)
+        dq, dk, dv = row[:, :heads], row[:, heads:heads + kvh], row[:, heads + kvh:heads + 2 * kvh]
+        wide = torch.full((T + behind, heads + 1, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+        out = wide[:, :heads]
+    mes.mes_attn_prompt(dq, dk, dv, _ints(off), out)
+    torch.cuda.synchronize()
+    assert torch.all(out[T:] == 7.0)                            # rows behind the last sequence
+    if fused:
+        assert torch.all(wide[:, heads] == 7.0)
+    for a, b in zip(off, off[1:]):
+        if b > a:
+            want, tol = O.attend(q[a:b], k[a:b], v[a:b], range(b - a), dim ** -0.5)
+            _check(out[a:b], want, tol, f"rows {a}..{b}")
+
+
+def test_a_long_prompt_by_sampled_rows():
+    """Several query tiles and many key tiles, the running maximum raised again and again (scores grow with the position)."""
+    g = torch.Generator().manual_seed(5)
+    T, heads, kvh, dim = 2500, 4, 2, 128
+    q, k, v = _rows(g, T, heads, dim, 2.0), _rows(g, T, kvh, dim), _rows(g, T, kvh, dim)
+    k[:, :, :8] += (torch.arange(T) / 250.0).to(torch.bfloat16)[:, None, None]
+    q[:, :, :8] = q[:, :, :8].abs()
+    out = mes.mes_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), _ints([0, T]))
+    torch.cuda.synchronize()
+    for i in (0, 1, 127, 128, 1000, 1023, 1024, 1999, 2303, 2304, 2499):
+        want, tol = O.attend(q[i:i + 1], k[:i + 1], v[:i + 1], [i], dim ** -0.5)
+        _check(out[i:i + 1], want, tol, f"row {i}")
+
+
+@pytest.mark.parametrize("bad", [NAN, INF, -INF, 3.3895e38])
+def test_prompt_rows_are_not_touched_by_what_they_do_not_see(bad):
+    """A NaN, an infinity or the type's largest value in a key or value: rows before it and other sequences as without it."""
+    g = torch.Generator().manual_seed(6)
+    lens, heads, kvh, dim = [70, 150, 40], 4, 2, 128
+    T = sum(lens)
+    q, k, v = _rows(g, T, heads, dim), _rows(g, T, kvh, dim), _rows(g, T, kvh, dim)
+    off = [0, 70, 220, 260]
+    at = 70 + 100
+    for which in ("k", "v"):
+        kk, vv = k.clone(), v.clone()
+        (kk if which == "k" else vv)[at, 0, 5] = bad
+        out = mes.mes_attn_prompt(q.to(DEV), kk.to(DEV), vv.to(DEV), _ints(off)).cpu()
+        for a, b, last in ((0, 70, 70), (70, at, 100), (220, 260, 40)):
+            want, tol = O.attend(q[a:b], k[a:b], v[a:b], range(last), dim ** -0.5)
+            _check(out[a:b], want, tol, f"{which} {bad}")
+        for h in (2, 3):                                        # heads of the other key / value head
+            want, tol = O.attend(q[70:220, h:h + 1], k[70:220, 1:], v[70:220, 1:], range(150), dim ** -0.5)
+            _check(out[70:220, h:h + 1], want, tol, f"{which} {bad}, head {h}")
+        if which == "v" and not math.isfinite(bad):             # rows that see it have it
+            assert not torch.isfinite(out[at:220, :2, 5]).any() and torch.isfinite(out[at:220, :2, 6]).all()
+
+
+# ------------------------------------------------------------------------------------------------------- the cache
+
+class Paged:
+    """A cache with random tokens, on both sides; pages in random order, unused ones full of NaN."""
+
+    def __init__(self, seed, lens, kvh, dim, page, e4m3=False, layers=2, layer=1, spare=2, width=None, share=None):
+        g, rng = torch.Generator().manual_seed(seed), random.Random(seed)
+        self.lens, self.page, self.layer = lens, page, layer
+        need = [-(-n // page) for n in lens]
+        n_pages = sum(need) + spare
+        ids = rng.sample(range(n_pages), n_pages)
+        self.width = width or max(need + [1])
+        table = []
+        for n in need:
+            table.append([ids.pop() for _ in range(n)])
+        self.k, self.v = ([torch.randn(n, kvh, dim, generator=g) for n in lens] for _ in range(2))
+        for s, (first, n) in enumerate(share or []):            # sequence s repeats the first n tokens of sequence `first`
+            if first != s:
+                self.k[s][:n], self.v[s][:n] = self.k[first][:n], self.v[first][:n]
+        shape = (layers, n_pages, kvh, page, dim)
+        kc, vc = torch.full(shape, NAN), torch.full(shape, NAN)
+        self.scales = [None, None]
+        if e4m3:
+            self.scales = [0.01 + 0.02 * torch.rand(layers, kvh, generator=g) for _ in range(2)]
+        for s, n in enumerate(lens):
+            for x, c, scale in ((self.k, kc, self.scales[0]), (self.v, vc, self.scales[1])):
+                if e4m3:
+                    code = (x[s] / scale[layer][:, None]).clamp(-448, 448).to(torch.float8_e4m3fn)
+                    x[s] = code.double() * scale[layer][:, None].double()
+                    put = code.float()
+                else:
+                    x[s] = x[s].to(torch.bfloat16)
+                    put = x[s].float()
+                for j in range(n):
+                    c[layer, table[s][j // page], :, j % page] = put[j]
+        kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+        self.cache = mes.KvCache.over(kc.to(kind).to(DEV), vc.to(kind).to(DEV), *[None if x is None else x.to(DEV) for x in self.scales])
+        self.table = [row + [0] * (self.width - len(row)) for row in table]
+        self.n_pages = n_pages
+
+    def batch(self, offsets=None, kv_len=None, table=None):
+        return mes.SeqBatch(_ints(self.lens if kv_len is None else kv_len), _ints(self.table if table is None else table).reshape(len(self.lens), self.width),
+                            None if offsets is None else _ints(offsets))
+
+
+EXTENDS = [
+    ([1], [1], 4, 2, 64, 16), ([40], [40], 2, 1, 128, 16), ([300], [1], 4, 2, 128, 32), ([300, 64, 17], [130, 64, 1], 4, 2, 64, 16),
+    ([129, 0, 200], [1, 0, 200], 2, 2, 128, 64), ([77, 500], [70, 129], 8, 1, 64, 256), ([20] * 66, [3] * 66, 2, 1, 64, 16),
+]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("lens,news,heads,kvh,dim,page", EXTENDS)
+def test_extend(lens, news, heads, kvh, dim, page, e4m3):
+    c = Paged(len(lens) * 7 + lens[0], lens, kvh, dim, page, e4m3)
+    g = torch.Generator().manual_seed(9)
+    off = [0]
+    for n in news:
+        off.append(off[-1] + n)
+    q = _rows(g, off[-1] + 2, heads, dim, 2.0)
+    out = torch.full((off[-1] + 2, heads, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q.to(DEV), out)
+    torch.cuda.synchronize()
+    assert torch.all(out[off[-1]:] == 7.0)
+    for s in range(len(lens)):
+        if news[s]:
+            want, tol = O.attend(q[off[s]:off[s + 1]], c.k[s], c.v[s], range(lens[s] - news[s], lens[s]), dim ** -0.5)
+            _check(out[off[s]:off[s + 1]], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_extend_with_lengths_and_pages_that_do_not_fit(e4m3):
+    """Fewer tokens than rows (the first rows see nothing), a negative length, more tokens than the table has room for, pages
+    outside the cache."""
+    lens, dim, heads, kvh = [100, 64, 50, 96], 64, 4, 2
+    c = Paged(3, lens, kvh, dim, 16, e4m3)
+    g = torch.Generator().manual_seed(2)
+    off, kv_len = [0, 130, 140, 150, 200], [100, -5, 50, 150]
+    table = [list(r) for r in c.table]
+    table[2][1] = c.n_pages
+    table[2][3] = -1
+    table = [r[:6] for r in table]                               # room for 96 tokens
+    c.width = 6
+    q = _rows(g, 200, heads, dim, 2.0)
+    out = mes.mes_attn_extend(c.cache, c.layer, c.batch(off, kv_len, table), q.to(DEV)).cpu()
+    assert not out[:30].any() and not out[130:140].any()
+    want, tol = O.attend(q[30:130], c.k[0][:96], c.v[0][:96], range(100), dim ** -0.5)
+    _check(out[30:130], want, tol, "longer than the table")
+    there = [j for j in range(50) if j // 16 not in (1, 3)]
+    for i in range(10):
+        seen = [x for x, j in enumerate(there) if j <= 40 + i]
+        want, tol = O.attend(q[140 + i:141 + i], c.k[2][there], c.v[2][there], [len(seen) - 1], dim ** -0.5)
+        _check(out[140 + i:141 + i], want, tol, "pages missing")
+    want, tol = O.attend(q[150:200], c.k[3], c.v[3], [min(100 + i, 95) for i in range(50)], dim ** -0.5)
+    _check(out[150:200], want, tol, "positions past the table")
+
+
+DECODES = [
+    # lens, heads, kv heads, dim, page, segs, prefix
+    ([1], 4, 2, 64, 16, None, None), ([0], 4, 2, 128, 16, None, None), ([31, 32, 33], 4, 1, 128, 16, None, None),
+    ([127, 128, 129, 0, 1000], 8, 2, 128, 32, None, None), ([700], 40, 40, 64, 64, None, None), ([50, 400], 17, 1, 128, 16, None, None),
+    ([260, 3], 64, 1, 64, 16, None, None), ([90, 150], 33, 1, 128, 256, None, None), ([5000], 2, 1, 64, 16, None, None),
+    ([200, 200, 200], 4, 2, 128, 16, [3], [200]),                                        # nothing but the prefix
+    ([300, 170, 161, 160, 159, 0], 8, 2, 64, 16, [6], [160]),                            # shorter than the prefix, and padding
+    ([90, 100, 400, 333, 350, 64], 4, 1, 128, 16, [2, 3, 0, 1], [77, 301, 50, 40]),      # inside a page; alone; empty
+    ([500 + i for i in range(40)], 12, 4, 64, 32, [17, 23], [333, 0]),                   # rows of a pass that 3 does not divide
+    ([150, 10, 20], 4, 2, 128, 16, [3], [100]),                                          # one sequence is long enough: nothing is shared
+    ([130 + i % 5 for i in range(30)], 64, 1, 64, 16, [30], [128]),                      # a pass per sequence
+]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("lens,heads,kvh,dim,page,segs,prefix", DECODES)
+def test_decode(lens, heads, kvh, dim, page, segs, prefix, e4m3):
+    share, seg = None, None
+    if segs:
+        seg, share = [0], []
+        for c, p in zip(segs, prefix):
+            # the first of them that is as long as the prefix gives it to the others
+            first = next((s for s in range(seg[-1], seg[-1] + c) if lens[s] >= p), None)
+            share += [(first if first is not None and lens[s] >= p else s, p) for s in range(seg[-1], seg[-1] + c)]
+            seg.append(seg[-1] + c)
+    c = Paged(heads + len(lens), lens, kvh, dim, page, e4m3, share=share)
+    g = torch.Generator().manual_seed(heads)
+    q = _rows(g, len(lens), heads, dim, 2.0)
+    call = mes.AttnDecode(c.cache, heads, max_seqs=len(lens))
+    call.ws.fill_(255)                                                                     # scratch: what is in it does not matter
+    wide = torch.full((len(lens), heads + 2, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    call(c.layer, c.batch(), q.to(DEV), seg, prefix, wide[:, :heads])
+    again = call(c.layer, c.batch(), q.to(DEV), seg, prefix)
+    torch.cuda.synchronize()
+    out = wide[:, :heads].cpu()
+    assert torch.equal(out.view(torch.int16), again.cpu().view(torch.int16)) and torch.all(wide[:, heads:] == 7.0)
+    for s, n in enumerate(lens):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [n - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
+
+
+def test_decode_with_lengths_and_pages_that_do_not_fit():
+    lens, heads, kvh, dim = [96, 64, 100, 80], 4, 2, 128
+    c = Paged(4, lens, kvh, dim, 16)
+    table = [list(r[:6]) for r in c.table]
+    table[3][2], table[3][4] = c.n_pages + 5, -7
+    c.width = 6
+    g = torch.Generator().manual_seed(1)
+    q = _rows(g, 4, heads, dim, 2.0)
+    call = mes.AttnDecode(c.cache, heads, 4)
+    out = call(c.layer, c.batch(None, [96, -3, 2 ** 31 - 1, 80], table), q.to(DEV)).cpu()
+    assert not out[1].any()
+    for s, there in ((0, range(96)), (2, range(96)), (3, [j for j in range(80) if j // 16 not in (2, 4)])):
+        there = list(there)
+        want, tol = O.attend(q[s:s + 1], c.k[s][there], c.v[s][there], [len(there) - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+def test_decode_rows_keep_what_is_not_finite_to_themselves(bad):
+    lens, heads, kvh, dim = [200, 210, 60], 4, 2, 64
+    c = Paged(8, lens, kvh, dim, 16, share=[(0, 150), (0, 150), (2, 0)])
+    g = torch.Generator().manual_seed(1)
+    q = _rows(g, 3, heads, dim)
+    q[1, 0, 3] = NAN                                                                       # one row of a shared pass
+    c.cache.v[c.layer, c.table[1][200 // 16], 1, 200 % 16, 7] = bad                        # a token of its own, second key / value head
+    out = mes.AttnDecode(c.cache, heads, 3)(c.layer, c.batch(), q.to(DEV), [0, 3], [150]).cpu()
+    for s in (0, 2):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [lens[s] - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
+    assert torch.isnan(out[1, 0]).all()
+    want, tol = O.attend(q[1:2, 1:2], c.k[1][:, :1], c.v[1][:, :1], [209], dim ** -0.5)
+    _check(out[1:2, 1:2], want, tol, "the row's other head")
+    assert not torch.isfinite(out[1, 2:, 7]).any() and torch.isfinite(out[1, 2:, 8]).all()
+
+
+# ---------------------------------------------------------------------------------------------------- append and copy
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("contexts,news,heads,kvh,dim,page", [
+    ([0], [1], 1, 1, 64, 16), ([5, 0, 100, 31], [1, 1, 1, 1], 4, 2, 128, 32), ([3, 16, 0, 250], [20, 0, 100, 7], 5, 1, 64, 16),
+    ([60] * 70, [2] * 70, 8, 8, 128, 64)])
+def test_append(contexts, news, heads, kvh, dim, page, e4m3):
+    lens = [a + b for a, b in zip(contexts, news)]
+    c = Paged(11, lens, kvh, dim, page, e4m3)
+    g = torch.Generator().manual_seed(4)
+    off = [0]
+    for n in news:
+        off.append(off[-1] + n)
+    T = off[-1]
+    q, k, v = _rows(g, T + 2, heads, dim), _rows(g, T + 2, kvh, dim, 3.0), _rows(g, T + 2, kvh, dim, 3.0)
+    k[0, 0, 0], v[0, 0, 1] = 1e30, -1e30                                                   # clamped in an 8-bit cache
+    rotary = mes.rotary_table(c.width * page, dim)
+    before = [x.clone().view(torch.uint8).cpu() for x in (c.cache.k, c.cache.v)]
+    offsets = None if set(news) == {1} else off
+    rows = T if offsets is None else T + 2
+    out = torch.full((T + 2, heads, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    row = torch.cat([k, v], 1).to(DEV)                                                      # k and v are views of one buffer
+    mes.mes_kv_append(c.cache, c.layer, c.batch(offsets), q.to(DEV)[:rows], row[:rows, :kvh], row[:rows, kvh:], rotary, out[:rows])
+    torch.cuda.synchronize()
+    pos = torch.tensor([lens[s] - news[s] + i for s in range(len(news)) for i in range(news[s])])
+    seq = [s for s in range(len(news)) for _ in range(news[s])]
+    table = rotary.cpu()
+    want_q = O.rotate(q[:T], table, pos).to(torch.bfloat16)
+    assert torch.equal(out[:T].cpu().view(torch.int16), want_q.view(torch.int16)) and torch.all(out[T:] == 7.0)
+    kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+    for x, cache, keep, scale in ((O.rotate(k[:T], table, pos), c.cache.k, before[0], c.scales[0]), (v[:T].float(), c.cache.v, before[1], c.scales[1])):
+        want = keep.view(kind).clone().view(torch.uint8 if e4m3 else torch.int16)
+        if e4m3:
+            x = (x / scale[c.layer][None, :, None]).clamp(-448, 448)
+        x = x.to(kind).view(want.dtype)
+        for t in range(T):
+            want[c.layer, c.table[seq[t]][pos[t] // page], :, pos[t] % page] = x[t]
+        assert torch.equal(cache.cpu().view(want.dtype), want)                              # and nothing else has changed
+
+
+def test_append_in_place_without_turning_and_without_a_place():
+    lens, heads, kvh, dim, page = [20, 40], 2, 2, 64, 16
+    c = Paged(2, lens, kvh, dim, page)
+    g = torch.Generator().manual_seed(3)
+    q, k, v = _rows(g, 12, heads, dim), _rows(g, 12, kvh, dim), _rows(g, 12, kvh, dim)
+    rotary = mes.rotary_table(c.width * page, dim)
+    batch = c.batch([0, 6, 12])
+    dq = q.to(DEV)
+    assert mes.mes_kv_append(c.cache, c.layer, batch, dq, k.to(DEV), v.to(DEV), rotary, dq) is dq
+    pos = torch.tensor(list(range(14, 20)) + list(range(34, 40)))
+    assert torch.equal(dq.cpu().view(torch.int16), O.rotate(q, rotary.cpu(), pos).to(torch.bfloat16).view(torch.int16))
+    assert mes.mes_kv_append(c.cache, c.layer, batch, None, k.to(DEV), v.to(DEV)) is None   # as they are
+    assert torch.equal(c.cache.k[c.layer, c.table[0][1], :, 3].cpu(), k[5])
+    # positions before 0 and behind the table, pages outside the cache: nothing is written
+    before = c.cache.k.clone().view(torch.int16), c.cache.v.clone().view(torch.int16)
+    table = [list(r) for r in c.table]
+    table[1][2] = c.n_pages
+    out = torch.full((12, heads, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    mes.mes_kv_append(c.cache, c.layer, c.batch([0, 6, 12], [-3, 40], table), q.to(DEV), k.to(DEV), v.to(DEV), rotary, out)
+    mes.mes_kv_append(c.cache, c.layer, c.batch([0, 6, 12], [1000, 2 ** 31 - 1]), q.to(DEV), k.to(DEV), v.to(DEV), rotary, out[:12])
+    torch.cuda.synchronize()
+    assert torch.equal(c.cache.k.view(torch.int16), before[0]) and torch.equal(c.cache.v.view(torch.int16), before[1])
+    assert torch.all(out[:6] == 7.0)
+    assert torch.equal(out[6:].cpu().view(torch.int16), O.rotate(q[6:], rotary.cpu(), pos[6:]).to(torch.bfloat16).view(torch.int16))
+
+
+@pytest.mark.parametrize("kvh,dim,page,layers,n,e4m3", [(1, 64, 16, 1, 1, True), (8, 128, 16, 3, 5, False), (3, 64, 32, 2, 7, False), (5, 128, 256, 2, 3, True),
+                                                        (1, 64, 16, 2, 1000, False)])
+def test_copy_pages(kvh, dim, page, layers, n, e4m3):
+    rng = random.Random(n)
+    n_pages = 2 * n + 3
+    shape = (layers, n_pages, kvh, page, dim)
+    bits = torch.randint(0, 256, shape + ((1,) if e4m3 else (2,)), dtype=torch.uint8, generator=torch.Generator().manual_seed(n))
+    kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+    k, v = bits.view(kind).reshape(shape).to(DEV), bits.flip(0).contiguous().view(kind).reshape(shape).to(DEV)
+    ones = torch.ones(layers, kvh, device=DEV) if e4m3 else None
+    cache = mes.KvCache.over(k, v, ones, ones)
+    pages = rng.sample(range(n_pages), 2 * n)
+    src, dst = [pages[rng.randrange(n)] for _ in range(n)], pages[n:]                       # a page may go to several places
+    item = torch.uint8 if e4m3 else torch.int16
+    want = []
+    for x in (k, v):
+        w = x.cpu().view(item).clone()
+        w[:, dst] = w[:, src]
+        want.append(w)
+    mes.mes_kv_copy_pages(cache, src, dst)
+    torch.cuda.synchronize()
+    assert torch.equal(k.cpu().view(item), want[0]) and torch.equal(v.cpu().view(item), want[1])
