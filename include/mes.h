@@ -358,15 +358,20 @@ mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, cons
 
 /* Attention over whole prompts: n_seqs sequences packed one after the other, rows seq_offsets[s] .. seq_offsets[s+1]
  * (DEVICE int32 [n_seqs + 1], 0 = o[0] <= ... <= o[n_seqs] <= T; rows behind are left as they are), every row sees the
- * rows of its own sequence up to itself.  out: [T][n_heads][head_dim], rows ld_out apart. */
+ * rows of its own sequence up to itself.  out: [T][n_heads][head_dim], rows ld_out apart.
+ * workspace: NULL, or >= mes_attn_prompt_workspace_bytes(T, n_seqs, n_heads, n_kv_heads, head_dim), 16-byte aligned, contents
+ * irrelevant; calls sharing a workspace must be stream-ordered.  With it the keys of long rows are shared out where few rows
+ * would leave most of the chip idle (up to 64 sequences), without it never. */
+size_t mes_attn_prompt_workspace_bytes(int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim);
 mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, int n_seqs, const int32_t* seq_offsets,
                            int n_heads, int n_kv_heads, int head_dim, int ld_q, int ld_k, int ld_v, float scale, void* out,
-                           int ld_out, void* stream);
+                           int ld_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The same with keys and values in the cache (a prompt behind a cached system prompt, the next piece of a long prompt):
- * the T rows are the last tokens of their sequences and their keys / values have been appended.  q_offsets not NULL. */
+ * the T rows are the last tokens of their sequences and their keys / values have been appended.  q_offsets not NULL.
+ * workspace: as for mes_attn_prompt. */
 mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, int T, int n_heads, int ld_q,
-                           float scale, void* out, int ld_out, void* stream);
+                           float scale, void* out, int ld_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* One token per sequence (q_offsets is not read): row s attends to the kv_len[s] cached tokens of sequence s.
  * Sequences that share a prefix: rows are sorted by expert as for mes_delta_linear, seg_offsets HOST [n_experts + 1]

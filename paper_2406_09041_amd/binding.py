@@ -23,6 +23,7 @@ MAX_EXPERTS = 64
 
 KV_BF16, KV_E4M3 = 0, 1
 MAX_SEQS = 4096
+SHORT_PROMPT = 384          # keys: rows that see no more are never shared out, and need no workspace
 
 STATUS_NAMES = {0: "MES_OK", 1: "MES_ERR_NULL", 2: "MES_ERR_SHAPE", 3: "MES_ERR_BITS", 4: "MES_ERR_SALIENT",
                 5: "MES_ERR_SEGMENTS", 6: "MES_ERR_ALIGN", 7: "MES_ERR_WORKSPACE", 8: "MES_ERR_DEVICE", 9: "MES_ERR_PAGES"}
@@ -38,7 +39,7 @@ EXPORTS = ["mes_base_bytes", "mes_codes_bytes", "mes_salient_bytes", "mes_pack_w
            "mes_gated_workspace_bytes", "mes_delta_linear_gated",
            "mes_step_grad_workspace_bytes", "mes_step_grad", "mes_step_adamw", "mes_noalloc_scratch_bytes",
            "mes_delta_linear_noalloc", "mes_long_segment_tokens",
-           "mes_kv_append", "mes_attn_prompt", "mes_attn_extend", "mes_attn_decode_workspace_bytes", "mes_attn_decode",
+           "mes_kv_append", "mes_attn_prompt", "mes_attn_prompt_workspace_bytes", "mes_attn_extend", "mes_attn_decode_workspace_bytes", "mes_attn_decode",
            "mes_kv_copy_pages", "mes_pages_create", "mes_pages_destroy", "mes_pages_grow", "mes_pages_fork", "mes_pages_free",
            "mes_pages_compact", "mes_pages_table", "mes_pages_length", "mes_pages_unused"]
 
@@ -167,9 +168,11 @@ def _load() -> ctypes.CDLL:
     lib.mes_kv_append.restype = c_int
     lib.mes_kv_append.argtypes = [kvp, c_int, sqp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, c_int, vp, c_int, vp]
     lib.mes_attn_prompt.restype = c_int
-    lib.mes_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, c_int, c_int, c_int, c_int, c_int, fl, vp, c_int, vp]
+    lib.mes_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, c_int, c_int, c_int, c_int, c_int, fl, vp, c_int, vp, c_sz, vp]
+    lib.mes_attn_prompt_workspace_bytes.restype = c_sz
+    lib.mes_attn_prompt_workspace_bytes.argtypes = [c_int] * 5
     lib.mes_attn_extend.restype = c_int
-    lib.mes_attn_extend.argtypes = [kvp, c_int, sqp, vp, c_int, c_int, c_int, fl, vp, c_int, vp]
+    lib.mes_attn_extend.argtypes = [kvp, c_int, sqp, vp, c_int, c_int, c_int, fl, vp, c_int, vp, c_sz, vp]
     lib.mes_attn_decode_workspace_bytes.restype = c_sz
     lib.mes_attn_decode_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
     lib.mes_attn_decode.restype = c_int
@@ -672,10 +675,16 @@ def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch
     return q_out if q is not None else None
 
 
+def prompt_workspace(T: int, n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, device) -> torch.Tensor:
+    """Allocates a workspace of mes_attn_prompt / mes_attn_extend (scratch: its contents do not matter)."""
+    return torch.empty(lib.mes_attn_prompt_workspace_bytes(T, n_seqs, n_heads, n_kv_heads, head_dim), dtype=torch.uint8, device=device)
+
+
 def mes_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_offsets: torch.Tensor, out: Optional[torch.Tensor] = None,
-                    scale: Optional[float] = None) -> torch.Tensor:
+                    scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Causal attention over packed prompts: q [T, heads, d], k and v [T, kv heads, d] (views of one buffer are fine),
-    seq_offsets int32 [n + 1] on the GPU.  Returns [T, heads, d]; rows behind the last sequence are left as they are."""
+    seq_offsets int32 [n + 1] on the GPU.  Returns [T, heads, d]; rows behind the last sequence are left as they are.
+    workspace: one to share between stream-ordered calls (prompt_workspace), or None to allocate one."""
     dev = q.device
     T, heads, dim = q.shape
     assert q.is_cuda and k.shape == v.shape and k.shape[0] == T and k.shape[2] == dim
@@ -683,23 +692,31 @@ def mes_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_offse
     if out is None:
         out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
     assert out.shape == q.shape
-    _call_on(dev, lib.mes_attn_prompt, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, seq_offsets.shape[0] - 1, seq_offsets.data_ptr(),
-             heads, k.shape[1], dim, _heads_of("q", q, dev), _heads_of("k", k, dev), _heads_of("v", v, dev),
-             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev))
+    n, kv_heads = seq_offsets.shape[0] - 1, k.shape[1]
+    if workspace is None and T > SHORT_PROMPT:
+        workspace = prompt_workspace(T, n, heads, kv_heads, dim, dev)
+    _call_on(dev, lib.mes_attn_prompt, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, n, seq_offsets.data_ptr(),
+             heads, kv_heads, dim, _heads_of("q", q, dev), _heads_of("k", k, dev), _heads_of("v", v, dev),
+             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev),
+             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
     return out
 
 
 def mes_attn_extend(cache: KvCache, layer: int, batch: SeqBatch, q: torch.Tensor, out: Optional[torch.Tensor] = None,
-                    scale: Optional[float] = None) -> torch.Tensor:
-    """Causal attention of the batch's new rows (its last tokens, already appended) over the cache."""
+                    scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of the batch's new rows (its last tokens, already appended) over the cache.  workspace: as for
+    mes_attn_prompt."""
     dev = cache.device
     T, heads, dim = q.shape
     assert batch.device == dev and dim == cache.head_dim
     if out is None:
         out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
     assert out.shape == q.shape
+    if workspace is None and batch.page_table.shape[1] * cache.page_tokens > SHORT_PROMPT:
+        workspace = prompt_workspace(T, batch.n, heads, cache.n_kv_heads, dim, dev)
     _call_on(dev, lib.mes_attn_extend, cache.ref, layer, batch.ref, q.data_ptr(), T, heads, _heads_of("q", q, dev),
-             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev))
+             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev),
+             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
     return out
 
 

@@ -362,9 +362,24 @@ mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, cons
   return check_hip(launch_append(a, T, kv->dtype == MES_KV_E4M3, (hipStream_t)stream), who);
 }
 
+size_t mes_attn_prompt_workspace_bytes(int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
+  if (T < 0 || n_seqs < 0 || n_seqs > MES_MAX_SEQS || n_kv_heads < 1 || n_heads < 1 || n_heads % n_kv_heads || n_heads / n_kv_heads > 64 ||
+      n_heads > 65535 || (head_dim != 64 && head_dim != 128))
+    return 0;
+  return attn_prompt_workspace_bytes(T, n_seqs, n_heads, n_kv_heads, head_dim);
+}
+
+static mes_status check_prompt_workspace(const char* who, int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim, const void* workspace, size_t bytes) {
+  if (!workspace) return MES_OK;
+  const size_t need = attn_prompt_workspace_bytes(T, n_seqs, n_heads, n_kv_heads, head_dim);
+  if (bytes < need) return fail(MES_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, need);
+  if (!aligned16(workspace)) return fail(MES_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+  return MES_OK;
+}
+
 mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, int n_seqs, const int32_t* seq_offsets,
                            int n_heads, int n_kv_heads, int head_dim, int ld_q, int ld_k, int ld_v, float scale, void* out,
-                           int ld_out, void* stream) {
+                           int ld_out, void* workspace, size_t workspace_bytes, void* stream) {
   static const char who[] = "mes_attn_prompt";
   if (mes_status st = check_heads(who, n_heads, n_kv_heads, head_dim)) return st;
   if (n_seqs < 0 || n_seqs > MES_MAX_SEQS) return fail(MES_ERR_SHAPE, "%s: n_seqs = %d outside [0, %d]", who, n_seqs, MES_MAX_SEQS);
@@ -376,7 +391,9 @@ mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, i
   if (mes_status st = check_rows(who, "k", k, ld_k, n_kv_heads, head_dim)) return st;
   if (mes_status st = check_rows(who, "v", v, ld_v, n_kv_heads, head_dim)) return st;
   if (mes_status st = check_rows(who, "out", out, ld_out, n_heads, head_dim)) return st;
+  if (mes_status st = check_prompt_workspace(who, T, n_seqs, n_heads, n_kv_heads, head_dim, workspace, workspace_bytes)) return st;
   PromptArgs a{};
+  a.ws = workspace;
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.out = (uint16_t*)out;
   a.q_offsets = seq_offsets;
   a.T = T; a.n_seqs = n_seqs; a.n_heads = n_heads; a.n_kv_heads = n_kv_heads; a.head_dim = head_dim;
@@ -385,7 +402,7 @@ mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, i
 }
 
 mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, int T, int n_heads, int ld_q,
-                           float scale, void* out, int ld_out, void* stream) {
+                           float scale, void* out, int ld_out, void* workspace, size_t workspace_bytes, void* stream) {
   static const char who[] = "mes_attn_extend";
   if (mes_status st = check_kv(who, kv, layer)) return st;
   if (mes_status st = check_seqs(who, kv, seqs, true)) return st;
@@ -396,7 +413,9 @@ mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, co
   if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, kv->head_dim)) return st;
   if (mes_status st = check_rows(who, "out", out, ld_out, n_heads, kv->head_dim)) return st;
   const bool fp8 = kv->dtype == MES_KV_E4M3;
+  if (mes_status st = check_prompt_workspace(who, T, seqs->n_seqs, n_heads, kv->n_kv_heads, kv->head_dim, workspace, workspace_bytes)) return st;
   PromptArgs a{};
+  a.ws = workspace;
   a.q = (const uint16_t*)q; a.out = (uint16_t*)out;
   a.k = (const uint16_t*)((const char*)kv->k + layer * kv_layer_bytes(*kv));
   a.v = (const uint16_t*)((const char*)kv->v + layer * kv_layer_bytes(*kv));

@@ -33,8 +33,10 @@ struct PromptArgs {
   int T, n_seqs, n_heads, n_kv_heads, head_dim, n_pages, page_shift, table_pages, capacity;
   int ld_q, ld_k, ld_v, ld_out;
   float scale;
+  void* ws;                            // nullptr: no item is cut
 };
 enum { KV_PACKED = 0, KV_PAGED = 1, KV_PAGED_E4M3 = 2 };
+size_t attn_prompt_workspace_bytes(int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim);
 hipError_t launch_attn_prompt(const PromptArgs& a, int source, hipStream_t s);
 
 // ---- implemented in mes_attn_decode.hip ---------------------------------------------------------

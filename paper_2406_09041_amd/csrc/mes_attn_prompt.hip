@@ -3,72 +3,143 @@
 //   m = max s_j (kept within kSlack of it), p_j = 2^(s_j log2e - m), l = sum p_j, o = sum p_j v_j / l
 // in one pass over the keys, 64 at a time, nothing of the scores in memory (mes_attn_tiles.h).
 //
-// A workgroup is 4 wavefronts of 64 query rows: of up to 4 heads that share keys and values (all of them then see as many keys,
-// and no wavefront waits for another), else of consecutive rows of one head.
+// A workgroup is 4 wavefronts of 32 query rows: of up to 4 heads that share keys and values (all of them then see as many keys,
+// and no wavefront waits for another), else of consecutive rows of one head.  Where some of these items see so many keys that they
+// would work long after the others, the call is cut: items one after the other make a line of (rows x keys), which is cut into equal
+// parts, one per workgroup, wherever that falls.  Pieces of an item leave their sums in the workspace and k_join_prompt adds them up.
+// The lengths are on the device, so every workgroup finds its part by itself.
 #include "mes_attn_tiles.h"
 
 namespace mes {
 namespace {
+
+constexpr int kHeld = 512;             // workgroups that the chip holds, 2 per compute unit
+constexpr int kMostCut = 1024;         // items of a call that is cut: with more, no compute unit is without work for long
+constexpr int kLeastPart = 256;        // keys of a workgroup's part
 
 // The part of the call a workgroup works on
 struct Item {
   int seq, row0, rows, tile, before;   // sequence; its first row in the call; its rows; tile of R of them; tokens before row 0
 };
 
-// Item j of the call.  Up to 64 sequences: items in order of the keys they see, most first (in units of R rows), so that no long
-// one starts last; lane s counts for sequence s.  More: tile t of sequence s has number floor(o[s] / R) + s + t, which leaves gaps
-// (no item) but needs no sum over the sequences before it; the last first, as they see most of their sequence.
 template <int SRC>
-__device__ bool find_item(const PromptArgs& a, int R, int j, int slots, Item& it) {
+__device__ __forceinline__ int rows_of(const PromptArgs& a, int s, int& lo) {
+  lo = min(max(a.q_offsets[s], 0), a.T);
+  return max(min(a.q_offsets[s + 1], a.T) - lo, 0);
+}
+
+// Up to 64 sequences: lane s looks after sequence s.  Keys are counted in units of R: item t of a sequence sees about base + t + 1.
+struct Lanes {
+  int lo, n, before, tiles, base;      // first row, rows, tokens before them; items; keys before the rows
+  int all_items, longest;
+  int chunk, all;                      // units of a workgroup's part (0: the call is not cut), and of the call
+  int items_before, units_before, units;
+};
+
+template <int SRC>
+__device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
   const int lane = threadIdx.x & 63;
-  auto rows_of = [&](int s, int& lo) {
-    lo = min(max(a.q_offsets[s], 0), a.T);
-    return max(min(a.q_offsets[s + 1], a.T) - lo, 0);
-  };
+  Lanes y = {};
+  if (lane < a.n_seqs) {
+    y.n = rows_of<SRC>(a, lane, y.lo);
+    if (SRC != KV_PACKED) y.before = max(a.kv_len[lane], 0) - y.n;
+  }
+  y.tiles = (y.n + R - 1) / R;
+  y.base = (max(y.before, 0) + R - 1) / R;
+  y.all_items = wave_sum(y.tiles);
+  y.longest = wave_max(y.tiles ? y.base + y.tiles : 0);
+  if (!may_cut || y.all_items * columns > kMostCut) return y;
+  y.units = y.tiles * y.base + y.tiles * (y.tiles + 1) / 2;
+  int units = y.units, items = y.tiles;                  // up to and with the lane
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(units, o), i = __shfl_up(items, o);
+    if (lane >= o) { units += u; items += i; }
+  }
+  y.units_before = units - y.units;
+  y.items_before = items - y.tiles;
+  y.all = __shfl(units, 63);
+  const int parts = max(kHeld / columns, 1), share = max((y.all + parts - 1) / parts, kLeastPart / R);
+  // an item may take half as long again as a share: pieces cost about as much
+  if (2 * y.longest > 3 * share) y.chunk = share;
+  return y;
+}
+
+__device__ __forceinline__ void pick(const Lanes& y, int s, int tile, Item& it) {
+  it.seq = s;
+  it.tile = tile;
+  it.row0 = __shfl(y.lo, s);
+  it.rows = __shfl(y.n, s);
+  it.before = __shfl(y.before, s);
+}
+
+// The item that unit u of the line belongs to; returns the unit's place in it
+__device__ int item_at(const Lanes& y, int u, Item& it, int& item) {
+  const int s = __builtin_ctzll(__ballot(u >= y.units_before && u < y.units_before + y.units));
+  const int base = __shfl(y.base, s), at = u - __shfl(y.units_before, s);
+  int low = 0, high = __shfl(y.tiles, s) - 1;             // last tile that begins at or before the unit
+  while (low < high) {
+    const int mid = (low + high + 1) >> 1;
+    if (mid * base + mid * (mid + 1) / 2 <= at) low = mid; else high = mid - 1;
+  }
+  pick(y, s, low, it);
+  item = __shfl(y.items_before, s) + low;
+  return at - (low * base + low * (low + 1) / 2);
+}
+
+// Item j of a call that is not cut.  Up to 64 sequences: items in order of the keys they see, most first, so that no long one starts
+// last.  More: tile t of sequence s has number floor(o[s] / R) + s + t, which leaves gaps (no item) but needs no sum over the
+// sequences before it; the last first, as they see most of their sequence.
+template <int SRC>
+__device__ bool item_number(const PromptArgs& a, const Lanes& y, int R, int j, int slots, Item& it) {
   if (a.n_seqs <= 64) {
-    int lo = 0, n = 0, before = 0;
-    if (lane < a.n_seqs) {
-      n = rows_of(lane, lo);
-      if (SRC != KV_PACKED) before = max(a.kv_len[lane], 0) - n;
-    }
-    const int tiles = (n + R - 1) / R, base = max(before, 0) / R;
-    if (j >= wave_sum(tiles)) return false;
+    const int lane = threadIdx.x & 63;
+    if (j >= y.all_items) return false;
     // the level L with C(L + 1) <= j < C(L), C(L) = number of tiles with base + t >= L
-    auto count = [&](int level) { return wave_sum(min(max(base + tiles - max(level, base), 0), tiles)); };
-    int low = 0, high = wave_max(base + tiles);           // C(low) > j >= C(high) = 0
+    auto count = [&](int level) { return wave_sum(min(max(y.base + y.tiles - max(level, y.base), 0), y.tiles)); };
+    int low = 0, high = y.longest;                        // C(low) > j >= C(high) = 0
     while (high - low > 1) {
       const int mid = low + (high - low) / 2;
       if (count(mid) > j) low = mid; else high = mid;
     }
     const int rank = j - count(low + 1);
-    const bool mine = base <= low && low < base + tiles;
+    const bool mine = y.base <= low && low < y.base + y.tiles;
     const uint64_t who = __ballot(mine);
-    const bool chosen = mine && __popcll(who & ((1ull << lane) - 1)) == rank;
-    const int s = __builtin_ctzll(__ballot(chosen));
-    it.seq = s;
-    it.row0 = __shfl(lo, s);
-    it.rows = __shfl(n, s);
-    it.before = __shfl(before, s);
-    it.tile = low - __shfl(base, s);
+    const int s = __builtin_ctzll(__ballot(mine && __popcll(who & ((1ull << lane) - 1)) == rank));
+    pick(y, s, low - __shfl(y.base, s), it);
     return true;
   }
   j = slots - 1 - j;
+  if (j < 0) return false;
   int lo = 0, hi = a.n_seqs - 1;                           // last s with floor(o[s] / R) + s <= j
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (max(a.q_offsets[mid], 0) / R + mid <= j) lo = mid; else hi = mid - 1;
   }
   it.seq = lo;
-  it.rows = rows_of(lo, it.row0);
+  it.rows = rows_of<SRC>(a, lo, it.row0);
   it.tile = j - max(a.q_offsets[lo], 0) / R - lo;
   it.before = SRC != KV_PACKED ? max(a.kv_len[lo], 0) - it.rows : 0;
   return it.tile >= 0 && it.tile < (it.rows + R - 1) / R;
 }
 
+// The pieces' results, per slot: (max, sum) of the 128 rows of the wavefronts, and their weighted values in the order of the
+// accumulators: [wavefront][4 dimensions: 8 (i / 4) + half][32 rows] x 4.  Part j of item i has slot i + j: both grow along the line,
+// one of them from piece to piece.
+struct PieceLayout {
+  size_t o, total;
+};
+__host__ __device__ inline PieceLayout piece_layout(int slots, int head_dim) {
+  PieceLayout y;
+  y.o = (size_t)slots * 4 * kWaveRows * sizeof(float2);
+  y.total = y.o + (size_t)slots * 4 * kWaveRows * head_dim * sizeof(float);
+  return y;
+}
+
 // Every row once more, key by key and with no key that it does not see: the way out where a value that some rows do not see is infinite
 // or NaN (a weight of 0 times it is NaN, also in the rows that must not notice).
 template <int D, int SRC>
-__device__ __forceinline__ void attend_by_key(TileRows<D>& w, Stage<D, SRC>& stage, int n_all, const int (&last)[NB], float scale) {
+__device__ __forceinline__ void attend_by_key(TileRows<D>& w, Stage<D, SRC>& stage, int first, int n_all, const int (&last)[NB], float scale) {
   constexpr int KS = D / 16, DT = D / 32;
   const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
@@ -79,7 +150,7 @@ __device__ __forceinline__ void attend_by_key(TileRows<D>& w, Stage<D, SRC>& sta
     for (int dt = 0; dt < DT; ++dt) w.acc[b][dt] = f32x16{};
   }
   stage.batch = -64;
-  for (int t = 0; t < n_all; ++t) {
+  for (int t = first; t < first + n_all; ++t) {
     barrier();                                                      // nobody reads the tiles of LDS any more
     stage.look_up(t);
     stage.request(t, 0);
@@ -125,30 +196,56 @@ __device__ __forceinline__ void attend_by_key(TileRows<D>& w, Stage<D, SRC>& sta
   }
 }
 
-// heads: heads of one workgroup (1, 2 or 4, a divisor of the heads per key / value head)
+// heads: heads of one workgroup (1, 2 or 4, a divisor of the heads per key / value head); slots: see item_number; cut_slots: what the
+// workspace has room for (0: the call is not cut)
 template <int D, int SRC>
-__global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, int slots, int heads) {
+__global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, int slots, int heads, int cut_slots) {
   constexpr int KS = D / 16, DT = D / 32;
   __shared__ __align__(16) TileLds<D> lds;
   __shared__ int lds_again;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int R = 4 * kWaveRows / heads, columns = a.n_heads / heads;  // rows of an item, workgroups of one item
-
-  Item it;
-  if (!find_item<SRC>(a, R, blockIdx.x / columns, slots, it)) return;
-  it.seq = uniform(it.seq); it.row0 = uniform(it.row0); it.rows = uniform(it.rows); it.tile = uniform(it.tile); it.before = uniform(it.before);
   // consecutive workgroups go to the XCDs in turn: those that share keys and values come n_kv_heads apart, which puts them on
   // one XCD (8, 16, 40 ... key / value heads), whose L2 then fetches them once
-  const int hx = blockIdx.x % columns, kvh = hx % a.n_kv_heads;
+  const int hx = blockIdx.x % columns, part = blockIdx.x / columns, kvh = hx % a.n_kv_heads;
   const int head = kvh * (a.n_heads / a.n_kv_heads) + hx / a.n_kv_heads * heads + wave % heads;
 
-  // keys [0, kv_end) are seen by some row of the workgroup
-  const int row_first = it.tile * R, capacity = SRC == KV_PACKED ? 0x7fffffff : a.capacity;
-  const int kv_end = min(it.before + min(row_first + R, it.rows), capacity);
-  const int n_all = kv_end > 0 ? (kv_end + kTile - 1) / kTile : 0;
+  // kept in LDS: across the loop below there are no registers for it
+  __shared__ Lanes lds_lanes[64];
+  int chunk = 0, all = 0;
+  if (a.n_seqs <= 64) {
+    const Lanes y = look<SRC>(a, R, columns, cut_slots > 0);
+    if (wave == 0) lds_lanes[lane] = y;
+    chunk = uniform(y.chunk);
+    all = uniform(y.all);
+  }
+  // the part of the line; not cut: one round for the one item
+  const int part_end = chunk ? (int)min((int64_t)(part + 1) * chunk, (int64_t)all) : 1;
+  for (int u = chunk ? (int)min((int64_t)part * chunk, (int64_t)all) : 0; u < part_end;) {
+  __syncthreads();                                                   // the last piece's reads of LDS are over
+  const Lanes y = lds_lanes[lane];
+  Item it;
+  int from = 0, to = 1, whole = 1, item = 0;                         // units [from, to) of the item's `whole`
+  if (chunk) {
+    from = uniform(item_at(y, u, it, item));
+    item = uniform(item);
+    whole = uniform((max(it.before, 0) + R - 1) / R + it.tile + 1);
+    to = min(from + part_end - u, whole);
+  } else if (!uniform(item_number<SRC>(a, y, R, part, slots, it))) {
+    return;
+  }
+  u = uniform(u + to - from);
+  it.seq = uniform(it.seq); it.row0 = uniform(it.row0); it.rows = uniform(it.rows); it.tile = uniform(it.tile); it.before = uniform(it.before);
+  const int row_first = it.tile * R;
+
+  // keys [kTile first, kv_end) are seen by some row of the workgroup
+  const int capacity = SRC == KV_PACKED ? 0x7fffffff : a.capacity;
+  const int first = uniform(from * R / kTile), piece_end = to < whole ? to * R / kTile * kTile : 0x7fffffff;
+  const int kv_end = uniform(min(min(it.before + min(row_first + R, it.rows), capacity), piece_end));
+  const int n_all = kv_end > first * kTile ? (kv_end + kTile - 1) / kTile - first : 0;
   const int wave_row = row_first + wave / heads * kWaveRows;         // the wavefront's first row
-  const int high = min(it.before + min(wave_row + kWaveRows, it.rows), capacity);   // keys seen by its last row
-  const int n = wave_row < it.rows && high > 0 ? (high + kTile - 1) / kTile : 0;
+  const int high = min(it.before + min(wave_row + kWaveRows, it.rows), kv_end);     // keys seen by its last row
+  const int n = wave_row < it.rows && high > first * kTile ? (high + kTile - 1) / kTile - first : 0;
   int last[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) last[b] = it.before + wave_row + 32 * b + col;
@@ -183,7 +280,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
   const float scale = a.scale * kLog2e * (SRC == KV_PAGED_E4M3 ? a.k_scale[kvh] : 1.0f);
   if (threadIdx.x == 0) lds_again = 0;
   if (n_all > 0) {
-    attend_tiles<D, SRC>(w, stage, 0, n, n_all, it.before + wave_row, last, scale);
+    attend_tiles<D, SRC>(w, stage, first, n, n_all, it.before + wave_row, last, scale);
     float test = 0.0f;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -193,9 +290,27 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
         for (int i = 0; i < 16; ++i) test = fmaf(w.acc[b][dt][i], 0.0f, test);
     if (test != test) lds_again = 1;
     __syncthreads();
-    if (uniform(lds_again)) attend_by_key<D, SRC>(w, stage, n_all, last, scale);
+    if (uniform(lds_again)) attend_by_key<D, SRC>(w, stage, first, n_all, last, scale);
   }
 
+  if (to - from < whole) {
+    const PieceLayout y = piece_layout(cut_slots, D);
+    const int slot = (item + part) * columns + hx;
+    char* ws = static_cast<char*>(a.ws);
+    float2* ml = reinterpret_cast<float2*>(ws) + (size_t)slot * 4 * kWaveRows + wave * kWaveRows;
+    f32x4* o = reinterpret_cast<f32x4*>(ws + y.o) + ((size_t)slot * 4 + wave) * kWaveRows * (D / 4);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const float l = w.l[b] + other_half(w.l[b]);
+      if (half == 0) ml[32 * b + col] = make_float2(w.m[b], l);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          o[((dt * 4 + i) * 2 + half) * kWaveRows + 32 * b + col] = f32x4{w.acc[b][dt][4 * i], w.acc[b][dt][4 * i + 1], w.acc[b][dt][4 * i + 2], w.acc[b][dt][4 * i + 3]};
+    }
+    continue;
+  }
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const int row = wave_row + 32 * b + col;
@@ -210,22 +325,123 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
         *reinterpret_cast<u32x2*>(dst + 32 * dt + 8 * i) =
             u32x2{pack2(w.acc[b][dt][4 * i] * inv, w.acc[b][dt][4 * i + 1] * inv), pack2(w.acc[b][dt][4 * i + 2] * inv, w.acc[b][dt][4 * i + 3] * inv)};
   }
+  }
+}
+
+// Adds up the pieces of the items that were cut.  A workgroup's job is 32 rows and 32 dimensions of an item, its wavefronts share out the
+// pieces; blockIdx.x is (item, heads), blockIdx.y takes every gridDim.y-th job of it.
+template <int D, int SRC>
+__global__ __launch_bounds__(kTileThreads) void k_join_prompt(PromptArgs a, int heads, int cut_slots) {
+  constexpr int kQuads = 4;                                          // groups of 4 dimensions x 2 halves per job
+  __shared__ f32x4 part[4][kQuads][64];
+  __shared__ float2 part_ml[4][64];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int R = 4 * kWaveRows / heads, columns = a.n_heads / heads, hx = blockIdx.x % columns, kvh = hx % a.n_kv_heads;
+  const int item = blockIdx.x / columns;
+  const Lanes y = look<SRC>(a, R, columns, true);
+  const int chunk = uniform(y.chunk);
+  if (!chunk || item >= y.all_items) return;
+  const int s = __builtin_ctzll(__ballot(item >= y.items_before && item < y.items_before + y.tiles));
+  const int tile = uniform(item - __shfl(y.items_before, s)), base = uniform(__shfl(y.base, s));
+  const int u = uniform(__shfl(y.units_before, s)) + tile * base + tile * (tile + 1) / 2;
+  const int part0 = u / chunk, pieces = (u + base + tile) / chunk - part0 + 1;
+  if (pieces == 1) return;
+  const int row0 = uniform(__shfl(y.lo, s)) + tile * R, rows = min(R, uniform(__shfl(y.n, s)) - tile * R);
+  const char* ws = static_cast<const char*>(a.ws);
+  const size_t slot = (size_t)(item + part0) * columns + hx, step_ml = (size_t)columns * 4 * kWaveRows, step_o = step_ml * (D / 4);
+  for (int job = blockIdx.y; job < 4 * (D / 32); job += gridDim.y) {
+    const int part_wave = job % 4, q0 = job / 4 * kQuads, row = part_wave / heads * kWaveRows + col;
+    if (part_wave / heads * kWaveRows >= rows) continue;
+    const float2* ml = reinterpret_cast<const float2*>(ws) + (slot * 4 + part_wave) * kWaveRows + col;
+    const f32x4* o = reinterpret_cast<const f32x4*>(ws + piece_layout(cut_slots, D).o) + ((slot * 4 + part_wave) * (D / 4) + 2 * q0 + half) * kWaveRows + col;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 x[kQuads] = {};
+    for (int p = wave; p < pieces; p += 4) {
+      const float2 v = ml[p * step_ml];
+      f32x4 r[kQuads];
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q) r[q] = o[p * step_o + q * 2 * kWaveRows];
+      const float raised = fmaxf(m, v.x), to = raised == -INFINITY ? 0.0f : raised;
+      const float old = exp2_fast(m - to), f = exp2_fast(v.x - to);
+      m = raised;
+      l = l * old + v.y * f;
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q) x[q] = x[q] * old + r[q] * f;
+    }
+    __syncthreads();
+    part_ml[wave][lane] = make_float2(m, l);
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) part[wave][q][lane] = x[q];
+    __syncthreads();
+    // wavefront w finishes group w
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 all = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, part_ml[w][lane].x);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast(part_ml[w][lane].x - (top == -INFINITY ? 0.0f : top));
+      sum += part_ml[w][lane].y * f;
+      all += part[w][wave][lane] * f;
+    }
+    if (row < rows) {
+      const int head = kvh * (a.n_heads / a.n_kv_heads) + hx / a.n_kv_heads * heads + part_wave % heads;
+      const float inv = sum == 0.0f ? 0.0f : (SRC == KV_PAGED_E4M3 ? a.v_scale[kvh] : 1.0f) / sum;
+      uint16_t* dst = a.out + (size_t)(row0 + row) * a.ld_out + (size_t)head * D + 8 * (q0 + wave) + 4 * half;
+      *reinterpret_cast<u32x2*>(dst) = u32x2{pack2(all[0] * inv, all[1] * inv), pack2(all[2] * inv, all[3] * inv)};
+    }
+  }
+}
+
+inline int heads_of(int group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
+// enough items for every way T rows can be shared out over the sequences
+inline int64_t slots_of(int T, int n_seqs, int heads) { return (int64_t)T / (4 * kWaveRows / heads) + n_seqs; }
+// slots of a call's pieces: see PieceLayout
+inline int cut_slots_of(int64_t workgroups) { return (int)std::min<int64_t>(workgroups, kMostCut) + kHeld; }
+
+// Whether look() could cut a call of packed prompts whose sequences take up all T rows: for some length of the longest, the others
+// sharing the rest evenly, which is the least work there can be beside it.
+bool packed_may_cut(int T, int n_seqs, int R, int columns) {
+  const double rows = (double)T / R;
+  for (double l = rows / n_seqs; l < 1.2 * rows; l *= 1.1) {
+    const double longest = std::min(l + 1, rows + 1), rest = std::max(rows - longest, 0.0);
+    const double work = 0.5 * (longest * longest + (n_seqs > 1 ? rest * rest / (n_seqs - 1) : 0.0));
+    if (2 * longest > 3 * std::max(work * columns / kHeld, (double)kLeastPart / R)) return true;
+  }
+  return false;
 }
 
 template <int D>
 hipError_t launch(const PromptArgs& a, int source, hipStream_t s) {
-  const int group = a.n_heads / a.n_kv_heads, heads = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
-  // enough items for every way T rows can be shared out over the sequences
-  const int64_t slots = (int64_t)a.T / (4 * kWaveRows / heads) + a.n_seqs, workgroups = slots * (a.n_heads / heads);
-  if (workgroups > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)workgroups);
-  if (source == KV_PACKED) k_attn_prompt<D, KV_PACKED><<<grid, kTileThreads, 0, s>>>(a, (int)slots, heads);
-  else if (source == KV_PAGED) k_attn_prompt<D, KV_PAGED><<<grid, kTileThreads, 0, s>>>(a, (int)slots, heads);
-  else k_attn_prompt<D, KV_PAGED_E4M3><<<grid, kTileThreads, 0, s>>>(a, (int)slots, heads);
+  const int heads = heads_of(a.n_heads / a.n_kv_heads), columns = a.n_heads / heads;
+  const int64_t slots = slots_of(a.T, a.n_seqs, heads), workgroups = slots * columns;
+  if (workgroups > 0x7fff0000) return hipErrorInvalidValue;
+  // not cut: where no item can be much longer than the shortest part; with capacities at which the line would pass 31 bits
+  const int longest = source == KV_PACKED ? a.T : a.capacity;
+  const bool cut = a.ws && a.n_seqs <= 64 && columns <= kHeld && longest > 3 * kLeastPart / 2 && longest <= 1 << 24 &&
+                   (source != KV_PACKED || packed_may_cut(a.T, a.n_seqs, 4 * kWaveRows / heads, columns));
+  const int cut_slots = cut ? cut_slots_of(workgroups) : 0;
+  const dim3 grid((unsigned)std::max<int64_t>(workgroups, cut ? kHeld / columns * columns : 0));
+  // joining workgroups: enough to fill the chip where there are few items
+  const int64_t items = std::min<int64_t>(workgroups, kMostCut);
+  const dim3 join((unsigned)items, (unsigned)std::max<int64_t>(1, std::min<int64_t>(4 * (D / 32), 2048 / items)));
+  auto go = [&](auto src) {
+    constexpr int SRC = decltype(src)::value;
+    k_attn_prompt<D, SRC><<<grid, kTileThreads, 0, s>>>(a, (int)slots, heads, cut_slots);
+    if (cut) k_join_prompt<D, SRC><<<join, kTileThreads, 0, s>>>(a, heads, cut_slots);
+  };
+  if (source == KV_PACKED) go(std::integral_constant<int, KV_PACKED>{});
+  else if (source == KV_PAGED) go(std::integral_constant<int, KV_PAGED>{});
+  else go(std::integral_constant<int, KV_PAGED_E4M3>{});
   return hipGetLastError();
 }
 
 }  // namespace
+
+size_t attn_prompt_workspace_bytes(int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
+  const int heads = heads_of(n_heads / n_kv_heads);
+  return piece_layout(cut_slots_of(slots_of(T, n_seqs, heads) * (n_heads / heads)), head_dim).total;
+}
 
 hipError_t launch_attn_prompt(const PromptArgs& a, int source, hipStream_t s) {
   return a.head_dim == 128 ? launch<128>(a, source, s) : launch<64>(a, source, s);

@@ -251,10 +251,8 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
   // an 8-bit cache pass through registers, keys during the first half of a tile's work, values during the second
   const int end_all = first + n_all, end = first + n;
   auto before = [&](int t) {
-    if (t > first) {
-      stage.arrive();
-      barrier();
-    }
+    stage.arrive();
+    barrier();                                                       // also at the first tile: its keys have been read, and make room
     if (t + 2 < end_all) {
       stage.look_up(t + 2);
       stage.request(t + 2, 0);

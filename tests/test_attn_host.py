@@ -30,13 +30,13 @@ def _append(kv=None, layer=0, seqs=None, q=FAKE, k=FAKE, v=FAKE, T=5, heads=4, l
     return lib.mes_kv_append(ctypes.byref(kv), layer, ctypes.byref(seqs), q, k, v, T, heads, ld_q, ld_k, ld_v, rotary, n_pos, q_out, ld_o, None)
 
 
-def _prompt(q=FAKE, k=FAKE, v=FAKE, T=5, n=1, off=FAKE, heads=4, kvh=2, dim=64, ld_q=256, ld_k=128, ld_v=128, scale=0.125, out=FAKE, ld_o=256):
-    return lib.mes_attn_prompt(q, k, v, T, n, off, heads, kvh, dim, ld_q, ld_k, ld_v, scale, out, ld_o, None)
+def _prompt(q=FAKE, k=FAKE, v=FAKE, T=5, n=1, off=FAKE, heads=4, kvh=2, dim=64, ld_q=256, ld_k=128, ld_v=128, scale=0.125, out=FAKE, ld_o=256, ws=None, wsb=0):
+    return lib.mes_attn_prompt(q, k, v, T, n, off, heads, kvh, dim, ld_q, ld_k, ld_v, scale, out, ld_o, ws, wsb, None)
 
 
-def _extend(kv=None, layer=0, seqs=None, q=FAKE, T=5, heads=4, ld_q=256, scale=0.125, out=FAKE, ld_o=256):
+def _extend(kv=None, layer=0, seqs=None, q=FAKE, T=5, heads=4, ld_q=256, scale=0.125, out=FAKE, ld_o=256, ws=None, wsb=0):
     kv, seqs = kv or _kv(), seqs or _seqs()
-    return lib.mes_attn_extend(ctypes.byref(kv), layer, ctypes.byref(seqs), q, T, heads, ld_q, scale, out, ld_o, None)
+    return lib.mes_attn_extend(ctypes.byref(kv), layer, ctypes.byref(seqs), q, T, heads, ld_q, scale, out, ld_o, ws, wsb, None)
 
 
 def _decode(kv=None, layer=0, seqs=None, q=FAKE, heads=4, ld_q=256, seg=(0, 1, 3), pre=(5, 0), E=None, scale=0.125, out=FAKE, ld_o=256, ws=FAKE, wsb=1 << 30):
@@ -94,6 +94,12 @@ def test_prompt_and_extend_errors():
         assert call(heads=3) == 2 and call(heads=0) == 2 and call(heads=130) == 2         # a multiple of 2, up to 64 times
         for scale in (0.0, -1.0, float("nan"), float("inf")):
             assert call(scale=scale) == 2
+        n = 1 if call is _prompt else 3
+        need = lib.mes_attn_prompt_workspace_bytes(5, n, 4, 2, 64)
+        assert need > 0 and call(ws=FAKE, wsb=need - 1) == 7 and call(ws=ODD, wsb=need) == 6       # NULL is fine: no item is cut
+    for bad in ((-1, 1, 4, 2, 64), (5, -1, 4, 2, 64), (5, 4097, 4, 2, 64), (5, 1, 5, 2, 64), (5, 1, 4, 2, 32)):
+        assert lib.mes_attn_prompt_workspace_bytes(*bad) == 0
+    assert lib.mes_attn_prompt_workspace_bytes(1 << 20, 64, 32, 8, 128) < 128 << 20
     assert _prompt(k=None) == 1 and _prompt(v=ODD) == 6 and _prompt(ld_k=64) == 2 and _prompt(ld_v=129) == 2
     assert _prompt(off=None) == 1 and _prompt(n=-1) == 2 and _prompt(n=4097) == 2 and _prompt(n=0) == 0
     assert _prompt(dim=80) == 2 and _prompt(kvh=0) == 2

@@ -198,6 +198,53 @@ def test_extend_with_lengths_and_pages_that_do_not_fit(e4m3):
     _check(out[150:200], want, tol, "positions past the table")
 
 
+CUTS = [  # few rows behind many tokens: their keys are shared out
+    ([3000], [1], 2, 1, 64, 16, 1), ([3000], [5], 4, 1, 128, 16, 1), ([4000, 300, 10], [40, 300, 1], 8, 2, 64, 32, 2), ([2500] * 3, [100, 33, 0], 3, 1, 128, 64, 3),
+    ([5000, 0, 700], [2, 0, 129], 6, 1, 64, 256, 4), ([1500], [700], 1, 1, 128, 16, 5),
+]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("lens,news,heads,kvh,dim,page,seed", CUTS)
+def test_extend_with_keys_shared_out(lens, news, heads, kvh, dim, page, seed, e4m3):
+    c = Paged(seed, lens, kvh, dim, page, e4m3)
+    g = torch.Generator().manual_seed(seed)
+    off = [0]
+    for n in news:
+        off.append(off[-1] + n)
+    q = _rows(g, off[-1] + 2, heads, dim, 2.0)
+    out = torch.full((off[-1] + 2, heads, dim), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = mes.binding.prompt_workspace(off[-1] + 2, len(lens), heads, kvh, dim, DEV)
+    ws.fill_(255)                                                # scratch: what is in it does not matter
+    mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q.to(DEV), out, workspace=ws)
+    again = mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q.to(DEV))
+    torch.cuda.synchronize()
+    assert torch.all(out[off[-1]:] == 7.0)
+    assert torch.equal(out[:off[-1]].view(torch.int16), again[:off[-1]].view(torch.int16))
+    for s in range(len(lens)):
+        rows = sorted(set(range(0, news[s], 37)) | {0, news[s] - 1}) if news[s] else []
+        if rows:
+            pick = [off[s] + r for r in rows]
+            want, tol = O.attend(q[pick], c.k[s], c.v[s], [lens[s] - news[s] + r for r in rows], dim ** -0.5)
+            _check(out[pick], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("lens,heads,kvh", [([1700], 2, 1), ([2000, 5, 900], 3, 3), ([1100], 8, 2)])
+def test_prompts_with_keys_shared_out(lens, heads, kvh):
+    g = torch.Generator().manual_seed(len(lens))
+    T, dim = sum(lens), 128
+    q, k, v = _rows(g, T, heads, dim, 2.0), _rows(g, T, kvh, dim), _rows(g, T, kvh, dim)
+    off = [0]
+    for n in lens:
+        off.append(off[-1] + n)
+    out = mes.mes_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), _ints(off))
+    torch.cuda.synchronize()
+    for a, b in zip(off, off[1:]):
+        rows = sorted(set(range(0, b - a, 61)) | {b - a - 1})
+        want, tol = O.attend(q[a:b][rows], k[a:b], v[a:b], rows, dim ** -0.5)
+        _check(out[a:b][rows], want, tol, f"rows {a}..{b}")
+
+
 DECODES = [
     # lens, heads, kv heads, dim, page, segs, prefix
     ([1], 4, 2, 64, 16, None, None), ([0], 4, 2, 128, 16, None, None), ([31, 32, 33], 4, 1, 128, 16, None, None),
