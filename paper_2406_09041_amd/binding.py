@@ -23,7 +23,7 @@ MAX_EXPERTS = 64
 
 KV_BF16, KV_E4M3 = 0, 1
 MAX_SEQS = 4096
-SHORT_PROMPT = 384          # keys: rows that see no more are never shared out, and need no workspace
+SHORT_PROMPT = 704          # keys: rows that see no more are never shared out, and need no workspace
 
 STATUS_NAMES = {0: "MES_OK", 1: "MES_ERR_NULL", 2: "MES_ERR_SHAPE", 3: "MES_ERR_BITS", 4: "MES_ERR_SALIENT",
                 5: "MES_ERR_SEGMENTS", 6: "MES_ERR_ALIGN", 7: "MES_ERR_WORKSPACE", 8: "MES_ERR_DEVICE", 9: "MES_ERR_PAGES"}
@@ -576,25 +576,34 @@ class ExpertPool:
 
 # ---------------------------------------------------------------------------------------- attention and its paged cache
 
-def _call_on(device: torch.device, entry, *args) -> None:
-    """entry(*args, stream) on the device's current stream, with that device current during the call."""
-    if torch.cuda.current_device() == device.index:
-        _check(entry(*args, torch.cuda.current_stream(device).cuda_stream))
+# These calls take microseconds, and so do torch's friendlier forms of the questions below.
+_BF16, _INT32 = torch.bfloat16, torch.int32
+_raw_stream, _current = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+
+
+def _call_on(index: int, entry, *args) -> None:
+    """entry(*args, stream) on the current stream of device `index`, with that device current during the call."""
+    if _current() == index:
+        status = entry(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            _check(entry(*args, torch.cuda.current_stream(device).cuda_stream))
+        with torch.cuda.device(index):
+            status = entry(*args, _raw_stream(index))
+    if status:
+        _check(status)
 
 
-def _heads_of(name: str, t: torch.Tensor, device: torch.device) -> int:
-    """Checks rows [T, heads, head_dim] of bf16 whose heads lie one behind the other; returns how far rows are apart."""
-    assert t.dtype == torch.bfloat16 and t.dim() == 3 and t.device == device, f"{name}: bf16 [T, heads, head_dim] on {device}"
-    heads, dim = t.shape[1], t.shape[2]
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim), f"{name}: the heads of a row lie one behind the other"
-    return t.stride(0) if t.shape[0] > 1 else heads * dim
+def _rows(name: str, t: torch.Tensor, index: int):
+    """Checks rows [T, heads, head_dim] of bf16 on device `index` whose heads lie one behind the other: T, heads, head_dim, and how
+    far rows are apart."""
+    n, heads, dim = t.shape
+    step, head, one = t.stride()
+    assert t.dtype is _BF16 and t.get_device() == index and (one == 1 or dim == 1) and (head == dim or heads == 1), \
+        f"{name}: bf16 [T, heads, head_dim] on device {index}, the heads of a row one behind the other"
+    return n, heads, dim, step if n > 1 else heads * dim
 
 
-def _int32_on(name: str, t: torch.Tensor, device: torch.device) -> None:
-    assert t.dtype == torch.int32 and t.is_contiguous() and t.device == device, f"{name}: contiguous int32 on {device}"
+def _int32_on(name: str, t: torch.Tensor, index: int) -> None:
+    assert t.dtype is _INT32 and t.get_device() == index and t.is_contiguous(), f"{name}: contiguous int32 on device {index}"
 
 
 class KvCache:
@@ -622,7 +631,7 @@ class KvCache:
         for t in (k_scale, v_scale):
             assert (t is not None) == fp8, "scales belong to an e4m3 cache"
             assert t is None or (t.dtype == torch.float32 and t.shape == (k.shape[0], k.shape[2]) and t.is_contiguous() and t.device == k.device)
-        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device
+        self.k, self.v, self.k_scale, self.v_scale, self.device, self.index = k, v, k_scale, v_scale, k.device, k.get_device()
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
         self.desc = mes_kv(self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, KV_E4M3 if fp8 else KV_BF16,
                            k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if fp8 else None, v_scale.data_ptr() if fp8 else None)
@@ -634,13 +643,13 @@ class SeqBatch:
     None (one row per sequence), all on the GPU; their contents may change between calls."""
 
     def __init__(self, kv_len: torch.Tensor, page_table: torch.Tensor, q_offsets: Optional[torch.Tensor] = None):
-        self.device = kv_len.device
+        self.index = kv_len.get_device()
         n = kv_len.shape[0]
-        _int32_on("kv_len", kv_len, self.device)
-        _int32_on("page_table", page_table, self.device)
+        _int32_on("kv_len", kv_len, self.index)
+        _int32_on("page_table", page_table, self.index)
         assert kv_len.is_cuda and kv_len.dim() == 1 and page_table.dim() == 2 and page_table.shape[0] == n
         if q_offsets is not None:
-            _int32_on("q_offsets", q_offsets, self.device)
+            _int32_on("q_offsets", q_offsets, self.index)
             assert q_offsets.shape == (n + 1,)
         self.kv_len, self.page_table, self.q_offsets, self.n = kv_len, page_table, q_offsets, n
         self.desc = mes_seqs(n, page_table.shape[1], None if q_offsets is None else q_offsets.data_ptr(), kv_len.data_ptr(), page_table.data_ptr())
@@ -656,23 +665,32 @@ def rotary_table(n_positions: int, head_dim: int, base: float = 10000.0, device=
 def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                   rotary: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """Rotates the new rows' queries (returned; q_out may be q) and keys and puts keys and values into the cache's pages."""
-    dev, T = cache.device, k.shape[0]
-    assert batch.device == dev and v.shape == k.shape and k.shape[1:] == (cache.n_kv_heads, cache.head_dim)
-    ld_k, ld_v = _heads_of("k", k, dev), _heads_of("v", v, dev)
+    index = cache.index
+    T, kv_heads, dim, ld_k = _rows("k", k, index)
+    rows_v = _rows("v", v, index)
+    assert batch.index == index and rows_v[:3] == (T, kv_heads, dim) == (T, cache.n_kv_heads, cache.head_dim), "k, v: [T, n_kv_heads, head_dim] of the cache"
     heads = ld_q = ld_o = n_pos = 0
+    rot = src = dst = None
     if rotary is not None:
-        assert rotary.dtype == torch.float32 and rotary.is_contiguous() and rotary.device == dev and rotary.shape[1:] == (2, cache.head_dim // 2)
-        n_pos = rotary.shape[0]
+        assert rotary.dtype is torch.float32 and rotary.is_contiguous() and rotary.get_device() == index and rotary.shape[1:] == (2, dim // 2)
+        n_pos, rot = rotary.shape[0], rotary.data_ptr()
     if q is not None:
-        assert q.shape[0] == T and q.shape[2] == cache.head_dim
-        heads, ld_q = q.shape[1], _heads_of("q", q, dev)
+        n, heads, d, ld_q = _rows("q", q, index)
+        assert n == T and d == dim
         if q_out is None:
-            q_out = torch.empty((T, heads, cache.head_dim), dtype=torch.bfloat16, device=dev)
-        assert q_out.shape == q.shape
-        ld_o = _heads_of("q_out", q_out, dev)
-    _call_on(dev, lib.mes_kv_append, cache.ref, layer, batch.ref, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), T, heads,
-             ld_q, ld_k, ld_v, None if rotary is None else rotary.data_ptr(), n_pos, None if q is None else q_out.data_ptr(), ld_o)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        n, h, d, ld_o = _rows("q_out", q_out, index)
+        assert (n, h, d) == (T, heads, dim)
+        src, dst = q.data_ptr(), q_out.data_ptr()
+    _call_on(index, lib.mes_kv_append, cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3], rot, n_pos, dst, ld_o)
     return q_out if q is not None else None
+
+
+def _scratch(workspace: Optional[torch.Tensor], index: int):
+    if workspace is None:
+        return None, 0
+    assert workspace.get_device() == index and workspace.dtype is torch.uint8 and workspace.is_contiguous()
+    return workspace.data_ptr(), workspace.numel()
 
 
 def prompt_workspace(T: int, n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, device) -> torch.Tensor:
@@ -685,20 +703,21 @@ def mes_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_offse
     """Causal attention over packed prompts: q [T, heads, d], k and v [T, kv heads, d] (views of one buffer are fine),
     seq_offsets int32 [n + 1] on the GPU.  Returns [T, heads, d]; rows behind the last sequence are left as they are.
     workspace: one to share between stream-ordered calls (prompt_workspace), or None to allocate one."""
-    dev = q.device
-    T, heads, dim = q.shape
-    assert q.is_cuda and k.shape == v.shape and k.shape[0] == T and k.shape[2] == dim
-    _int32_on("seq_offsets", seq_offsets, dev)
+    index = q.get_device()
+    T, heads, dim, ld_q = _rows("q", q, index)
+    n, kv_heads, d, ld_k = _rows("k", k, index)
+    rows_v = _rows("v", v, index)
+    assert rows_v[:3] == (n, kv_heads, d) == (T, kv_heads, dim) and q.is_cuda, "k, v: [T, kv heads, head_dim], as many rows as q"
+    _int32_on("seq_offsets", seq_offsets, index)
     if out is None:
-        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
-    assert out.shape == q.shape
-    n, kv_heads = seq_offsets.shape[0] - 1, k.shape[1]
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    rows_o = _rows("out", out, index)
+    assert rows_o[:3] == (T, heads, dim)
+    n = seq_offsets.shape[0] - 1
     if workspace is None and T > SHORT_PROMPT:
-        workspace = prompt_workspace(T, n, heads, kv_heads, dim, dev)
-    _call_on(dev, lib.mes_attn_prompt, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, n, seq_offsets.data_ptr(),
-             heads, kv_heads, dim, _heads_of("q", q, dev), _heads_of("k", k, dev), _heads_of("v", v, dev),
-             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev),
-             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
+        workspace = prompt_workspace(T, n, heads, kv_heads, dim, q.device)
+    _call_on(index, lib.mes_attn_prompt, q.data_ptr(), k.data_ptr(), v.data_ptr(), T, n, seq_offsets.data_ptr(), heads, kv_heads, dim, ld_q, ld_k, rows_v[3],
+             dim ** -0.5 if scale is None else scale, out.data_ptr(), rows_o[3], *_scratch(workspace, index))
     return out
 
 
@@ -706,17 +725,17 @@ def mes_attn_extend(cache: KvCache, layer: int, batch: SeqBatch, q: torch.Tensor
                     scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Causal attention of the batch's new rows (its last tokens, already appended) over the cache.  workspace: as for
     mes_attn_prompt."""
-    dev = cache.device
-    T, heads, dim = q.shape
-    assert batch.device == dev and dim == cache.head_dim
+    index = cache.index
+    T, heads, dim, ld_q = _rows("q", q, index)
+    assert batch.index == index and dim == cache.head_dim
     if out is None:
-        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=dev)
-    assert out.shape == q.shape
-    if workspace is None and batch.page_table.shape[1] * cache.page_tokens > SHORT_PROMPT:
-        workspace = prompt_workspace(T, batch.n, heads, cache.n_kv_heads, dim, dev)
-    _call_on(dev, lib.mes_attn_extend, cache.ref, layer, batch.ref, q.data_ptr(), T, heads, _heads_of("q", q, dev),
-             dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev),
-             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    rows_o = _rows("out", out, index)
+    assert rows_o[:3] == (T, heads, dim)
+    if workspace is None and batch.desc.table_pages * cache.page_tokens > SHORT_PROMPT:
+        workspace = prompt_workspace(T, batch.n, heads, cache.n_kv_heads, dim, cache.device)
+    _call_on(index, lib.mes_attn_extend, cache.ref, layer, batch.ref, q.data_ptr(), T, heads, ld_q, dim ** -0.5 if scale is None else scale,
+             out.data_ptr(), rows_o[3], *_scratch(workspace, index))
     return out
 
 
@@ -727,24 +746,26 @@ class AttnDecode:
         self.cache, self.n_heads = cache, n_heads
         n = max(lib.mes_attn_decode_workspace_bytes(max_seqs, n_heads, cache.n_kv_heads, cache.head_dim), 16)
         self.ws = workspace if workspace is not None else torch.empty(n, dtype=torch.uint8, device=cache.device)
+        self.scratch = _scratch(self.ws, cache.index)
 
     def __call__(self, layer: int, batch: SeqBatch, q: torch.Tensor, seg_offsets: Optional[Sequence[int]] = None,
                  prefix_len: Optional[Sequence[int]] = None, out: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
         """q [n, heads, d], one row per sequence.  seg_offsets [E + 1] and prefix_len [E] (host): rows are sorted by expert and
         the sequences of expert e share their first prefix_len[e] tokens, which are then read once."""
-        dev = self.cache.device
-        n, heads, dim = q.shape
-        assert batch.device == dev and n == batch.n and heads == self.n_heads and dim == self.cache.head_dim
+        cache, index = self.cache, self.cache.index
+        n, heads, dim, ld_q = _rows("q", q, index)
+        assert batch.index == index and n == batch.n and heads == self.n_heads and dim == cache.head_dim
         if out is None:
-            out = torch.empty((n, heads, dim), dtype=torch.bfloat16, device=dev)
-        assert out.shape == q.shape
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        rows_o = _rows("out", out, index)
+        assert rows_o[:3] == (n, heads, dim)
         E, seg, pre = 0, None, None
         if seg_offsets is not None:
             E = len(prefix_len)
             assert len(seg_offsets) == E + 1
             seg, pre = (ctypes.c_int32 * (E + 1))(*seg_offsets), (ctypes.c_int32 * E)(*prefix_len)
-        _call_on(dev, lib.mes_attn_decode, self.cache.ref, layer, batch.ref, q.data_ptr(), heads, _heads_of("q", q, dev), E, seg, pre,
-                 dim ** -0.5 if scale is None else scale, out.data_ptr(), _heads_of("out", out, dev), self.ws.data_ptr(), self.ws.numel())
+        _call_on(index, lib.mes_attn_decode, cache.ref, layer, batch.ref, q.data_ptr(), heads, ld_q, E, seg, pre,
+                 dim ** -0.5 if scale is None else scale, out.data_ptr(), rows_o[3], *self.scratch)
         return out
 
 
@@ -752,7 +773,8 @@ def mes_kv_copy_pages(cache: KvCache, src: Sequence[int], dst: Sequence[int]) ->
     """Copies page src[i] to page dst[i] in all layers of keys and values (what PagePool.grow and .compact ask for)."""
     n = len(src)
     assert len(dst) == n
-    _call_on(cache.device, lib.mes_kv_copy_pages, cache.ref, (ctypes.c_int32 * n)(*src), (ctypes.c_int32 * n)(*dst), n)
+    pages = ctypes.c_int32 * n
+    _call_on(cache.index, lib.mes_kv_copy_pages, cache.ref, pages(*src), pages(*dst), n)
 
 
 class PagePool:

@@ -53,15 +53,27 @@ __device__ __forceinline__ u32x2 widen4(uint32_t w) {
   return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
-__device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+// Over the lanes of a wavefront, without LDS.  scan: the sum up to and with the lane; max: of values that are not negative.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_below(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+  v += from_below<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8: inside rows of 16
+  v += from_below<0x112, 0xf>(v);
+  v += from_below<0x114, 0xf>(v);
+  v += from_below<0x118, 0xf>(v);
+  v += from_below<0x142, 0xa>(v);   // row_bcast 15: row 0 to 1, 2 to 3
+  v += from_below<0x143, 0xc>(v);   // row_bcast 31: rows 0 and 1 to 2 and 3
   return v;
 }
+__device__ __forceinline__ int wave_sum(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
 __device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o));
-  return v;
+  v = max(v, from_below<0x111, 0xf>(v));
+  v = max(v, from_below<0x112, 0xf>(v));
+  v = max(v, from_below<0x114, 0xf>(v));
+  v = max(v, from_below<0x118, 0xf>(v));
+  v = max(v, from_below<0x142, 0xa>(v));
+  v = max(v, from_below<0x143, 0xc>(v));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 

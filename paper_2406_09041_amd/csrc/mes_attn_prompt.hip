@@ -5,17 +5,19 @@
 //
 // A workgroup is 4 wavefronts of 32 query rows: of up to 4 heads that share keys and values (all of them then see as many keys,
 // and no wavefront waits for another), else of consecutive rows of one head.  Where some of these items see so many keys that they
-// would work long after the others, the call is cut: items one after the other make a line of (rows x keys), which is cut into equal
-// parts, one per workgroup, wherever that falls.  Pieces of an item leave their sums in the workspace and k_join_prompt adds them up.
-// The lengths are on the device, so every workgroup finds its part by itself.
+// would work long after the others, the call is cut: the keys of every sequence in blocks, an item's part of a block is a workgroup's.
+// The parts of a block run at about the same time, so that its keys and values come from HBM once and then from L2 (parts cut
+// wherever an equal share ended were 4.2 TB/s of different tiles at a time: 120 us instead of @ for the prompts behind cached contexts that
+// the table of this operator measures).  The parts of an item leave their sums in the workspace and k_join_prompt adds them up.  The
+// lengths are on the device, so every workgroup finds its part by itself.
 #include "mes_attn_tiles.h"
 
 namespace mes {
 namespace {
 
-constexpr int kHeld = 512;             // workgroups that the chip holds, 2 per compute unit
+constexpr int kHeld = 512;             // workgroups that the chip holds, two per compute unit
 constexpr int kMostCut = 1024;         // items of a call that is cut: with more, no compute unit is without work for long
-constexpr int kLeastPart = 256;        // keys of a workgroup's part
+constexpr int kLeastPart = 256;        // keys of a block
 
 // The part of the call a workgroup works on
 struct Item {
@@ -32,9 +34,15 @@ __device__ __forceinline__ int rows_of(const PromptArgs& a, int s, int& lo) {
 struct Lanes {
   int lo, n, before, tiles, base;      // first row, rows, tokens before them; items; keys before the rows
   int all_items, longest;
-  int chunk, all;                      // units of a workgroup's part (0: the call is not cut), and of the call
-  int items_before, units_before, units;
+  int block, parts, ahead, all_parts;  // units of a block (0: the call is not cut); parts of the sequence, and before it
 };
+
+// Parts of the blocks below block b of a sequence: block i is seen by the items whose keys reach past its beginning.
+__device__ __forceinline__ int parts_below(int b, int block, int base, int tiles) {
+  const int full = min(b, base / block + 1);             // blocks that begin at or before base: all items
+  return full * tiles + (b - full) * (tiles + base) - block * ((b - full) * (full + b - 1) / 2);
+}
+__device__ __forceinline__ int first_item(int b, int block, int base) { return max(b * block - base, 0); }
 
 template <int SRC>
 __device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
@@ -49,42 +57,47 @@ __device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
   y.all_items = wave_sum(y.tiles);
   y.longest = wave_max(y.tiles ? y.base + y.tiles : 0);
   if (!may_cut || y.all_items * columns > kMostCut) return y;
-  y.units = y.tiles * y.base + y.tiles * (y.tiles + 1) / 2;
-  int units = y.units, items = y.tiles;                  // up to and with the lane
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(units, o), i = __shfl_up(items, o);
-    if (lane >= o) { units += u; items += i; }
+  const int units = wave_sum(y.tiles * y.base + y.tiles * (y.tiles + 1) / 2);
+  const int share = units / max(kHeld / columns, 1) + 1;  // of a workgroup, if all had the same
+  // A tile of keys takes a workgroup 1.1 us alone on its compute unit and 2.3 us beside another; writing and adding up parts about as long
+  // as 11 tiles (measured: 512 rows behind 4096 tokens 70 us cut and 87 whole; a prompt of 1024 tokens 38 us cut and 24 whole).
+  if (y.longest <= 21 * share / 8 + 11 * kTile / R) return y;
+  // parts of a share fit the chip at once; whole tiles (R is 32, 64 or 128)
+  int block = max(share + share / 8 + 1, kLeastPart / R);
+  block += R < kTile ? block & 1 : 0;
+  y.block = block;
+  y.parts = y.tiles ? parts_below((y.base + y.tiles + block - 1) / block, block, y.base, y.tiles) : 0;
+  // sequences in order of their longest rows
+  for (int k = 0; k < a.n_seqs; ++k) {
+    const int reach = __builtin_amdgcn_readlane(y.base + y.tiles, k), count = __builtin_amdgcn_readlane(y.parts, k);
+    if (reach > y.base + y.tiles || (reach == y.base + y.tiles && k < lane)) y.ahead += count;
+    y.all_parts += count;
   }
-  y.units_before = units - y.units;
-  y.items_before = items - y.tiles;
-  y.all = __shfl(units, 63);
-  const int parts = max(kHeld / columns, 1), share = max((y.all + parts - 1) / parts, kLeastPart / R);
-  // an item may take half as long again as a share: pieces cost about as much
-  if (2 * y.longest > 3 * share) y.chunk = share;
   return y;
 }
 
 __device__ __forceinline__ void pick(const Lanes& y, int s, int tile, Item& it) {
   it.seq = s;
   it.tile = tile;
-  it.row0 = __shfl(y.lo, s);
-  it.rows = __shfl(y.n, s);
-  it.before = __shfl(y.before, s);
+  it.row0 = __builtin_amdgcn_readlane(y.lo, s);
+  it.rows = __builtin_amdgcn_readlane(y.n, s);
+  it.before = __builtin_amdgcn_readlane(y.before, s);
 }
 
-// The item that unit u of the line belongs to; returns the unit's place in it
-__device__ int item_at(const Lanes& y, int u, Item& it, int& item) {
-  const int s = __builtin_ctzll(__ballot(u >= y.units_before && u < y.units_before + y.units));
-  const int base = __shfl(y.base, s), at = u - __shfl(y.units_before, s);
-  int low = 0, high = __shfl(y.tiles, s) - 1;             // last tile that begins at or before the unit
+// Part j of a call that is cut; block: which block of keys.  The blocks of a sequence one after the other, so that its short parts
+// (the last block of every item) come late.
+__device__ bool part_number(const Lanes& y, int j, Item& it, int& block) {
+  if (j >= y.all_parts) return false;
+  const int s = __builtin_ctzll(__ballot(y.ahead <= j && j < y.ahead + y.parts));
+  const int base = __builtin_amdgcn_readlane(y.base, s), tiles = __builtin_amdgcn_readlane(y.tiles, s), at = j - __builtin_amdgcn_readlane(y.ahead, s);
+  int low = 0, high = (base + tiles - 1) / y.block;       // last block whose parts begin at or before this one
   while (low < high) {
     const int mid = (low + high + 1) >> 1;
-    if (mid * base + mid * (mid + 1) / 2 <= at) low = mid; else high = mid - 1;
+    if (parts_below(mid, y.block, base, tiles) <= at) low = mid; else high = mid - 1;
   }
-  pick(y, s, low, it);
-  item = __shfl(y.items_before, s) + low;
-  return at - (low * base + low * (low + 1) / 2);
+  block = low;
+  pick(y, s, first_item(low, y.block, base) + at - parts_below(low, y.block, base, tiles), it);
+  return true;
 }
 
 // Item j of a call that is not cut.  Up to 64 sequences: items in order of the keys they see, most first, so that no long one starts
@@ -106,7 +119,7 @@ __device__ bool item_number(const PromptArgs& a, const Lanes& y, int R, int j, i
     const bool mine = y.base <= low && low < y.base + y.tiles;
     const uint64_t who = __ballot(mine);
     const int s = __builtin_ctzll(__ballot(mine && __popcll(who & ((1ull << lane) - 1)) == rank));
-    pick(y, s, low - __shfl(y.base, s), it);
+    pick(y, s, low - __builtin_amdgcn_readlane(y.base, s), it);
     return true;
   }
   j = slots - 1 - j;
@@ -123,16 +136,15 @@ __device__ bool item_number(const PromptArgs& a, const Lanes& y, int R, int j, i
   return it.tile >= 0 && it.tile < (it.rows + R - 1) / R;
 }
 
-// The pieces' results, per slot: (max, sum) of the 128 rows of the wavefronts, and their weighted values in the order of the
-// accumulators: [wavefront][4 dimensions: 8 (i / 4) + half][32 rows] x 4.  Part j of item i has slot i + j: both grow along the line,
-// one of them from piece to piece.
+// The parts' results, per part and head group: (max, sum) of the 128 rows of the wavefronts, and their weighted values in the order of the
+// accumulators: [wavefront][4 dimensions: 8 (i / 4) + half][32 rows] x 4.
 struct PieceLayout {
   size_t o, total;
 };
 __host__ __device__ inline PieceLayout piece_layout(int slots, int head_dim) {
   PieceLayout y;
-  y.o = (size_t)slots * 4 * kWaveRows * sizeof(float2);
-  y.total = y.o + (size_t)slots * 4 * kWaveRows * head_dim * sizeof(float);
+  y.o = (size_t)slots * kTileWaves * kWaveRows * sizeof(float2);
+  y.total = y.o + (size_t)slots * kTileWaves * kWaveRows * head_dim * sizeof(float);
   return y;
 }
 
@@ -157,7 +169,7 @@ __device__ __forceinline__ void attend_by_key(TileRows<D>& w, Stage<D, SRC>& sta
     stage.deposit(t, 0);
     stage.request(t, 1);
     stage.deposit(t, 1);
-    stage.arrive();
+    stage.template arrive<0>();
     barrier();
     const char* lk = stage.slot(t, 0);
     const char* lv = stage.slot(t, 1);
@@ -204,44 +216,35 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
   __shared__ __align__(16) TileLds<D> lds;
   __shared__ int lds_again;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int R = 4 * kWaveRows / heads, columns = a.n_heads / heads;  // rows of an item, workgroups of one item
+  const int R = kTileWaves * kWaveRows / heads, columns = a.n_heads / heads;  // rows of an item, workgroups of one item
   // consecutive workgroups go to the XCDs in turn: those that share keys and values come n_kv_heads apart, which puts them on
   // one XCD (8, 16, 40 ... key / value heads), whose L2 then fetches them once
-  const int hx = blockIdx.x % columns, part = blockIdx.x / columns, kvh = hx % a.n_kv_heads;
+  const int hx = blockIdx.x % columns, kvh = hx % a.n_kv_heads;
   const int head = kvh * (a.n_heads / a.n_kv_heads) + hx / a.n_kv_heads * heads + wave % heads;
 
-  // kept in LDS: across the loop below there are no registers for it
-  __shared__ Lanes lds_lanes[64];
-  int chunk = 0, all = 0;
-  if (a.n_seqs <= 64) {
-    const Lanes y = look<SRC>(a, R, columns, cut_slots > 0);
-    if (wave == 0) lds_lanes[lane] = y;
-    chunk = uniform(y.chunk);
-    all = uniform(y.all);
-  }
-  // the part of the line; not cut: one round for the one item
-  const int part_end = chunk ? (int)min((int64_t)(part + 1) * chunk, (int64_t)all) : 1;
-  for (int u = chunk ? (int)min((int64_t)part * chunk, (int64_t)all) : 0; u < part_end;) {
-  __syncthreads();                                                   // the last piece's reads of LDS are over
-  const Lanes y = lds_lanes[lane];
   Item it;
-  int from = 0, to = 1, whole = 1, item = 0;                         // units [from, to) of the item's `whole`
-  if (chunk) {
-    from = uniform(item_at(y, u, it, item));
-    item = uniform(item);
-    whole = uniform((max(it.before, 0) + R - 1) / R + it.tile + 1);
-    to = min(from + part_end - u, whole);
-  } else if (!uniform(item_number<SRC>(a, y, R, part, slots, it))) {
-    return;
+  int block = 0, blocks = 1, block_keys = 0;                         // of the item's keys
+  bool found;
+  {
+    Lanes y = {};
+    if (a.n_seqs <= 64) y = look<SRC>(a, R, columns, cut_slots > 0);
+    if (uniform(y.block)) {
+      found = part_number(y, blockIdx.x / columns, it, block);
+      block = uniform(block);
+      block_keys = uniform(y.block) * R;
+      blocks = uniform(found ? ((max(it.before, 0) + R - 1) / R + it.tile) / y.block + 1 : 1);
+    } else {
+      found = item_number<SRC>(a, y, R, blockIdx.x / columns, slots, it);
+    }
   }
-  u = uniform(u + to - from);
+  if (!uniform(found)) return;
   it.seq = uniform(it.seq); it.row0 = uniform(it.row0); it.rows = uniform(it.rows); it.tile = uniform(it.tile); it.before = uniform(it.before);
   const int row_first = it.tile * R;
 
   // keys [kTile first, kv_end) are seen by some row of the workgroup
   const int capacity = SRC == KV_PACKED ? 0x7fffffff : a.capacity;
-  const int first = uniform(from * R / kTile), piece_end = to < whole ? to * R / kTile * kTile : 0x7fffffff;
-  const int kv_end = uniform(min(min(it.before + min(row_first + R, it.rows), capacity), piece_end));
+  const int first = block * (block_keys / kTile), block_end = block + 1 < blocks ? (block + 1) * block_keys : 0x7fffffff;
+  const int kv_end = uniform(min(min(it.before + min(row_first + R, it.rows), capacity), block_end));
   const int n_all = kv_end > first * kTile ? (kv_end + kTile - 1) / kTile - first : 0;
   const int wave_row = row_first + wave / heads * kWaveRows;         // the wavefront's first row
   const int high = min(it.before + min(wave_row + kWaveRows, it.rows), kv_end);     // keys seen by its last row
@@ -293,12 +296,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
     if (uniform(lds_again)) attend_by_key<D, SRC>(w, stage, first, n_all, last, scale);
   }
 
-  if (to - from < whole) {
+  if (blocks > 1) {
     const PieceLayout y = piece_layout(cut_slots, D);
-    const int slot = (item + part) * columns + hx;
+    const int slot = blockIdx.x;
     char* ws = static_cast<char*>(a.ws);
-    float2* ml = reinterpret_cast<float2*>(ws) + (size_t)slot * 4 * kWaveRows + wave * kWaveRows;
-    f32x4* o = reinterpret_cast<f32x4*>(ws + y.o) + ((size_t)slot * 4 + wave) * kWaveRows * (D / 4);
+    float2* ml = reinterpret_cast<float2*>(ws) + ((size_t)slot * kTileWaves + wave) * kWaveRows;
+    f32x4* o = reinterpret_cast<f32x4*>(ws + y.o) + ((size_t)slot * kTileWaves + wave) * kWaveRows * (D / 4);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const float l = w.l[b] + other_half(w.l[b]);
@@ -309,7 +312,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
         for (int i = 0; i < 4; ++i)
           o[((dt * 4 + i) * 2 + half) * kWaveRows + 32 * b + col] = f32x4{w.acc[b][dt][4 * i], w.acc[b][dt][4 * i + 1], w.acc[b][dt][4 * i + 2], w.acc[b][dt][4 * i + 3]};
     }
-    continue;
+    return;
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
@@ -325,42 +328,43 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
         *reinterpret_cast<u32x2*>(dst + 32 * dt + 8 * i) =
             u32x2{pack2(w.acc[b][dt][4 * i] * inv, w.acc[b][dt][4 * i + 1] * inv), pack2(w.acc[b][dt][4 * i + 2] * inv, w.acc[b][dt][4 * i + 3] * inv)};
   }
-  }
 }
 
-// Adds up the pieces of the items that were cut.  A workgroup's job is 32 rows and 32 dimensions of an item, its wavefronts share out the
-// pieces; blockIdx.x is (item, heads), blockIdx.y takes every gridDim.y-th job of it.
+// Adds up the parts of the items that were cut.  A workgroup's job is 32 rows and 32 dimensions of an item, its wavefronts share out the
+// blocks; blockIdx.x is (item, heads), blockIdx.y takes every gridDim.y-th job of it.
+constexpr int kJoinThreads = 256;
 template <int D, int SRC>
-__global__ __launch_bounds__(kTileThreads) void k_join_prompt(PromptArgs a, int heads, int cut_slots) {
+__global__ __launch_bounds__(kJoinThreads) void k_join_prompt(PromptArgs a, int heads, int cut_slots) {
   constexpr int kQuads = 4;                                          // groups of 4 dimensions x 2 halves per job
   __shared__ f32x4 part[4][kQuads][64];
   __shared__ float2 part_ml[4][64];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int R = 4 * kWaveRows / heads, columns = a.n_heads / heads, hx = blockIdx.x % columns, kvh = hx % a.n_kv_heads;
+  const int R = kTileWaves * kWaveRows / heads, columns = a.n_heads / heads, hx = blockIdx.x % columns, kvh = hx % a.n_kv_heads;
   const int item = blockIdx.x / columns;
   const Lanes y = look<SRC>(a, R, columns, true);
-  const int chunk = uniform(y.chunk);
-  if (!chunk || item >= y.all_items) return;
-  const int s = __builtin_ctzll(__ballot(item >= y.items_before && item < y.items_before + y.tiles));
-  const int tile = uniform(item - __shfl(y.items_before, s)), base = uniform(__shfl(y.base, s));
-  const int u = uniform(__shfl(y.units_before, s)) + tile * base + tile * (tile + 1) / 2;
-  const int part0 = u / chunk, pieces = (u + base + tile) / chunk - part0 + 1;
-  if (pieces == 1) return;
-  const int row0 = uniform(__shfl(y.lo, s)) + tile * R, rows = min(R, uniform(__shfl(y.n, s)) - tile * R);
+  const int block = uniform(y.block);
+  if (!block || item >= y.all_items) return;
+  const int upto = wave_scan(y.tiles);                               // items up to and with the lane's
+  const int s = __builtin_ctzll(__ballot(upto > item));
+  const int tiles = __builtin_amdgcn_readlane(y.tiles, s), base = __builtin_amdgcn_readlane(y.base, s), tile = uniform(item - __builtin_amdgcn_readlane(upto, s) + tiles);
+  const int blocks = (base + tile) / block + 1;
+  if (blocks == 1) return;
+  const int ahead = __builtin_amdgcn_readlane(y.ahead, s), row0 = __builtin_amdgcn_readlane(y.lo, s) + tile * R, rows = min(R, __builtin_amdgcn_readlane(y.n, s) - tile * R);
   const char* ws = static_cast<const char*>(a.ws);
-  const size_t slot = (size_t)(item + part0) * columns + hx, step_ml = (size_t)columns * 4 * kWaveRows, step_o = step_ml * (D / 4);
-  for (int job = blockIdx.y; job < 4 * (D / 32); job += gridDim.y) {
-    const int part_wave = job % 4, q0 = job / 4 * kQuads, row = part_wave / heads * kWaveRows + col;
+  for (int job = blockIdx.y; job < kTileWaves * (D / 32); job += gridDim.y) {
+    const int part_wave = job % kTileWaves, q0 = job / kTileWaves * kQuads, row = part_wave / heads * kWaveRows + col;
     if (part_wave / heads * kWaveRows >= rows) continue;
-    const float2* ml = reinterpret_cast<const float2*>(ws) + (slot * 4 + part_wave) * kWaveRows + col;
-    const f32x4* o = reinterpret_cast<const f32x4*>(ws + piece_layout(cut_slots, D).o) + ((slot * 4 + part_wave) * (D / 4) + 2 * q0 + half) * kWaveRows + col;
+    const float2* ml = reinterpret_cast<const float2*>(ws) + part_wave * kWaveRows + col;
+    const f32x4* o = reinterpret_cast<const f32x4*>(ws + piece_layout(cut_slots, D).o) + (part_wave * (D / 4) + 2 * q0 + half) * kWaveRows + col;
     float m = -INFINITY, l = 0.0f;
     f32x4 x[kQuads] = {};
-    for (int p = wave; p < pieces; p += 4) {
-      const float2 v = ml[p * step_ml];
+    for (int p = wave; p < blocks; p += 4) {
+      const int number = ahead + parts_below(p, block, base, tiles) + tile - first_item(p, block, base);
+      const size_t slot = (size_t)number * columns + hx, step_ml = slot * kTileWaves * kWaveRows, step_o = step_ml * (D / 4);
+      const float2 v = ml[step_ml];
       f32x4 r[kQuads];
 #pragma unroll
-      for (int q = 0; q < kQuads; ++q) r[q] = o[p * step_o + q * 2 * kWaveRows];
+      for (int q = 0; q < kQuads; ++q) r[q] = o[step_o + q * 2 * kWaveRows];
       const float raised = fmaxf(m, v.x), to = raised == -INFINITY ? 0.0f : raised;
       const float old = exp2_fast(m - to), f = exp2_fast(v.x - to);
       m = raised;
@@ -395,8 +399,8 @@ __global__ __launch_bounds__(kTileThreads) void k_join_prompt(PromptArgs a, int 
 
 inline int heads_of(int group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
 // enough items for every way T rows can be shared out over the sequences
-inline int64_t slots_of(int T, int n_seqs, int heads) { return (int64_t)T / (4 * kWaveRows / heads) + n_seqs; }
-// slots of a call's pieces: see PieceLayout
+inline int64_t slots_of(int T, int n_seqs, int heads) { return (int64_t)T / (kTileWaves * kWaveRows / heads) + n_seqs; }
+// parts of a call: one per item, and one per block, which is longer than a share
 inline int cut_slots_of(int64_t workgroups) { return (int)std::min<int64_t>(workgroups, kMostCut) + kHeld; }
 
 // Whether look() could cut a call of packed prompts whose sequences take up all T rows: for some length of the longest, the others
@@ -406,7 +410,7 @@ bool packed_may_cut(int T, int n_seqs, int R, int columns) {
   for (double l = rows / n_seqs; l < 1.2 * rows; l *= 1.1) {
     const double longest = std::min(l + 1, rows + 1), rest = std::max(rows - longest, 0.0);
     const double work = 0.5 * (longest * longest + (n_seqs > 1 ? rest * rest / (n_seqs - 1) : 0.0));
-    if (2 * longest > 3 * std::max(work * columns / kHeld, (double)kLeastPart / R)) return true;
+    if (longest > 2.5 * work * columns / kHeld + 11 * kTile / R) return true;
   }
   return false;
 }
@@ -418,17 +422,17 @@ hipError_t launch(const PromptArgs& a, int source, hipStream_t s) {
   if (workgroups > 0x7fff0000) return hipErrorInvalidValue;
   // not cut: where no item can be much longer than the shortest part; with capacities at which the line would pass 31 bits
   const int longest = source == KV_PACKED ? a.T : a.capacity;
-  const bool cut = a.ws && a.n_seqs <= 64 && columns <= kHeld && longest > 3 * kLeastPart / 2 && longest <= 1 << 24 &&
-                   (source != KV_PACKED || packed_may_cut(a.T, a.n_seqs, 4 * kWaveRows / heads, columns));
+  const bool cut = a.ws && a.n_seqs <= 64 && columns <= kHeld && longest > 11 * kTile && longest <= 1 << 24 &&
+                   (source != KV_PACKED || packed_may_cut(a.T, a.n_seqs, kTileWaves * kWaveRows / heads, columns));
   const int cut_slots = cut ? cut_slots_of(workgroups) : 0;
-  const dim3 grid((unsigned)std::max<int64_t>(workgroups, cut ? kHeld / columns * columns : 0));
+  const dim3 grid((unsigned)std::max<int64_t>(workgroups, cut_slots / columns * columns));
   // joining workgroups: enough to fill the chip where there are few items
   const int64_t items = std::min<int64_t>(workgroups, kMostCut);
-  const dim3 join((unsigned)items, (unsigned)std::max<int64_t>(1, std::min<int64_t>(4 * (D / 32), 2048 / items)));
+  const dim3 join((unsigned)items, (unsigned)std::max<int64_t>(1, std::min<int64_t>(kTileWaves * (D / 32), 2048 / items)));
   auto go = [&](auto src) {
     constexpr int SRC = decltype(src)::value;
     k_attn_prompt<D, SRC><<<grid, kTileThreads, 0, s>>>(a, (int)slots, heads, cut_slots);
-    if (cut) k_join_prompt<D, SRC><<<join, kTileThreads, 0, s>>>(a, heads, cut_slots);
+    if (cut) k_join_prompt<D, SRC><<<join, kJoinThreads, 0, s>>>(a, heads, cut_slots);
   };
   if (source == KV_PACKED) go(std::integral_constant<int, KV_PACKED>{});
   else if (source == KV_PAGED) go(std::integral_constant<int, KV_PAGED>{});

@@ -26,7 +26,8 @@
 
 namespace mes {
 
-constexpr int kTile = 64, kRing = 2, kTileThreads = 256, NB = 1, kWaveRows = 32 * NB;
+constexpr int kTile = 64, kRing = 2, kTileWaves = 4, kTileThreads = 64 * kTileWaves, NB = 1, kWaveRows = 32 * NB;
+constexpr int kPart = kTile / kTileWaves;                             // keys of a tile that a wavefront brings
 
 constexpr int kBlock = 1024 + 16;                                     // bytes between blocks of rows
 
@@ -64,7 +65,7 @@ __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n
 // lane in order, so the turn is applied to the address that a lane fetches.  Key j of the tiles is token j of the sequence.
 template <int D, int SRC>
 struct Stage {
-  static constexpr int kPieces = Row<D>::kPieces, kRowsCopy = Row<D>::kPerBlock, kCopies = 16 / kRowsCopy;
+  static constexpr int kPieces = Row<D>::kPieces, kRowsCopy = Row<D>::kPerBlock, kCopies = kPart / kRowsCopy;
   const char *k, *v;              // packed: the sequence's row 0 of this head; paged: the cache's layer
   int ld_k, ld_v;                 // packed: elements between rows
   const int32_t* table;           // paged: the sequence's page table
@@ -74,7 +75,8 @@ struct Stage {
   int lane, wave;
   uint32_t offset[2];             // of a lane's 16 bytes from the first row of its copy
   int pages[4], batch;            // pages of the 16-token parts of tiles batch .. batch + 63, one tile per lane
-  u32x4 raw[2];                   // e4m3: codes on their way
+  static constexpr int kLanes = 64 / kPart, kWords = D / kLanes / 4;   // e4m3: lanes per key, words of codes of a lane
+  u32x4 raw[kWords / 4];          // e4m3: codes on their way
 
   __device__ Stage(TileLds<D>& l) : ld_k(D), ld_v(D), lds(l), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), batch(-64) {}
   __device__ __forceinline__ void begin(int tile) {
@@ -108,21 +110,22 @@ struct Stage {
   }
   // kv: 0 keys, 1 values
   __device__ __forceinline__ void request(int tile, int kv) {
-    const int token0 = tile * kTile + 16 * wave;
+    const int token0 = tile * kTile + kPart * wave;
     const char* base = kv ? v : k;
     const int step = (SRC == KV_PACKED ? (kv ? ld_v : ld_k) : D) * (SRC == KV_PAGED_E4M3 ? 1 : 2);   // bytes between rows
     bool real = true;
     if constexpr (SRC == KV_PACKED) {
       base += (int64_t)token0 * step;
     } else {
-      int page = wave == 0 ? page_of(tile, 0) : wave == 1 ? page_of(tile, 1) : wave == 2 ? page_of(tile, 2) : page_of(tile, 3);
+      const int part = wave * kPart / 16;
+      int page = part == 0 ? page_of(tile, 0) : part == 1 ? page_of(tile, 1) : part == 2 ? page_of(tile, 2) : page_of(tile, 3);
       real = (unsigned)page < (unsigned)n_pages;
       if (!real) page = 0;
       base += ((((int64_t)page * n_kv_heads + kvh) << page_shift) + (token0 & ((1 << page_shift) - 1))) * step;
     }
     if constexpr (SRC != KV_PAGED_E4M3) {
-      const uint32_t at = (uint32_t)(uintptr_t)slot(tile, kv) + Row<D>::at(16 * wave);
-      if (real && token0 + 16 <= to) {
+      const uint32_t at = (uint32_t)(uintptr_t)slot(tile, kv) + Row<D>::at(kPart * wave);
+      if (real && token0 + kPart <= to) {
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) copy_to_lds(base + (int64_t)i * kRowsCopy * step, offset[kv], at + i * kBlock);
       } else {
@@ -133,22 +136,24 @@ struct Stage {
         }
       }
     } else {
-      const int r = lane >> 2, part = lane & 3;                      // four lanes per key, D / 4 codes each
-      const char* from = base + (uint32_t)(r * D + part * (D / 4));
+      const int r = lane / kLanes;
+      const char* from = base + (uint32_t)(r * D + lane % kLanes * (D / kLanes));
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) raw[i] = real && token0 + r < to ? *reinterpret_cast<const u32x4*>(from + 16 * i) : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < kWords / 4; ++i) raw[i] = real && token0 + r < to ? *reinterpret_cast<const u32x4*>(from + 16 * i) : u32x4{0, 0, 0, 0};
     }
   }
-  __device__ __forceinline__ void arrive() {                         // this wavefront's copies
-    if constexpr (SRC != KV_PAGED_E4M3) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // all of this wavefront's copies but the last `younger`
+  template <int younger>
+  __device__ __forceinline__ void arrive() {
+    if constexpr (SRC != KV_PAGED_E4M3) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(younger) : "memory");
   }
   __device__ __forceinline__ void deposit(int tile, int kv) {        // e4m3: codes -> bf16 rows in LDS
     if constexpr (SRC == KV_PAGED_E4M3) {
-      const int r = 16 * wave + (lane >> 2), part = lane & 3;
+      const int r = kPart * wave + lane / kLanes, piece = lane % kLanes * (kWords / 2);
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
+      for (int i = 0; i < kWords / 2; ++i) {
         const u32x2 x = widen4(raw[i / 2][2 * (i % 2)]), y = widen4(raw[i / 2][2 * (i % 2) + 1]);
-        *reinterpret_cast<u32x4*>(slot(tile, kv) + Row<D>::at(r) + (((part * (D / 32) + i) ^ Row<D>::turn(r)) * 16)) = u32x4{x[0], x[1], y[0], y[1]};
+        *reinterpret_cast<u32x4*>(slot(tile, kv) + Row<D>::at(r) + (((piece + i) ^ Row<D>::turn(r)) * 16)) = u32x4{x[0], x[1], y[0], y[1]};
       }
     }
   }
@@ -208,17 +213,28 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
   for (int i = 0; i < 4; ++i) k_at[i] = R::at(col) + (((2 * kTogether * i + half) ^ R::turn(col)) * 16);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) v_at[dt] = R::at(v_r) + (((4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ R::turn(v_r)) * 16) + 8 * (lane & 1);
-  auto k_operand = [&](int slot, int g) {                           // group g: dimensions 16 (g / 2) .., keys 32 (g % 2) ..
+  auto k_operand = [&](int g) {                                     // group g: dimensions 16 (g / 2) .., keys 32 (g % 2) ..
     const int ks = g / 2;
-    return *(lds_b128)(base + k_at[ks / kTogether] + (slot * kTileBytes + R::at(32 * (g % 2)) + ks % kTogether * 32));
+    return *(lds_b128)(base + k_at[ks / kTogether] + (R::at(32 * (g % 2)) + ks % kTogether * 32));
   };
-  auto v_operand = [&](int slot, int g) {                           // group g: keys 16 (g / DT) .., dimensions 32 (g % DT) ..
+  auto v_operand = [&](int g) {                                     // group g: keys 16 (g / DT) .., dimensions 32 (g % DT) ..
     // lanes of 16 read 4 keys x 16 dimensions, 8 bytes each, and get a dimension's 4 keys
-    const int at = (kRing + slot) * kTileBytes + R::at(16 * (g / DT));
+    const int at = kRing * kTileBytes + R::at(16 * (g / DT));
     struct { i16x4 lo, hi; } v;
     v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(base + v_at[g % DT] + at));
     v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr)(base + v_at[g % DT] + at + R::at(8)));
     return __builtin_bit_cast(bf16x8, v);
+  };
+  // the addresses move on to the next tile of the ring
+  auto next_k = [&](int tile) {
+    const uint32_t by = (tile - first) % kRing == 0 ? (uint32_t)(-(kRing - 1) * kTileBytes) : (uint32_t)kTileBytes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k_at[i] += by;
+  };
+  auto next_v = [&](int tile) {
+    const uint32_t by = (tile - first) % kRing == 0 ? (uint32_t)(-(kRing - 1) * kTileBytes) : (uint32_t)kTileBytes;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) v_at[dt] += by;
   };
 
   f32x16 s0[NB][2], s1[NB][2];                                        // scores [block][32 keys] of two tiles in turn
@@ -247,44 +263,47 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
   };
   auto partial = [&](int tile, int there) { return tile * kTile + kTile - 1 > low || tile * kTile + kTile > stage.to || there != 15; };
 
-  // ---- keys run one tile ahead of the values: at tile t keys t + 1 and values t are needed, keys t + 2 and values t + 1 asked for; codes of
-  // an 8-bit cache pass through registers, keys during the first half of a tile's work, values during the second
+  // ---- keys run one tile ahead of the values: at tile t keys t + 1 and values t are needed, keys t + 2 and values t + 1 asked for (a ring of
+  // three tiles and 8 wavefronts, which ask for them a tile earlier, measured the same).  Codes of an 8-bit cache pass through registers:
+  // keys t + 2 during the first half of the work on tile t, values t + 1 during the second.
   const int end_all = first + n_all, end = first + n;
+  constexpr bool kDirect = SRC != KV_PAGED_E4M3;
   auto before = [&](int t) {
-    stage.arrive();
-    barrier();                                                       // also at the first tile: its keys have been read, and make room
+    stage.template arrive<0>();
+    barrier();                                                       // nobody reads keys t and values t - 1 any more
     if (t + 2 < end_all) {
       stage.look_up(t + 2);
       stage.request(t + 2, 0);
     }
-    if (SRC != KV_PAGED_E4M3 && t + 1 < end_all) stage.request(t + 1, 1);
+    if (kDirect && t + 1 < end_all) stage.request(t + 1, 1);
   };
   auto between = [&](int t) {
     if (t + 2 < end_all) stage.deposit(t + 2, 0);
-    if (SRC == KV_PAGED_E4M3 && t + 1 < end_all) stage.request(t + 1, 1);
+    if (!kDirect && t + 1 < end_all) stage.request(t + 1, 1);
   };
   auto after = [&](int t) {
     if (t + 1 < end_all) stage.deposit(t + 1, 1);
   };
 
   // Tile t, whose scores are in s; the scores of tile t + 1 go to sn, unless this wavefront does not take it (next = 0).
-  auto step = [&](auto next, auto slot, f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
+  auto step = [&](auto next, f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
     constexpr bool kNext = decltype(next)::value;
-    constexpr int lv = decltype(slot)::value, lk = (lv + 1) % kRing;  // where the values of tile t and the keys of t + 1 are
+    if (kNext) next_k(t + 1);
+    if (t > first) next_v(t);
     u32x4 p[NB][4];
     constexpr int kAhead = 3;                                       // operands on their way
     bf16x8 ring[kAhead + 1];
     if constexpr (kNext) {
 #pragma unroll
-      for (int g = 0; g < kAhead; ++g) ring[g] = k_operand(lk, g);
+      for (int g = 0; g < kAhead; ++g) ring[g] = k_operand(g);
     } else {
 #pragma unroll
-      for (int g = 0; g < kAhead; ++g) ring[g] = v_operand(lv, g);
+      for (int g = 0; g < kAhead; ++g) ring[g] = v_operand(g);
     }
 #pragma unroll
     for (int g = 0; g < kGroups1; ++g) {
       if constexpr (kNext) {
-        ring[(g + kAhead) % (kAhead + 1)] = g + kAhead < kGroups1 ? k_operand(lk, g + kAhead) : v_operand(lv, g + kAhead - kGroups1);
+        ring[(g + kAhead) % (kAhead + 1)] = g + kAhead < kGroups1 ? k_operand(g + kAhead) : v_operand(g + kAhead - kGroups1);
         const f32x16 zero = {};
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -314,7 +333,7 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
     constexpr int kFirst = kNext ? kGroups1 : 0;                    // place of group 0's operand in the ring
 #pragma unroll
     for (int g = 0; g < kGroups2; ++g) {
-      if (g + kAhead < kGroups2) ring[(kFirst + g + kAhead) % (kAhead + 1)] = v_operand(lv, g + kAhead);
+      if (g + kAhead < kGroups2) ring[(kFirst + g + kAhead) % (kAhead + 1)] = v_operand(g + kAhead);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
         w.acc[b][g % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(kFirst + g) % (kAhead + 1)], __builtin_bit_cast(bf16x8, p[b][g / DT]), w.acc[b][g % DT], 0, 0, 0);
@@ -341,13 +360,14 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
     stage.request(first + 1, 0);
     stage.deposit(first + 1, 0);
   }
-  stage.arrive();
+  // the first keys are there
+  if (kDirect && n_all > 1) stage.template arrive<2 * Stage<D, SRC>::kCopies>(); else stage.template arrive<0>();
   barrier();
   if (n > 0) {
     const f32x16 zero = {};
 #pragma unroll
     for (int g = 0; g < kGroups1; ++g) {
-      const bf16x8 k = k_operand(0, g);
+      const bf16x8 k = k_operand(g);
 #pragma unroll
       for (int b = 0; b < NB; ++b) s0[b][g % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, w.q[b][g / 2], g < 2 ? zero : s0[b][g % 2], 0, 0, 0);
     }
@@ -364,26 +384,24 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
         for (int i = 0; i < 16; ++i) top[b] = fmaxf(top[b], s0[b][tt][i]);
     raise(top);
   }
-  auto turn = [&](auto next, auto slot, f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
+  auto turn = [&](auto next, f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
     before(t);
-    step(next, slot, s, sn, t);
+    step(next, s, sn, t);
     after(t);
   };
-  constexpr std::integral_constant<int, 0> even;
-  constexpr std::integral_constant<int, 1> odd;
   constexpr std::true_type more;
   constexpr std::false_type none;
   int t = first;
   if (n > 0) {
     for (; t + 2 < end; t += 2) {                                    // one way out of the loop: with two, the compiler keeps two sets of accumulators
-      turn(more, even, s0, s1, t);
-      turn(more, odd, s1, s0, t + 1);
+      turn(more, s0, s1, t);
+      turn(more, s1, s0, t + 1);
     }
     if (t + 1 < end) {
-      turn(more, even, s0, s1, t++);
-      turn(none, odd, s1, s0, t++);
+      turn(more, s0, s1, t++);
+      turn(none, s1, s0, t++);
     } else {
-      turn(none, even, s0, s1, t++);
+      turn(none, s0, s1, t++);
     }
   }
   for (; t < end_all; ++t) {                                         // other wavefronts' tiles

@@ -99,7 +99,7 @@ def test_prompt_and_extend_errors():
         assert need > 0 and call(ws=FAKE, wsb=need - 1) == 7 and call(ws=ODD, wsb=need) == 6       # NULL is fine: no item is cut
     for bad in ((-1, 1, 4, 2, 64), (5, -1, 4, 2, 64), (5, 4097, 4, 2, 64), (5, 1, 5, 2, 64), (5, 1, 4, 2, 32)):
         assert lib.mes_attn_prompt_workspace_bytes(*bad) == 0
-    assert lib.mes_attn_prompt_workspace_bytes(1 << 20, 64, 32, 8, 128) < 128 << 20
+    assert lib.mes_attn_prompt_workspace_bytes(1 << 20, 64, 32, 8, 128) == (1024 + 512) * 128 * (8 + 128 * 4)
     assert _prompt(k=None) == 1 and _prompt(v=ODD) == 6 and _prompt(ld_k=64) == 2 and _prompt(ld_v=129) == 2
     assert _prompt(off=None) == 1 and _prompt(n=-1) == 2 and _prompt(n=4097) == 2 and _prompt(n=0) == 0
     assert _prompt(dim=80) == 2 and _prompt(kvh=0) == 2
