@@ -322,7 +322,7 @@ mes_status mes_step_adamw(float* step, const float* grad, float* m, float* v, in
  * aligned.  MES_KV_BF16: bf16.  MES_KV_E4M3: 8-bit floating point (4 exponent, 3 mantissa bits, largest value 448), value =
  * code * scale with one fp32 scale per layer and head, k_scale and v_scale [n_layers][n_kv_heads] (NULL for bf16). */
 enum { MES_KV_BF16 = 0, MES_KV_E4M3 = 1 };
-#define MES_MAX_SEQS 4096
+#define MES_MAX_SEQS 2048
 typedef struct {           /* HOST struct; pointers DEVICE, caller-owned */
   int32_t n_layers, n_pages, page_tokens, n_kv_heads, head_dim, dtype;
   void* k;

@@ -22,7 +22,7 @@ STEP_GIVEN, STEP_MAXABS, STEP_MEANABS = 0, 1, 2
 MAX_EXPERTS = 64
 
 KV_BF16, KV_E4M3 = 0, 1
-MAX_SEQS = 4096
+MAX_SEQS = 2048
 SHORT_PROMPT = 704          # keys: rows that see no more are never shared out, and need no workspace
 
 STATUS_NAMES = {0: "MES_OK", 1: "MES_ERR_NULL", 2: "MES_ERR_SHAPE", 3: "MES_ERR_BITS", 4: "MES_ERR_SALIENT",

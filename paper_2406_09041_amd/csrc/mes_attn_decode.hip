@@ -8,19 +8,22 @@
 // piece of the line that does not cover a sequence alone leaves (max, sum, weighted values) in the workspace, and k_join
 // adds the pieces of a row in their order.
 //
-// A wavefront takes 32 tokens at a time with all query rows of the unit (up to 4 tiles of 16).  Scores are formed transposed,
-// S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K's operand is 16 tokens x 8 dimensions per lane straight from memory, and the
-// result holds one query row (lane & 15) and tokens 4 g + (0..3) per lane (g = lane / 16), which rounded to bf16 IS the operand P^T of
-// O^T = V^T P^T over the 32 tokens in the order (4 g + i, 16 + 4 g + i).  V is read by rows, 16 lanes a row, lane r the
-// dimensions VD r .. VD r + VD - 1 of its 8 tokens: product j of VD then yields the dimensions VD m + j, and its operand is pairs of
-// 16-bit halves put together, one v_perm each.  So neither keys nor values pass through LDS.  Of the 16 columns of a tile 4
-// (n_heads / n_kv_heads) are used where nothing is shared: the matrix cores are idle most of the time anyway.
-#include "mes_attn_common.h"
+// Up to 16 query rows (one sequence of a group of up to 16 heads, or few sequences' shared prefix): a wavefront takes 32 tokens at a
+// time.  Scores are formed transposed, S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K's operand is 16 tokens x 8 dimensions per lane
+// straight from memory, and the result holds one query row (lane & 15) and tokens 4 g + (0..3) per lane (g = lane / 16), which rounded
+// to bf16 IS the operand P^T of O^T = V^T P^T over the 32 tokens in the order (4 g + i, 16 + 4 g + i).  V is read by rows, 16 lanes a
+// row, lane r the dimensions VD r .. VD r + VD - 1 of its 8 tokens: product j of VD then yields the dimensions VD m + j, and its operand
+// is pairs of 16-bit halves put together, one v_perm each.  So neither keys nor values pass through LDS.  Of the 16 columns of a
+// tile 4 (n_heads / n_kv_heads) are used where nothing is shared: the matrix cores are idle most of the time anyway.
+//
+// More rows: up to 128 of them share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from about 100 rows on.
+#include "mes_attn_tiles.h"
 
 namespace mes {
 namespace {
 
-constexpr int kThreads = 256, kUnit = 128, kRowsPass = 64, kWorkgroups = 512;
+constexpr int kThreads = 256, kUnit = 128, kRowsPass = 128, kFewRows = 16, kWorkgroups = 512;
+static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
 
 struct Shape {                       // what host and device derive alike
   int group, per_pass, n_passes;     // query heads per key / value head, sequences per pass, passes of all groups
@@ -74,52 +77,45 @@ __device__ __forceinline__ int dim_of(int c, int g) {
 
 struct Segment {                                    // a piece of the line
   int seq, seq0, rows;                              // page table; sequence of row 0; query rows
-  int from, to, t0, t1;                             // tokens of [from, to) in the steps [t0, t1), t0 a multiple of 32
+  int from, to, t0, t1;                             // tokens of [from, to) in the units [t0, t1), t0 a multiple of 64
 };
 
-template <int D, bool FP8>
+template <int D>
 struct Shared {
-  float merge[4][16][D + 4];
-  u32x4 q[4][D / 32][64];
-  float2 ml[4][kRowsPass];
+  union {
+    TileLds<D> tiles;
+    struct {
+      float merge[4][kFewRows][D + 4];
+      float2 ml[4][kFewRows];
+    };
+  };
   int cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
   int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: fewer than two are
   int part[4];
 };
 
-// The weighted sum over one piece, all query rows, into o / ml (or out where the piece is all that its rows see).
-template <int D, bool FP8, int NT>
-__device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D, FP8>& sh, bool direct, float* o, float2* ml_out) {
+// The weighted sum over one piece, up to 16 query rows, into o / ml_out (or out where the piece is all that its rows see).
+template <int D, bool FP8>
+__device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D>& sh, bool direct, float* o, float2* ml_out) {
   constexpr int VD = D / 16, KS = D / 32;
   typedef Raw<D, FP8> R;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
 
-  // Q^T operands: one tile in registers, more in LDS
-  u32x4 q1[KS];
-  __syncthreads();                                  // the last piece's reads of LDS are over
-  for (int nt = NT == 1 ? 0 : wave; nt < NT; nt += NT == 1 ? 1 : 4) {
-    const int row = 16 * nt + col;
+  u32x4 q[KS];
 #pragma unroll
-    for (int c = 0; c < KS; ++c) {
-      u32x4 w = {0, 0, 0, 0};
-      if (row < g.rows)
-        w = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + row / group) * a.ld_q + (size_t)(kvh * group + row % group) * D + dim_of<D, FP8>(c, quad));
-      if constexpr (NT == 1) q1[c] = w; else sh.q[nt][c][lane] = w;
-    }
+  for (int c = 0; c < KS; ++c) {
+    q[c] = u32x4{0, 0, 0, 0};
+    if (col < g.rows)
+      q[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(kvh * group + col % group) * D + dim_of<D, FP8>(c, quad));
   }
-  if constexpr (NT > 1) __syncthreads();
+  __syncthreads();                                  // the last piece's reads of LDS are over
 
   const float scale = a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f);
   const int32_t* table = a.page_table + (size_t)g.seq * a.table_pages;
-  f32x4 acc[NT][VD];
-  float m[NT], l[NT];
+  f32x4 acc[VD];
+  float m = -INFINITY, l = 0.0f;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m[nt] = -INFINITY;
-    l[nt] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < VD; ++j) acc[nt][j] = f32x4{0, 0, 0, 0};
-  }
+  for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
 
   // the pages of this wavefront's next 64 steps, one step per lane
   const int n_steps = (g.t1 - g.t0 + 31) / 32, mine = (n_steps - wave + 3) / 4;   // steps wave, wave + 4, ...
@@ -180,14 +176,11 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
       const int tok = t + 16 * h + 4 * quad + e;
       return (h ? ok1 : ok0) && tok >= g.from && tok < g.to;
     };
-    u32x4 p[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    u32x4 p;
+    {
       f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
       for (int c = 0; c < KS; ++c) {
-        u32x4 qc;
-        if constexpr (NT == 1) qc = q1[c]; else qc = sh.q[nt][c][lane];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           u32x4 kc;
@@ -195,7 +188,7 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
             const u32x2 x = widen4(raw.k[h][c / 2][2 * (c % 2)]), y = widen4(raw.k[h][c / 2][2 * (c % 2) + 1]);
             kc = u32x4{x[0], x[1], y[0], y[1]};
           } else kc = raw.k[h][c];
-          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc), __builtin_bit_cast(bf16x8, qc), s[h], 0, 0, 0);
+          s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc), __builtin_bit_cast(bf16x8, q[c]), s[h], 0, 0, 0);
         }
       }
       if (!whole) {
@@ -206,21 +199,21 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
             if (!seen(h, e)) s[h][e] = -INFINITY;
       }
       float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * scale;
-      if (__any(top > m[nt] + kSlack)) {
+      if (__any(top > m + kSlack)) {
         top = fmaxf(top, other_row16(top));
         top = fmaxf(top, other_half(top));
-        const float raised = fmaxf(m[nt], top);
-        const float shrink = exp2_fast(m[nt] - (raised == -INFINITY ? 0.0f : raised));
-        l[nt] *= shrink;
+        const float raised = fmaxf(m, top);
+        const float shrink = exp2_fast(m - (raised == -INFINITY ? 0.0f : raised));
+        l *= shrink;
 #pragma unroll
-        for (int j = 0; j < VD; ++j) acc[nt][j] *= shrink;
-        m[nt] = raised;
+        for (int j = 0; j < VD; ++j) acc[j] *= shrink;
+        m = raised;
       }
-      const float from = m[nt] == -INFINITY ? 0.0f : m[nt];
+      const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        p[nt][x] = pack2(exp2_fast(s[x / 2][2 * (x % 2)] * scale - from), exp2_fast(s[x / 2][2 * (x % 2) + 1] * scale - from));
-        l[nt] = add_pair(p[nt][x], l[nt]);          // the sum of what is multiplied with V
+        p[x] = pack2(exp2_fast(s[x / 2][2 * (x % 2)] * scale - from), exp2_fast(s[x / 2][2 * (x % 2) + 1] * scale - from));
+        l = add_pair(p[x], l);          // the sum of what is multiplied with V
       }
     }
     int next[2] = {-1, -1};
@@ -249,9 +242,7 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
         u32x4 v;
 #pragma unroll
         for (int x = 0; x < 4; ++x) v[x] = __builtin_amdgcn_perm(pair[2 * x + 1], pair[2 * x], odd ? 0x07060302u : 0x05040100u);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          acc[nt][2 * jw + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p[nt]), acc[nt][2 * jw + odd], 0, 0, 0);
+        acc[2 * jw + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[2 * jw + odd], 0, 0, 0);
       }
     }
     if (more) request_v(i + 1, next);
@@ -260,28 +251,24 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
   }
 
   // ---- the four wavefronts' results on one maximum, added in their order
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    l[nt] += other_row16(l[nt]);
-    l[nt] += other_half(l[nt]);
-    if (lane < 16) sh.ml[wave][16 * nt + lane] = make_float2(m[nt], l[nt]);
-  }
+  l += other_row16(l);
+  l += other_half(l);
+  if (lane < 16) sh.ml[wave][lane] = make_float2(m, l);
   __syncthreads();
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  {
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, sh.ml[w][16 * nt + col].x);
-    const float shrink = exp2_fast(m[nt] - (top == -INFINITY ? 0.0f : top));
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, sh.ml[w][col].x);
+    const float shrink = exp2_fast(m - (top == -INFINITY ? 0.0f : top));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float* to = &sh.merge[wave][col][VD * (4 * quad + i)];
 #pragma unroll
       for (int j = 0; j < VD; j += 4)
-        *reinterpret_cast<f32x4*>(to + j) = f32x4{acc[nt][j][i], acc[nt][j + 1][i], acc[nt][j + 2][i], acc[nt][j + 3][i]} * shrink;
+        *reinterpret_cast<f32x4*>(to + j) = f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]} * shrink;
     }
     __syncthreads();
-    const int r = threadIdx.x >> 4, row = 16 * nt + r, d0 = (threadIdx.x & 15) * VD;
+    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VD;
     if (row < g.rows) {
       float lr = 0.0f, mr = -INFINITY, x[VD];
 #pragma unroll
@@ -289,7 +276,7 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
 #pragma unroll
       for (int w = 0; w < 4; ++w) lr += sh.ml[w][row].y * exp2_fast(sh.ml[w][row].x - (mr == -INFINITY ? 0.0f : mr));
 #pragma unroll
-      for (int j = 0; j < VD; ++j) x[j] = sh.merge[0][r][d0 + j] + sh.merge[1][r][d0 + j] + sh.merge[2][r][d0 + j] + sh.merge[3][r][d0 + j];
+      for (int j = 0; j < VD; ++j) x[j] = sh.merge[0][row][d0 + j] + sh.merge[1][row][d0 + j] + sh.merge[2][row][d0 + j] + sh.merge[3][row][d0 + j];
       if (direct) {
         const float inv = lr == 0.0f ? 0.0f : (FP8 ? a.v_scale[kvh] : 1.0f) / lr;
         uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(kvh * group + row % group) * D + d0;
@@ -302,25 +289,64 @@ __device__ void run_segment(const DecodeArgs& a, int group, int kvh, const Segme
         if (d0 == 0) ml_out[row] = make_float2(mr, lr);
       }
     }
-    __syncthreads();
+  }
+}
+
+// The same for up to 128 rows: 32 per wavefront.
+template <int D, bool FP8>
+__device__ __forceinline__ void run_many(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D>& sh, bool direct, float* o, float2* ml_out) {
+  constexpr int KS = D / 16, DT = D / 32, SRC = FP8 ? KV_PAGED_E4M3 : KV_PAGED;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, row = kWaveRows * wave + (lane & 31);
+  Stage<D, SRC> stage(sh.tiles);
+  stage.k = static_cast<const char*>(a.k);
+  stage.v = static_cast<const char*>(a.v);
+  stage.kvh = kvh;
+  stage.from = g.from;
+  stage.to = g.to;
+  stage.table = a.page_table + (size_t)g.seq * a.table_pages;
+  stage.page_shift = a.page_shift;
+  stage.n_pages = a.n_pages;
+  stage.n_kv_heads = a.n_kv_heads;
+  TileRows<D> w;
+  const int there = min(row, g.rows - 1);
+  const uint16_t* src = a.q + (size_t)(g.seq0 + there / group) * a.ld_q + (size_t)(kvh * group + there % group) * D + 8 * half;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) w.q[0][ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
+  w.m[0] = -INFINITY;
+  w.l[0] = 0.0f;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) w.acc[0][dt] = f32x16{};
+  const int last[NB] = {0x7fffffff}, first = g.t0 / kTile, n = (g.t1 - g.t0 + kTile - 1) / kTile;
+  __syncthreads();                                  // the last piece's reads of LDS are over
+  attend_tiles<D, SRC>(w, stage, first, kWaveRows * wave < g.rows ? n : 0, n, 0x7fffffff, last, a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f));
+  const float l = w.l[0] + other_half(w.l[0]);
+  if (row >= g.rows) return;
+  if (direct) {
+    const float inv = l == 0.0f ? 0.0f : (FP8 ? a.v_scale[kvh] : 1.0f) / l;
+    uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(kvh * group + row % group) * D + 4 * half;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<u32x2*>(dst + 32 * dt + 8 * i) = u32x2{pack2(w.acc[0][dt][4 * i] * inv, w.acc[0][dt][4 * i + 1] * inv), pack2(w.acc[0][dt][4 * i + 2] * inv, w.acc[0][dt][4 * i + 3] * inv)};
+  } else {
+    if (half == 0) ml_out[row] = make_float2(w.m[0], l);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(o + (size_t)row * D + 32 * dt + 8 * i + 4 * half) = f32x4{w.acc[0][dt][4 * i], w.acc[0][dt][4 * i + 1], w.acc[0][dt][4 * i + 2], w.acc[0][dt][4 * i + 3]};
   }
 }
 
 template <int D, bool FP8>
-__device__ void run_tiles(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D, FP8>& sh, bool direct, float* o, float2* ml) {
-  if (g.rows <= 16) run_segment<D, FP8, 1>(a, group, kvh, g, sh, direct, o, ml);
-  else if (g.rows <= 32) run_segment<D, FP8, 2>(a, group, kvh, g, sh, direct, o, ml);
-  else run_segment<D, FP8, 4>(a, group, kvh, g, sh, direct, o, ml);
-}
-
-template <int D, bool FP8>
 __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
-  __shared__ Shared<D, FP8> sh;
+  __shared__ __align__(16) Shared<D> sh;
   const DecodeArgs& a = c.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int n_items = a.n_groups + a.n_seqs;
   auto length = [&](int s) { return min(max(a.kv_len[s], 0), a.capacity); };
-  auto units = [](int from, int to) { return to > from ? (to - (from & ~31) + kUnit - 1) / kUnit : 0; };
+  auto units = [](int from, int to) { return to > from ? (to - (from & ~63) + kUnit - 1) / kUnit : 0; };
 
   // ---- units of every item, groups first
   for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[a.n_groups + s] = units(0, length(s));
@@ -348,12 +374,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     const int per = (n_items + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * per, n_items), hi = min(lo + per, n_items);
     int sum = 0;
     for (int i = lo; i < hi; ++i) sum += sh.cum[i];
-    int run = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int up = __shfl_up(run, o);
-      if (lane >= o) run += up;
-    }
+    const int run = wave_scan(sum);
     if (lane == 63) sh.part[wave] = run;
     __syncthreads();
     int at = run - sum;
@@ -408,6 +429,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     const int it = uniform(lo), first = uniform(sh.cum[it]), n = uniform(sh.cum[it + 1]) - first;
     int from_unit = in_head - first, to_unit = min(from_unit + end - u, n);
     Segment g;
+    float* o;
+    float2* ml;
+    bool direct = false;
     if (it < a.n_groups) {
       const int tiles = (a.prefix[it] + kUnit - 1) / kUnit, pass = from_unit / tiles;
       from_unit -= pass * tiles;
@@ -420,24 +444,29 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       g.t0 = from_unit * kUnit;
       g.t1 = min(to_unit * kUnit, g.to);
       const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
-      run_tiles<D, FP8>(a, c.sh.group, h, g, sh, false, reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D,
-                        reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass);
+      o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
+      ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
     } else {
       const int s = it - a.n_groups;
       g.seq = g.seq0 = s;
       g.rows = c.sh.group;
+      g.to = uniform(length(s));
       g.from = 0;
       for (int k = 0; k < a.n_groups; ++k)
-        if (s >= a.first[k] && s < a.behind[k] && sh.group_src[k] >= 0 && length(s) >= a.prefix[k]) g.from = a.prefix[k];
+        if (s >= a.first[k] && s < a.behind[k] && sh.group_src[k] >= 0 && g.to >= a.prefix[k]) g.from = a.prefix[k];
       g.from = uniform(g.from);
-      g.to = uniform(length(s));
-      g.t0 = (g.from & ~31) + from_unit * kUnit;
-      g.t1 = min((g.from & ~31) + to_unit * kUnit, g.to);
+      g.t0 = (g.from & ~63) + from_unit * kUnit;
+      g.t1 = min((g.from & ~63) + to_unit * kUnit, g.to);
       const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
-      const bool direct = g.from == 0 && from_unit == 0 && to_unit == n;
-      if (c.sh.group <= 16) run_segment<D, FP8, 1>(a, c.sh.group, h, g, sh, direct, reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D, reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group);
-      else run_tiles<D, FP8>(a, c.sh.group, h, g, sh, direct, reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D, reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group);
+      direct = g.from == 0 && from_unit == 0 && to_unit == n;
+      o = reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D;
+      ml = reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group;
     }
+    g.t0 = uniform(g.t0);
+    g.t1 = uniform(g.t1);
+    g.rows = uniform(g.rows);
+    if (g.rows <= kFewRows) run_few<D, FP8>(a, c.sh.group, h, g, sh, direct, o, ml);
+    else run_many<D, FP8>(a, c.sh.group, h, g, sh, direct, o, ml);
     u += to_unit - from_unit;
   }
 }

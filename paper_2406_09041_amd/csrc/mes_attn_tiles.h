@@ -70,7 +70,7 @@ struct Stage {
   int ld_k, ld_v;                 // packed: elements between rows
   const int32_t* table;           // paged: the sequence's page table
   int page_shift, n_pages, n_kv_heads, kvh;
-  int first, to;                  // the first tile; tokens [0, to) are there
+  int first, from, to;            // the first tile; tokens [from, to) are seen
   TileLds<D>& lds;
   int lane, wave;
   uint32_t offset[2];             // of a lane's 16 bytes from the first row of its copy
@@ -78,7 +78,7 @@ struct Stage {
   static constexpr int kLanes = 64 / kPart, kWords = D / kLanes / 4;   // e4m3: lanes per key, words of codes of a lane
   u32x4 raw[kWords / 4];          // e4m3: codes on their way
 
-  __device__ Stage(TileLds<D>& l) : ld_k(D), ld_v(D), lds(l), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), batch(-64) {}
+  __device__ Stage(TileLds<D>& l) : ld_k(D), ld_v(D), from(0), lds(l), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), batch(-64) {}
   __device__ __forceinline__ void begin(int tile) {
     first = tile;
     const int r = lane / kPieces;
@@ -168,7 +168,7 @@ struct TileRows {
 };
 
 // One tile's scores -> -inf where the row does not see the key.  `last[b]`: the last key that the lane's row of block b sees.
-__device__ __forceinline__ void mask_scores(f32x16 (&s)[NB][2], int key0, const int (&last)[NB], int to, int there) {
+__device__ __forceinline__ void mask_scores(f32x16 (&s)[NB][2], int key0, const int (&last)[NB], int from, int to, int there) {
   const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
@@ -178,6 +178,15 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[NB][2], int key0, const 
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (32 * tt + 8 * (i / 4) + i % 4 > limit) s[b][tt][i] = -INFINITY;
+  }
+  if (key0 < from) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * tt + 8 * (i / 4) + i % 4 < from - key0 - 4 * half) s[b][tt][i] = -INFINITY;
   }
   if (there == 15) return;
 #pragma unroll
@@ -261,7 +270,7 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
 #pragma unroll
     for (int b = 0; b < NB; ++b) from[b] = w.m[b] == -INFINITY ? 0.0f : w.m[b];
   };
-  auto partial = [&](int tile, int there) { return tile * kTile + kTile - 1 > low || tile * kTile + kTile > stage.to || there != 15; };
+  auto partial = [&](int tile, int there) { return tile * kTile + kTile - 1 > low || tile * kTile + kTile > stage.to || tile * kTile < stage.from || there != 15; };
 
   // ---- keys run one tile ahead of the values: at tile t keys t + 1 and values t are needed, keys t + 2 and values t + 1 asked for (a ring of
   // three tiles and 8 wavefronts, which ask for them a tile earlier, measured the same).  Codes of an 8-bit cache pass through registers:
@@ -317,15 +326,17 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
       }
       if constexpr (kNext) __builtin_amdgcn_sched_barrier(0);
     }
-    between(t);
     if constexpr (kNext) {
-      // the weights are needed behind the branch only, and would be formed there, with no products beside them
+      // the weights are needed behind the branches only, and would be formed there, with no products beside them
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int st = 0; st < 4; ++st) asm volatile("" : "+v"(p[b][st]));
+    }
+    between(t);
+    if constexpr (kNext) {
       const int there = stage.there(t + 1);
-      if (partial(t + 1, there)) mask_scores(sn, (t + 1) * kTile, last, stage.to, there);
+      if (partial(t + 1, there)) mask_scores(sn, (t + 1) * kTile, last, stage.from, stage.to, there);
     }
     float top[NB];
 #pragma unroll
@@ -372,7 +383,7 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
       for (int b = 0; b < NB; ++b) s0[b][g % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, w.q[b][g / 2], g < 2 ? zero : s0[b][g % 2], 0, 0, 0);
     }
     const int there = stage.there(first);
-    if (partial(first, there)) mask_scores(s0, first * kTile, last, stage.to, there);
+    if (partial(first, there)) mask_scores(s0, first * kTile, last, stage.from, stage.to, there);
     float top[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) top[b] = -INFINITY;

@@ -65,7 +65,7 @@ def test_cache_descriptor_errors(call):
 
 @pytest.mark.parametrize("call", [_append, _extend, _decode])
 def test_batch_errors(call):
-    assert call(seqs=_seqs(n_seqs=-1)) == 2 and call(seqs=_seqs(n_seqs=4097)) == 2
+    assert call(seqs=_seqs(n_seqs=-1)) == 2 and call(seqs=_seqs(n_seqs=2049)) == 2
     assert call(seqs=_seqs(table_pages=0)) == 2 and call(seqs=_seqs(table_pages=1 << 30)) == 2
     assert call(seqs=_seqs(kv_len=None)) == 1 and call(seqs=_seqs(page_table=None)) == 1
     assert call(seqs=_seqs(n_seqs=0, kv_len=None, page_table=None)) == 0                  # no sequences: nothing to do
@@ -97,11 +97,11 @@ def test_prompt_and_extend_errors():
         n = 1 if call is _prompt else 3
         need = lib.mes_attn_prompt_workspace_bytes(5, n, 4, 2, 64)
         assert need > 0 and call(ws=FAKE, wsb=need - 1) == 7 and call(ws=ODD, wsb=need) == 6       # NULL is fine: no item is cut
-    for bad in ((-1, 1, 4, 2, 64), (5, -1, 4, 2, 64), (5, 4097, 4, 2, 64), (5, 1, 5, 2, 64), (5, 1, 4, 2, 32)):
+    for bad in ((-1, 1, 4, 2, 64), (5, -1, 4, 2, 64), (5, 2049, 4, 2, 64), (5, 1, 5, 2, 64), (5, 1, 4, 2, 32)):
         assert lib.mes_attn_prompt_workspace_bytes(*bad) == 0
     assert lib.mes_attn_prompt_workspace_bytes(1 << 20, 64, 32, 8, 128) == (1024 + 512) * 128 * (8 + 128 * 4)
     assert _prompt(k=None) == 1 and _prompt(v=ODD) == 6 and _prompt(ld_k=64) == 2 and _prompt(ld_v=129) == 2
-    assert _prompt(off=None) == 1 and _prompt(n=-1) == 2 and _prompt(n=4097) == 2 and _prompt(n=0) == 0
+    assert _prompt(off=None) == 1 and _prompt(n=-1) == 2 and _prompt(n=2049) == 2 and _prompt(n=0) == 0
     assert _prompt(dim=80) == 2 and _prompt(kvh=0) == 2
     assert _extend(seqs=_seqs(q_offsets=None)) == 1
 
@@ -117,8 +117,8 @@ def test_decode_errors():
     need = lib.mes_attn_decode_workspace_bytes(3, 4, 2, 64)
     assert need > 0 and _decode(wsb=need - 1) == 7 and _decode(ws=None) == 7 and _decode(ws=ODD) == 6
     assert b"workspace" in lib.mes_last_error()
-    assert _decode(seqs=_seqs(n_seqs=4096, table_pages=1 << 20), seg=None, pre=None) == 2  # more units than 32 bits number
-    for bad in ((0, 4, 2, 64), (4097, 4, 2, 64), (3, 5, 2, 64), (3, 4, 0, 64), (3, 4, 2, 96), (3, 130, 2, 64)):
+    assert _decode(seqs=_seqs(n_seqs=2048, table_pages=1 << 22), seg=None, pre=None) == 2  # more units than 32 bits number
+    for bad in ((0, 4, 2, 64), (2049, 4, 2, 64), (3, 5, 2, 64), (3, 4, 0, 64), (3, 4, 2, 96), (3, 130, 2, 64)):
         assert lib.mes_attn_decode_workspace_bytes(*bad) == 0
     assert lib.mes_attn_decode_workspace_bytes(256, 32, 8, 128) < 64 << 20
 
