@@ -22,7 +22,12 @@
 namespace mes {
 namespace {
 
-constexpr int kThreads = 256, kUnit = 128, kRowsPass = 128, kFewRows = 16, kWorkgroups = 512;
+constexpr int kThreads = 256, kUnit = 128, kRowsPass = 128, kFewRows = 16;
+// Workgroups of a launch: what the chip holds.  Without shared prefixes and with up to 16 heads per key / value head only the small body is
+// needed, which leaves room for three per compute unit.
+constexpr int kWorkgroups = 512, kWorkgroupsFew = 768;
+// Up to this many tokens a sequence is one workgroup's, where nothing is shared: no second launch to add up pieces.
+constexpr int kWholeTokens = 512;
 static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
 
 struct Shape {                       // what host and device derive alike
@@ -41,7 +46,7 @@ struct Layout {
 
 __host__ __device__ inline Layout layout(int n_seqs, int n_kv_heads, int group, int n_passes, int head_dim) {
   const size_t pre = (size_t)(n_passes ? kWorkgroups + n_kv_heads * n_passes : 0) * kRowsPass;
-  const size_t own = (size_t)(kWorkgroups + n_kv_heads * n_seqs) * group;
+  const size_t own = (size_t)(kWorkgroupsFew + n_kv_heads * n_seqs) * group;
   Layout y;
   y.prefix_o = 0;
   y.own_o = y.prefix_o + pre * head_dim * 4;
@@ -76,14 +81,15 @@ __device__ __forceinline__ int dim_of(int c, int g) {
 }
 
 struct Segment {                                    // a piece of the line
-  int seq, seq0, rows;                              // page table; sequence of row 0; query rows
+  int kvh, seq, seq0, rows;                         // key / value head; page table; sequence of row 0; query rows
   int from, to, t0, t1;                             // tokens of [from, to) in the units [t0, t1), t0 a multiple of 64
 };
 
-template <int D>
+struct Nothing {};
+template <int D, bool MANY>
 struct Shared {
   union {
-    TileLds<D> tiles;
+    std::conditional_t<MANY, TileLds<D>, Nothing> tiles;
     struct {
       float merge[4][kFewRows][D + 4];
       float2 ml[4][kFewRows];
@@ -94,62 +100,61 @@ struct Shared {
   int part[4];
 };
 
-// The weighted sum over one piece, up to 16 query rows, into o / ml_out (or out where the piece is all that its rows see).
+// The weighted sum over a piece with up to 16 query rows.  Pieces follow one another without a pause: a wavefront asks for the next piece's
+// first tokens where it would ask for more of this one's, and knows their pages by then.
 template <int D, bool FP8>
-__device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D>& sh, bool direct, float* o, float2* ml_out) {
-  constexpr int VD = D / 16, KS = D / 32;
+struct Few {
+  static constexpr int VD = D / 16, KS = D / 32;
   typedef Raw<D, FP8> R;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+  const DecodeArgs& a;
+  int group, lane, wave, col, quad;
+  u32x4 q[KS];                                      // Q^T operands
+  R raw;                                            // the step that comes next
+  int there[2];                                     // its pages
+  int pages[2];                                     // of 64 steps of the piece, one step per lane
 
-  u32x4 q[KS];
-#pragma unroll
-  for (int c = 0; c < KS; ++c) {
-    q[c] = u32x4{0, 0, 0, 0};
-    if (col < g.rows)
-      q[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(kvh * group + col % group) * D + dim_of<D, FP8>(c, quad));
-  }
-  __syncthreads();                                  // the last piece's reads of LDS are over
+  __device__ Few(const DecodeArgs& args, int g) : a(args), group(g), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), col(lane & 15), quad(lane >> 4) {}
 
-  const float scale = a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f);
-  const int32_t* table = a.page_table + (size_t)g.seq * a.table_pages;
-  f32x4 acc[VD];
-  float m = -INFINITY, l = 0.0f;
-#pragma unroll
-  for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
-
-  // the pages of this wavefront's next 64 steps, one step per lane
-  const int n_steps = (g.t1 - g.t0 + 31) / 32, mine = (n_steps - wave + 3) / 4;   // steps wave, wave + 4, ...
-  int pages[2] = {-1, -1};
-  auto look_up = [&](int first) {
+  __device__ __forceinline__ int steps(const Segment& g) const { return ((g.t1 - g.t0 + 31) / 32 - wave + 3) / 4; }   // steps wave, wave + 4, ...
+  __device__ __forceinline__ void look_up(const Segment& g, int first, int (&pg)[2]) const {
+    const int32_t* table = a.page_table + (size_t)g.seq * a.table_pages;
+    const int mine = steps(g);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int t = g.t0 + (4 * (first + lane) + wave) * 32 + 16 * h;
-      pages[h] = first + lane < mine && t < g.to ? table[t >> a.page_shift] : -1;
+      pg[h] = first + lane < mine && t < g.to ? table[t >> a.page_shift] : -1;
     }
-  };
-  R raw;
-  int there[2];                                     // pages of the step in `raw`
-  auto request_k = [&](int i, int (&pg)[2]) {
+  }
+  __device__ __forceinline__ void load_q(const Segment& g) {
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      q[c] = u32x4{0, 0, 0, 0};
+      if (col < g.rows)
+        q[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(g.kvh * group + col % group) * D + dim_of<D, FP8>(c, quad));
+    }
+  }
+  __device__ __forceinline__ size_t row_of(const Segment& g, int t, int page) const {   // first element of token t's row
+    return ((((size_t)((unsigned)page < (unsigned)a.n_pages ? page : 0) * a.n_kv_heads + g.kvh) << a.page_shift) + (t & ((1 << a.page_shift) - 1))) * D;
+  }
+  __device__ __forceinline__ void request_k(const Segment& g, int i, const int (&pg)[2], int (&next)[2]) {
     const int t = g.t0 + (4 * i + wave) * 32;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      pg[h] = __builtin_amdgcn_readlane(pages[h], i & 63);
-      const int page = (unsigned)pg[h] < (unsigned)a.n_pages ? pg[h] : 0;
-      const size_t at = ((((size_t)page * a.n_kv_heads + kvh) << a.page_shift) + ((t + 16 * h) & ((1 << a.page_shift) - 1)) + col) * D;
+      next[h] = __builtin_amdgcn_readlane(pg[h], i & 63);
+      const size_t at = row_of(g, t + 16 * h, next[h]) + col * D;
 #pragma unroll
       for (int c = 0; c < R::KC; ++c) {
         if constexpr (FP8) raw.k[h][c] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.k) + at + 64 * c + 16 * quad);
         else raw.k[h][c] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.k) + at + 32 * c + 8 * quad);
       }
     }
-  };
-  auto request_v = [&](int i, const int (&pg)[2]) {
+  }
+  __device__ __forceinline__ void request_v(const Segment& g, int i, const int (&next)[2]) {
     const int t = g.t0 + (4 * i + wave) * 32;
+    typedef uint32_t words __attribute__((ext_vector_type(R::VW)));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int page = (unsigned)pg[h] < (unsigned)a.n_pages ? pg[h] : 0;
-      const size_t at = ((((size_t)page * a.n_kv_heads + kvh) << a.page_shift) + ((t + 16 * h) & ((1 << a.page_shift) - 1)) + 4 * quad) * D + VD * col;
-      typedef uint32_t words __attribute__((ext_vector_type(R::VW)));
+      const size_t at = row_of(g, t + 16 * h, next[h]) + 4 * quad * D + VD * col;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const void* p = FP8 ? (const void*)(static_cast<const uint8_t*>(a.v) + at + e * D) : (const void*)(static_cast<const uint16_t*>(a.v) + at + e * D);
@@ -161,13 +166,29 @@ __device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh,
         }
       }
     }
-  };
-
-  if (mine > 0) {
-    look_up(0);
-    request_k(0, there);
-    request_v(0, there);
   }
+  __device__ __forceinline__ void start(const Segment& g) {   // a piece that nobody has asked for
+    look_up(g, 0, pages);
+    load_q(g);
+    if (steps(g) > 0) {
+      request_k(g, 0, pages, there);
+      request_v(g, 0, there);
+    }
+  }
+
+  // The piece g, its first step asked for; ahead: so is the first step of the piece `then` at the end.  Into o / ml_out, or out where the piece
+  // is all that its rows see.
+  template <class SH>
+  __device__ __forceinline__ void run(const Segment& g, bool ahead, const Segment& then, SH& sh, bool direct, float* o, float2* ml_out) {
+  const float scale = a.scale * kLog2e * (FP8 ? a.k_scale[g.kvh] : 1.0f);
+  f32x4 acc[VD];
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll
+  for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
+  const int mine = steps(g);
+  int pages_then[2] = {-1, -1};
+  if (ahead) look_up(then, 0, pages_then);
+  ahead = ahead && steps(then) > 0;
   for (int i = 0; i < mine; ++i) {
     const int t = g.t0 + (4 * i + wave) * 32;
     const bool ok0 = (unsigned)there[0] < (unsigned)a.n_pages, ok1 = (unsigned)there[1] < (unsigned)a.n_pages;
@@ -219,8 +240,10 @@ __device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh,
     int next[2] = {-1, -1};
     const bool more = i + 1 < mine;
     if (more) {
-      if (((i + 1) & 63) == 0) look_up(i + 1);
-      request_k(i + 1, next);
+      if (((i + 1) & 63) == 0) look_up(g, i + 1, pages);
+      request_k(g, i + 1, pages, next);
+    } else if (ahead) {
+      request_k(then, 0, pages_then, next);
     }
     if (!whole) {                                   // what no row sees must not turn a weight of 0 into NaN
 #pragma unroll
@@ -245,12 +268,23 @@ __device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh,
         acc[2 * jw + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[2 * jw + odd], 0, 0, 0);
       }
     }
-    if (more) request_v(i + 1, next);
+    if (more) request_v(g, i + 1, next);
+    else if (ahead) request_v(then, 0, next);
     there[0] = next[0];
     there[1] = next[1];
   }
+  if (ahead) {
+    load_q(then);
+    if (mine == 0) {
+      request_k(then, 0, pages_then, there);
+      request_v(then, 0, there);
+    }
+  }
+  pages[0] = pages_then[0];
+  pages[1] = pages_then[1];
 
   // ---- the four wavefronts' results on one maximum, added in their order
+  __syncthreads();                                  // the last piece's reads of LDS are over
   l += other_row16(l);
   l += other_half(l);
   if (lane < 16) sh.ml[wave][lane] = make_float2(m, l);
@@ -278,8 +312,8 @@ __device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh,
 #pragma unroll
       for (int j = 0; j < VD; ++j) x[j] = sh.merge[0][row][d0 + j] + sh.merge[1][row][d0 + j] + sh.merge[2][row][d0 + j] + sh.merge[3][row][d0 + j];
       if (direct) {
-        const float inv = lr == 0.0f ? 0.0f : (FP8 ? a.v_scale[kvh] : 1.0f) / lr;
-        uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(kvh * group + row % group) * D + d0;
+        const float inv = lr == 0.0f ? 0.0f : (FP8 ? a.v_scale[g.kvh] : 1.0f) / lr;
+        uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(g.kvh * group + row % group) * D + d0;
 #pragma unroll
         for (int j = 0; j < VD; j += 4)
           *reinterpret_cast<u32x2*>(dst + j) = u32x2{pack2(x[j] * inv, x[j + 1] * inv), pack2(x[j + 2] * inv, x[j + 3] * inv)};
@@ -290,13 +324,15 @@ __device__ __forceinline__ void run_few(const DecodeArgs& a, int group, int kvh,
       }
     }
   }
-}
+  }
+};
 
 // The same for up to 128 rows: 32 per wavefront.
 template <int D, bool FP8>
-__device__ __forceinline__ void run_many(const DecodeArgs& a, int group, int kvh, const Segment& g, Shared<D>& sh, bool direct, float* o, float2* ml_out) {
+__device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const Segment& g, Shared<D, true>& sh, bool direct, float* o, float2* ml_out) {
   constexpr int KS = D / 16, DT = D / 32, SRC = FP8 ? KV_PAGED_E4M3 : KV_PAGED;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, row = kWaveRows * wave + (lane & 31);
+  const int kvh = g.kvh;
   Stage<D, SRC> stage(sh.tiles);
   stage.k = static_cast<const char*>(a.k);
   stage.v = static_cast<const char*>(a.v);
@@ -339,14 +375,24 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, int kvh
   }
 }
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
-  __shared__ __align__(16) Shared<D> sh;
+// MANY: pieces of more than 16 rows can occur.  WHOLE: workgroup i does sequence i % n_seqs alone, and there is nothing to join.
+template <int D, bool FP8, bool MANY, bool WHOLE>
+__global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCall c) {
+  __shared__ __align__(16) Shared<D, MANY> sh;
   const DecodeArgs& a = c.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int n_items = a.n_groups + a.n_seqs;
   auto length = [&](int s) { return min(max(a.kv_len[s], 0), a.capacity); };
   auto units = [](int from, int to) { return to > from ? (to - (from & ~63) + kUnit - 1) / kUnit : 0; };
+
+  if constexpr (WHOLE) {
+    Few<D, FP8> few(a, c.sh.group);
+    const int s = blockIdx.x % a.n_seqs;
+    const Segment g = {(int)blockIdx.x / a.n_seqs, s, s, c.sh.group, 0, uniform(length(s)), 0, uniform(length(s))};
+    few.start(g);
+    few.run(g, false, g, sh, true, nullptr, nullptr);
+    return;
+  }
 
   // ---- units of every item, groups first
   for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[a.n_groups + s] = units(0, length(s));
@@ -417,9 +463,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
   }
 
   // ---- this workgroup's chunk, piece by piece
-  int u = (int)blockIdx.x * chunk;                  // at most `all` + grid, which fits
-  const int end = min(u + chunk, all);
-  while (u < end) {
+  const int begin = (int)min((int64_t)blockIdx.x * chunk, (int64_t)all), end = min(begin + chunk, all);
+  struct Piece {
+    Segment g;
+    int units;
+    bool direct;
+    float* o;
+    float2* ml;
+  };
+  auto piece_at = [&](int u) {
+    Piece p;
+    Segment& g = p.g;
     const int h = u / per_head, in_head = u % per_head;
     int lo = 0, hi = n_items - 1;                   // last item that begins at or before the unit (those of no units come before it)
     while (lo < hi) {
@@ -428,10 +482,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     }
     const int it = uniform(lo), first = uniform(sh.cum[it]), n = uniform(sh.cum[it + 1]) - first;
     int from_unit = in_head - first, to_unit = min(from_unit + end - u, n);
-    Segment g;
-    float* o;
-    float2* ml;
-    bool direct = false;
+    g.kvh = h;
+    p.direct = false;
     if (it < a.n_groups) {
       const int tiles = (a.prefix[it] + kUnit - 1) / kUnit, pass = from_unit / tiles;
       from_unit -= pass * tiles;
@@ -441,11 +493,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       g.rows = min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group;
       g.from = 0;
       g.to = a.prefix[it];
-      g.t0 = from_unit * kUnit;
-      g.t1 = min(to_unit * kUnit, g.to);
       const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
-      o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
-      ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
+      p.o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
+      p.ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
     } else {
       const int s = it - a.n_groups;
       g.seq = g.seq0 = s;
@@ -455,19 +505,45 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       for (int k = 0; k < a.n_groups; ++k)
         if (s >= a.first[k] && s < a.behind[k] && sh.group_src[k] >= 0 && g.to >= a.prefix[k]) g.from = a.prefix[k];
       g.from = uniform(g.from);
-      g.t0 = (g.from & ~63) + from_unit * kUnit;
-      g.t1 = min((g.from & ~63) + to_unit * kUnit, g.to);
       const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
-      direct = g.from == 0 && from_unit == 0 && to_unit == n;
-      o = reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D;
-      ml = reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group;
+      p.direct = g.from == 0 && from_unit == 0 && to_unit == n;
+      p.o = reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D;
+      p.ml = reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group;
     }
-    g.t0 = uniform(g.t0);
-    g.t1 = uniform(g.t1);
+    g.t0 = uniform((g.from & ~63) + from_unit * kUnit);
+    g.t1 = uniform(min((g.from & ~63) + to_unit * kUnit, g.to));
     g.rows = uniform(g.rows);
-    if (g.rows <= kFewRows) run_few<D, FP8>(a, c.sh.group, h, g, sh, direct, o, ml);
-    else run_many<D, FP8>(a, c.sh.group, h, g, sh, direct, o, ml);
-    u += to_unit - from_unit;
+    p.units = uniform(to_unit - from_unit);
+    return p;
+  };
+  if (begin >= end) return;
+  // first the pieces of many rows, then the others: in one loop both bodies would keep registers for each other
+  if constexpr (MANY) {
+    for (int u = begin; u < end;) {
+      const Piece p = piece_at(u);
+      u += p.units;
+      if (p.g.rows > kFewRows) run_many<D, FP8>(a, c.sh.group, p.g, sh, p.direct, p.o, p.ml);
+    }
+    asm volatile("" ::: "memory");
+  }
+  int u = begin;
+  auto next_few = [&](Piece& p) {
+    while (u < end) {
+      p = piece_at(u);
+      u += p.units;
+      if (!MANY || p.g.rows <= kFewRows) return true;
+    }
+    return false;
+  };
+  Piece p;
+  if (!next_few(p)) return;
+  Few<D, FP8> few(a, c.sh.group);
+  few.start(p.g);
+  for (bool more = true; more;) {
+    Piece then = p;
+    more = next_few(then);                          // while the piece's first tokens are on their way
+    few.run(p.g, more, then.g, sh, p.direct, p.o, p.ml);
+    p = then;
   }
 }
 
@@ -546,11 +622,23 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
 
 template <int D>
 hipError_t launch(const DecodeCall& c, bool fp8, hipStream_t s) {
+  const bool many = c.sh.group > kFewRows || c.a.n_groups > 0;
+  if (!many && c.a.capacity <= kWholeTokens) {
+    const unsigned items = (unsigned)(c.a.n_kv_heads * c.a.n_seqs);
+    if (fp8) k_attn_decode<D, true, false, true><<<items, kThreads, 0, s>>>(c);
+    else k_attn_decode<D, false, false, true><<<items, kThreads, 0, s>>>(c);
+    return hipGetLastError();
+  }
   // never more workgroups than units there can be
   const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kUnit - 1) / kUnit + 1);
-  const unsigned grid = (unsigned)std::min<int64_t>(kWorkgroups, most);
-  if (fp8) k_attn_decode<D, true><<<grid, kThreads, 0, s>>>(c);
-  else k_attn_decode<D, false><<<grid, kThreads, 0, s>>>(c);
+  const unsigned grid = (unsigned)std::min<int64_t>(many ? kWorkgroups : kWorkgroupsFew, most);
+  if (many) {
+    if (fp8) k_attn_decode<D, true, true, false><<<grid, kThreads, 0, s>>>(c);
+    else k_attn_decode<D, false, true, false><<<grid, kThreads, 0, s>>>(c);
+  } else {
+    if (fp8) k_attn_decode<D, true, false, false><<<grid, kThreads, 0, s>>>(c);
+    else k_attn_decode<D, false, false, false><<<grid, kThreads, 0, s>>>(c);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   const int rows = c.a.n_seqs * c.a.n_heads;
   if (rows <= 1024) k_join<D, 4><<<rows, kThreads, 0, s>>>(c, fp8);

@@ -300,7 +300,7 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
     if (kNext) next_k(t + 1);
     if (t > first) next_v(t);
     u32x4 p[NB][4];
-    constexpr int kAhead = 3;                                       // operands on their way
+    constexpr int kAhead = SRC == KV_PAGED_E4M3 ? 2 : 3;            // operands on their way; codes of the 8-bit cache need the registers
     bf16x8 ring[kAhead + 1];
     if constexpr (kNext) {
 #pragma unroll

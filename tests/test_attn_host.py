@@ -120,7 +120,7 @@ def test_decode_errors():
     assert _decode(seqs=_seqs(n_seqs=2048, table_pages=1 << 22), seg=None, pre=None) == 2  # more units than 32 bits number
     for bad in ((0, 4, 2, 64), (2049, 4, 2, 64), (3, 5, 2, 64), (3, 4, 0, 64), (3, 4, 2, 96), (3, 130, 2, 64)):
         assert lib.mes_attn_decode_workspace_bytes(*bad) == 0
-    assert lib.mes_attn_decode_workspace_bytes(256, 32, 8, 128) < 64 << 20
+    assert lib.mes_attn_decode_workspace_bytes(256, 32, 8, 128) < 96 << 20
 
 
 def test_copy_errors():
