@@ -30,6 +30,9 @@ constexpr int kWorkgroups = 512, kWorkgroupsFew = 768;
 constexpr int kWholeTokens = 512;
 static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
 
+// tokens of a unit of a shared prefix: tiles of many rows take about as long as twice as many tokens of few rows
+__device__ __forceinline__ int prefix_unit(int sequences, int per_pass, int group) { return kUnit; }
+
 struct Shape {                       // what host and device derive alike
   int group, per_pass, n_passes;     // query heads per key / value head, sequences per pass, passes of all groups
 };
@@ -170,16 +173,15 @@ struct Few {
   __device__ __forceinline__ void start(const Segment& g) {   // a piece that nobody has asked for
     look_up(g, 0, pages);
     load_q(g);
-    if (steps(g) > 0) {
-      request_k(g, 0, pages, there);
-      request_v(g, 0, there);
-    }
+    raw = R{};
+    there[0] = there[1] = -1;
   }
 
-  // The piece g, its first step asked for; ahead: so is the first step of the piece `then` at the end.  Into o / ml_out, or out where the piece
-  // is all that its rows see.
+  // The piece g, its first step asked for unless it is `fresh`; ahead: so is the first step of the piece `then` at the end.  Into o / ml_out, or
+  // out where the piece is all that its rows see.  A fresh piece takes a step of nothing first, which asks for its first tokens: the code of
+  // a step is then there before the loads of a whole chip are on their way, behind which it would be fetched (3 to 8 us).
   template <class SH>
-  __device__ __forceinline__ void run(const Segment& g, bool ahead, const Segment& then, SH& sh, bool direct, float* o, float2* ml_out) {
+  __device__ __forceinline__ void run(const Segment& g, bool fresh, bool ahead, const Segment& then, SH& sh, bool direct, float* o, float2* ml_out) {
   const float scale = a.scale * kLog2e * (FP8 ? a.k_scale[g.kvh] : 1.0f);
   f32x4 acc[VD];
   float m = -INFINITY, l = 0.0f;
@@ -189,7 +191,7 @@ struct Few {
   int pages_then[2] = {-1, -1};
   if (ahead) look_up(then, 0, pages_then);
   ahead = ahead && steps(then) > 0;
-  for (int i = 0; i < mine; ++i) {
+  for (int i = fresh || mine == 0 ? -1 : 0; i < mine; ++i) {
     const int t = g.t0 + (4 * i + wave) * 32;
     const bool ok0 = (unsigned)there[0] < (unsigned)a.n_pages, ok1 = (unsigned)there[1] < (unsigned)a.n_pages;
     const bool whole = ok0 && ok1 && t >= g.from && t + 32 <= g.to;
@@ -240,7 +242,7 @@ struct Few {
     int next[2] = {-1, -1};
     const bool more = i + 1 < mine;
     if (more) {
-      if (((i + 1) & 63) == 0) look_up(g, i + 1, pages);
+      if (((i + 1) & 63) == 0 && i > 0) look_up(g, i + 1, pages);
       request_k(g, i + 1, pages, next);
     } else if (ahead) {
       request_k(then, 0, pages_then, next);
@@ -273,13 +275,7 @@ struct Few {
     there[0] = next[0];
     there[1] = next[1];
   }
-  if (ahead) {
-    load_q(then);
-    if (mine == 0) {
-      request_k(then, 0, pages_then, there);
-      request_v(then, 0, there);
-    }
-  }
+  if (ahead) load_q(then);
   pages[0] = pages_then[0];
   pages[1] = pages_then[1];
 
@@ -338,7 +334,7 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const S
   stage.v = static_cast<const char*>(a.v);
   stage.kvh = kvh;
   stage.from = g.from;
-  stage.to = g.to;
+  stage.to = g.t1;
   stage.table = a.page_table + (size_t)g.seq * a.table_pages;
   stage.page_shift = a.page_shift;
   stage.n_pages = a.n_pages;
@@ -381,7 +377,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
   __shared__ __align__(16) Shared<D, MANY> sh;
   const DecodeArgs& a = c.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int n_items = a.n_groups + a.n_seqs;
+  const int n_groups = MANY ? a.n_groups : 0, n_items = n_groups + a.n_seqs;
   auto length = [&](int s) { return min(max(a.kv_len[s], 0), a.capacity); };
   auto units = [](int from, int to) { return to > from ? (to - (from & ~63) + kUnit - 1) / kUnit : 0; };
 
@@ -390,14 +386,14 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     const int s = blockIdx.x % a.n_seqs;
     const Segment g = {(int)blockIdx.x / a.n_seqs, s, s, c.sh.group, 0, uniform(length(s)), 0, uniform(length(s))};
     few.start(g);
-    few.run(g, false, g, sh, true, nullptr, nullptr);
+    few.run(g, true, false, g, sh, true, nullptr, nullptr);
     return;
   }
 
   // ---- units of every item, groups first
-  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[a.n_groups + s] = units(0, length(s));
+  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[n_groups + s] = units(0, length(s));
   __syncthreads();
-  for (int g = wave; g < a.n_groups; g += 4) {
+  for (int g = wave; g < n_groups; g += 4) {
     const int first = a.first[g], behind = a.behind[g], prefix = a.prefix[g];
     int count = 0, src = -1;
     for (int s0 = first; s0 < behind; s0 += 64) {
@@ -408,10 +404,11 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     const bool active = count >= 2;
     if (active)
       for (int s = first + lane; s < behind; s += 64)
-        if (length(s) >= prefix) sh.cum[a.n_groups + s] = units(prefix, length(s));
+        if (length(s) >= prefix) sh.cum[n_groups + s] = units(prefix, length(s));
     if (lane == 0) {
       sh.group_src[g] = active ? src : -1;
-      sh.cum[g] = active ? (prefix + kUnit - 1) / kUnit * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
+      const int unit = prefix_unit(behind - first, c.sh.per_pass, c.sh.group);
+      sh.cum[g] = active ? (prefix + unit - 1) / unit * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
     }
   }
   __syncthreads();
@@ -436,31 +433,8 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
   const int per_head = uniform(sh.cum[n_items]), all = per_head * a.n_kv_heads;
   const int chunk = max((all + (int)gridDim.x - 1) / (int)gridDim.x, 1);
 
-  // ---- where the join finds every row's pieces
   const Layout y = layout(a.n_seqs, a.n_kv_heads, c.sh.group, c.sh.n_passes, D);
   char* ws = static_cast<char*>(a.ws);
-  Meta* meta = reinterpret_cast<Meta*>(ws + y.meta);
-  for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_kv_heads * a.n_seqs; i += gridDim.x * kThreads) {
-    const int h = i / a.n_seqs, s = i % a.n_seqs, it = a.n_groups + s;
-    Meta w = make_int4(0, 0, 0, 0);
-    for (int g = 0; g < a.n_groups; ++g) {
-      if (s < a.first[g] || s >= a.behind[g]) continue;
-      if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
-        const int n = (a.prefix[g] + kUnit - 1) / kUnit, pass = (s - a.first[g]) / c.sh.per_pass;
-        const int u0 = h * per_head + sh.cum[g] + pass * n, w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
-        w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
-        w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
-      }
-      break;
-    }
-    const int u0 = h * per_head + sh.cum[it], n = sh.cum[it + 1] - sh.cum[it];
-    if (n > 0) {
-      const int w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
-      w.x = w0 + i;
-      w.y = w0 == w1 && w.w == 0 ? -1 : w1 - w0 + 1;
-    }
-    meta[i] = w;
-  }
 
   // ---- this workgroup's chunk, piece by piece
   const int begin = (int)min((int64_t)blockIdx.x * chunk, (int64_t)all), end = min(begin + chunk, all);
@@ -484,8 +458,9 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     int from_unit = in_head - first, to_unit = min(from_unit + end - u, n);
     g.kvh = h;
     p.direct = false;
-    if (it < a.n_groups) {
-      const int tiles = (a.prefix[it] + kUnit - 1) / kUnit, pass = from_unit / tiles;
+    if (it < n_groups) {
+      const int unit = prefix_unit(a.behind[it] - a.first[it], c.sh.per_pass, c.sh.group);
+      const int tiles = (a.prefix[it] + unit - 1) / unit, pass = from_unit / tiles;
       from_unit -= pass * tiles;
       to_unit = min(to_unit - pass * tiles, tiles);
       g.seq = uniform(sh.group_src[it]);
@@ -493,25 +468,29 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
       g.rows = min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group;
       g.from = 0;
       g.to = a.prefix[it];
+      g.t0 = from_unit * unit;
+      g.t1 = min(to_unit * unit, g.to);
       const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
       p.o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
       p.ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
     } else {
-      const int s = it - a.n_groups;
+      const int s = it - n_groups;
       g.seq = g.seq0 = s;
       g.rows = c.sh.group;
       g.to = uniform(length(s));
       g.from = 0;
-      for (int k = 0; k < a.n_groups; ++k)
+      for (int k = 0; k < n_groups; ++k)
         if (s >= a.first[k] && s < a.behind[k] && sh.group_src[k] >= 0 && g.to >= a.prefix[k]) g.from = a.prefix[k];
       g.from = uniform(g.from);
       const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
       p.direct = g.from == 0 && from_unit == 0 && to_unit == n;
       p.o = reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D;
       p.ml = reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group;
+      g.t0 = (g.from & ~63) + from_unit * kUnit;
+      g.t1 = min((g.from & ~63) + to_unit * kUnit, g.to);
     }
-    g.t0 = uniform((g.from & ~63) + from_unit * kUnit);
-    g.t1 = uniform(min((g.from & ~63) + to_unit * kUnit, g.to));
+    g.t0 = uniform(g.t0);
+    g.t1 = uniform(g.t1);
     g.rows = uniform(g.rows);
     p.units = uniform(to_unit - from_unit);
     return p;
@@ -535,15 +514,38 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     }
     return false;
   };
-  Piece p;
-  if (!next_few(p)) return;
+  Piece p, then;
   Few<D, FP8> few(a, c.sh.group);
-  few.start(p.g);
-  for (bool more = true; more;) {
-    Piece then = p;
-    more = next_few(then);                          // while the piece's first tokens are on their way
-    few.run(p.g, more, then.g, sh, p.direct, p.o, p.ml);
+  for (int round = 0;; ++round) {
+    const bool more = next_few(then);               // while the first tokens of piece p are on their way
+    if (round) few.run(p.g, round == 1, more, then.g, sh, p.direct, p.o, p.ml);
+    else if (more) few.start(then.g);
+    if (!more) break;
     p = then;
+  }
+
+  // ---- where the join finds every row's pieces
+  Meta* meta = reinterpret_cast<Meta*>(ws + y.meta);
+  for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_kv_heads * a.n_seqs; i += gridDim.x * kThreads) {
+    const int h = i / a.n_seqs, s = i % a.n_seqs, it = n_groups + s;
+    Meta w = make_int4(0, 0, 0, 0);
+    for (int g = 0; g < n_groups; ++g) {
+      if (s < a.first[g] || s >= a.behind[g]) continue;
+      if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
+        const int unit = prefix_unit(a.behind[g] - a.first[g], c.sh.per_pass, c.sh.group), n = (a.prefix[g] + unit - 1) / unit, pass = (s - a.first[g]) / c.sh.per_pass;
+        const int u0 = h * per_head + sh.cum[g] + pass * n, w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
+        w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
+        w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
+      }
+      break;
+    }
+    const int u0 = h * per_head + sh.cum[it], n = sh.cum[it + 1] - sh.cum[it];
+    if (n > 0) {
+      const int w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
+      w.x = w0 + i;
+      w.y = w0 == w1 && w.w == 0 ? -1 : w1 - w0 + 1;
+    }
+    meta[i] = w;
   }
 }
 
@@ -552,7 +554,6 @@ template <int D, int W>
 __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
   constexpr int E = D / 64;                          // dimensions per lane
   __shared__ float part[4][D];
-  __shared__ float2 part_ml[4];
   const DecodeArgs& a = c.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), group = c.sh.group;
   const int row = W == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
@@ -570,8 +571,9 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
   float m = -INFINITY, l = 0.0f, x[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] = 0.0f;
-  // up to 64 pieces at a time: lane i weighs piece i
-  for (int i0 = W == 4 ? wave * 64 : 0; i0 < n; i0 += 64 * W) {
+  // up to 64 pieces at a time: lane i weighs piece i; a wavefront adds up every W-th, kBatch of them on their way at a time
+  constexpr int kBatch = 8;
+  for (int i0 = 0; i0 < n; i0 += 64) {
     const int i = i0 + lane, count = min(64, n - i0);
     float2 ml = make_float2(-INFINITY, 0.0f);
     if (i < n) ml = i < n_pre ? pre_ml[(size_t)i * kRowsPass] : own_ml[(size_t)(i - n_pre) * group];
@@ -587,32 +589,30 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
     m = raised;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= shrink;
-#pragma unroll 4
-    for (int k = 0; k < count; ++k) {
-      const int p = i0 + k;
-      const float f = __shfl(weight, k);
-      const float* o = p < n_pre ? pre_o + (size_t)p * kRowsPass * D : own_o + (size_t)(p - n_pre) * group * D;
+    for (int k0 = W == 4 ? wave : 0; k0 < count; k0 += W * kBatch) {
+      float v[kBatch][E], f[kBatch];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(f, o[E * lane + e], x[e]);
+      for (int b = 0; b < kBatch; ++b) {
+        const int k = min(k0 + W * b, count - 1), p = i0 + k;
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), k));
+        f[b] = k0 + W * b < count ? w : 0.0f;
+        const float* o = p < n_pre ? pre_o + (size_t)p * kRowsPass * D : own_o + (size_t)(p - n_pre) * group * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[b][e] = o[E * lane + e];
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(f[b], v[b][e], x[e]);
     }
   }
-  if constexpr (W == 4) {
+  if constexpr (W == 4) {                            // all four have the same maximum and sum
 #pragma unroll
     for (int e = 0; e < E; ++e) part[wave][E * lane + e] = x[e];
-    if (lane == 0) part_ml[wave] = make_float2(m, l);
     __syncthreads();
     if (wave) return;
-    float top = -INFINITY;
-    for (int k = 0; k < 4; ++k) top = fmaxf(top, part_ml[k].x);
-    l = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.0f;
-    for (int k = 0; k < 4; ++k) {
-      const float f = exp2_fast(part_ml[k].x - (top == -INFINITY ? 0.0f : top));
-      l += part_ml[k].y * f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(f, part[k][E * lane + e], x[e]);
-    }
+    for (int e = 0; e < E; ++e) x[e] = part[0][E * lane + e] + part[1][E * lane + e] + part[2][E * lane + e] + part[3][E * lane + e];
   }
   const float inv = l == 0.0f ? 0.0f : (fp8 ? a.v_scale[h] : 1.0f) / l;
   uint16_t* dst = a.out + (size_t)s * a.ld_out + (size_t)head * D + E * lane;

@@ -20,8 +20,6 @@
 // a constant.
 #pragma once
 
-#include <type_traits>
-
 #include "mes_attn_common.h"
 
 namespace mes {
@@ -199,7 +197,8 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[NB][2], int key0, const 
     }
 }
 
-// Tiles [first, first + n) of this wavefront's rows, of the workgroup's [first, first + n_all) (n <= n_all).  low: the last key that the row
+// Tiles [first, first + n) of this wavefront's rows, of the workgroup's [first, first + n_all) (n <= n_all), keys up to stage.to; no row sees a key
+// behind the last tile.  low: the last key that the row
 // seeing least sees; last: see mask_scores.  Every wavefront of the workgroup makes the call; LDS is free before it.
 template <int D, int SRC>
 __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stage, int first, int n, int n_all, int low, const int (&last)[NB], float scale) {
@@ -294,71 +293,57 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
     if (t + 1 < end_all) stage.deposit(t + 1, 1);
   };
 
-  // Tile t, whose scores are in s; the scores of tile t + 1 go to sn, unless this wavefront does not take it (next = 0).
-  auto step = [&](auto next, f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
-    constexpr bool kNext = decltype(next)::value;
-    if (kNext) next_k(t + 1);
+  // Tile t, whose scores are in s; the scores of tile t + 1 go to sn.  Where there is none its scores are of what LDS holds, and all
+  // masked: a step of its own for the last tile is more code, and code is fetched when it is first run.
+  auto step = [&](f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
+    next_k(t + 1);
     if (t > first) next_v(t);
     u32x4 p[NB][4];
     constexpr int kAhead = SRC == KV_PAGED_E4M3 ? 2 : 3;            // operands on their way; codes of the 8-bit cache need the registers
     bf16x8 ring[kAhead + 1];
-    if constexpr (kNext) {
 #pragma unroll
-      for (int g = 0; g < kAhead; ++g) ring[g] = k_operand(g);
-    } else {
-#pragma unroll
-      for (int g = 0; g < kAhead; ++g) ring[g] = v_operand(g);
-    }
+    for (int g = 0; g < kAhead; ++g) ring[g] = k_operand(g);
 #pragma unroll
     for (int g = 0; g < kGroups1; ++g) {
-      if constexpr (kNext) {
-        ring[(g + kAhead) % (kAhead + 1)] = g + kAhead < kGroups1 ? k_operand(g + kAhead) : v_operand(g + kAhead - kGroups1);
-        const f32x16 zero = {};
+      ring[(g + kAhead) % (kAhead + 1)] = g + kAhead < kGroups1 ? k_operand(g + kAhead) : v_operand(g + kAhead - kGroups1);
+      const f32x16 zero = {};
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-          sn[b][g % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[g % (kAhead + 1)], w.q[b][g / 2], g < 2 ? zero : sn[b][g % 2], 0, 0, 0);
-      }
+      for (int b = 0; b < NB; ++b)
+        sn[b][g % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[g % (kAhead + 1)], w.q[b][g / 2], g < 2 ? zero : sn[b][g % 2], 0, 0, 0);
 #pragma unroll
       for (int x = 0; x < kPairs; ++x) {
         const int i = (g * kPairs + x) % 4, b = (g * kPairs + x) / 4 % NB, st = (g * kPairs + x) / (4 * NB), e = 8 * (st % 2) + 2 * i;
         p[b][st][i] = pack2(exp2_fast(s[b][st / 2][e] * scale - from[b]), exp2_fast(s[b][st / 2][e + 1] * scale - from[b]));
         w.l[b] = add_pair(p[b][st][i], w.l[b]);                     // the sum of what is multiplied with V
       }
-      if constexpr (kNext) __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (kNext) {
-      // the weights are needed behind the branches only, and would be formed there, with no products beside them
+    // the weights are needed behind the branches only, and would be formed there, with no products beside them
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int st = 0; st < 4; ++st) asm volatile("" : "+v"(p[b][st]));
-    }
+      for (int st = 0; st < 4; ++st) asm volatile("" : "+v"(p[b][st]));
     between(t);
-    if constexpr (kNext) {
-      const int there = stage.there(t + 1);
-      if (partial(t + 1, there)) mask_scores(sn, (t + 1) * kTile, last, stage.from, stage.to, there);
-    }
+    const int there = stage.there(t + 1);
+    if (partial(t + 1, there)) mask_scores(sn, (t + 1) * kTile, last, stage.from, stage.to, there);
     float top[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) top[b] = -INFINITY;
-    constexpr int kFirst = kNext ? kGroups1 : 0;                    // place of group 0's operand in the ring
 #pragma unroll
     for (int g = 0; g < kGroups2; ++g) {
-      if (g + kAhead < kGroups2) ring[(kFirst + g + kAhead) % (kAhead + 1)] = v_operand(g + kAhead);
+      if (g + kAhead < kGroups2) ring[(kGroups1 + g + kAhead) % (kAhead + 1)] = v_operand(g + kAhead);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        w.acc[b][g % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(kFirst + g) % (kAhead + 1)], __builtin_bit_cast(bf16x8, p[b][g / DT]), w.acc[b][g % DT], 0, 0, 0);
-      if constexpr (kNext) {
-        constexpr int kEach = 32 * NB / kGroups2;                        // maxima per group
+        w.acc[b][g % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[(kGroups1 + g) % (kAhead + 1)], __builtin_bit_cast(bf16x8, p[b][g / DT]), w.acc[b][g % DT], 0, 0, 0);
+      constexpr int kEach = 32 * NB / kGroups2;                     // maxima per group
 #pragma unroll
-        for (int x = 0; x < kEach; ++x) {
-          const int e = g * kEach + x;
-          top[e / 32] = fmaxf(top[e / 32], sn[e / 32][e / 16 % 2][e % 16]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+      for (int x = 0; x < kEach; ++x) {
+        const int e = g * kEach + x;
+        top[e / 32] = fmaxf(top[e / 32], sn[e / 32][e / 16 % 2][e % 16]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (kNext) raise(top);
+    raise(top);
   };
 
   stage.begin(first);
@@ -395,26 +380,18 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
         for (int i = 0; i < 16; ++i) top[b] = fmaxf(top[b], s0[b][tt][i]);
     raise(top);
   }
-  auto turn = [&](auto next, f32x16 (&s)[NB][2], f32x16 (&sn)[NB][2], int t) {
-    before(t);
-    step(next, s, sn, t);
-    after(t);
-  };
-  constexpr std::true_type more;
-  constexpr std::false_type none;
   int t = first;
-  if (n > 0) {
-    for (; t + 2 < end; t += 2) {                                    // one way out of the loop: with two, the compiler keeps two sets of accumulators
-      turn(more, s0, s1, t);
-      turn(more, s1, s0, t + 1);
-    }
+  for (; t < end; t += 2) {                                          // one way out of the loop: with two, the compiler keeps two sets of accumulators
+    before(t);
+    step(s0, s1, t);
+    after(t);
     if (t + 1 < end) {
-      turn(more, s0, s1, t++);
-      turn(none, s1, s0, t++);
-    } else {
-      turn(none, s0, s1, t++);
+      before(t + 1);
+      step(s1, s0, t + 1);
+      after(t + 1);
     }
   }
+  t = end;
   for (; t < end_all; ++t) {                                         // other wavefronts' tiles
     before(t);
     between(t);
