@@ -132,13 +132,16 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(CopyArgs a) {
   const size_t at = (size_t)part * kCopyBytes + threadIdx.x * 16;
   const char* from = base + a.src[pair] * a.page_bytes;
   char* to = base + a.dst[pair] * a.page_bytes;
+  constexpr int kStep = kCopyThreads * 16;
   uint4 w[kCopyWords];
+  if ((size_t)(part + 1) * kCopyBytes <= a.page_bytes) {
 #pragma unroll
-  for (int i = 0; i < kCopyWords; ++i)
-    if (at + i * kCopyThreads * 16 < a.page_bytes) w[i] = *reinterpret_cast<const uint4*>(from + at + i * kCopyThreads * 16);
+    for (int i = 0; i < kCopyWords; ++i) w[i] = *reinterpret_cast<const uint4*>(from + at + i * kStep);
 #pragma unroll
-  for (int i = 0; i < kCopyWords; ++i)
-    if (at + i * kCopyThreads * 16 < a.page_bytes) *reinterpret_cast<uint4*>(to + at + i * kCopyThreads * 16) = w[i];
+    for (int i = 0; i < kCopyWords; ++i) *reinterpret_cast<uint4*>(to + at + i * kStep) = w[i];
+  } else {
+    for (size_t x = at; x < a.page_bytes; x += kStep) *reinterpret_cast<uint4*>(to + x) = *reinterpret_cast<const uint4*>(from + x);
+  }
 }
 
 }  // namespace
