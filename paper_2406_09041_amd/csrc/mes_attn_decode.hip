@@ -30,9 +30,6 @@ constexpr int kWorkgroups = 512, kWorkgroupsFew = 768;
 constexpr int kWholeTokens = 512;
 static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
 
-// tokens of a unit of a shared prefix: tiles of many rows take about as long as twice as many tokens of few rows
-__device__ __forceinline__ int prefix_unit(int sequences, int per_pass, int group) { return kUnit; }
-
 struct Shape {                       // what host and device derive alike
   int group, per_pass, n_passes;     // query heads per key / value head, sequences per pass, passes of all groups
 };
@@ -407,8 +404,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
         if (length(s) >= prefix) sh.cum[n_groups + s] = units(prefix, length(s));
     if (lane == 0) {
       sh.group_src[g] = active ? src : -1;
-      const int unit = prefix_unit(behind - first, c.sh.per_pass, c.sh.group);
-      sh.cum[g] = active ? (prefix + unit - 1) / unit * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
+      sh.cum[g] = active ? (prefix + kUnit - 1) / kUnit * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
     }
   }
   __syncthreads();
@@ -459,8 +455,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     g.kvh = h;
     p.direct = false;
     if (it < n_groups) {
-      const int unit = prefix_unit(a.behind[it] - a.first[it], c.sh.per_pass, c.sh.group);
-      const int tiles = (a.prefix[it] + unit - 1) / unit, pass = from_unit / tiles;
+      const int tiles = (a.prefix[it] + kUnit - 1) / kUnit, pass = from_unit / tiles;
       from_unit -= pass * tiles;
       to_unit = min(to_unit - pass * tiles, tiles);
       g.seq = uniform(sh.group_src[it]);
@@ -468,8 +463,8 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
       g.rows = min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group;
       g.from = 0;
       g.to = a.prefix[it];
-      g.t0 = from_unit * unit;
-      g.t1 = min(to_unit * unit, g.to);
+      g.t0 = from_unit * kUnit;
+      g.t1 = min(to_unit * kUnit, g.to);
       const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
       p.o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
       p.ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
@@ -495,7 +490,6 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     p.units = uniform(to_unit - from_unit);
     return p;
   };
-  if (begin >= end) return;
   // first the pieces of many rows, then the others: in one loop both bodies would keep registers for each other
   if constexpr (MANY) {
     for (int u = begin; u < end;) {
@@ -532,7 +526,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     for (int g = 0; g < n_groups; ++g) {
       if (s < a.first[g] || s >= a.behind[g]) continue;
       if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
-        const int unit = prefix_unit(a.behind[g] - a.first[g], c.sh.per_pass, c.sh.group), n = (a.prefix[g] + unit - 1) / unit, pass = (s - a.first[g]) / c.sh.per_pass;
+        const int n = (a.prefix[g] + kUnit - 1) / kUnit, pass = (s - a.first[g]) / c.sh.per_pass;
         const int u0 = h * per_head + sh.cum[g] + pass * n, w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
         w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
         w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
