@@ -312,8 +312,9 @@ mes_status mes_step_adamw(float* step, const float* grad, float* m, float* v, in
  * n_heads and its key / value head g = h / (n_heads / n_kv_heads), for the token at position p of its sequence
  *     out[h] = sum_{j <= p} softmax_j(scale * <q[h], k_j[g]>) v_j[g]                    (causal; scale usually head_dim^-1/2)
  * Queries, fresh keys / values and outputs are bf16 [T][heads][head_dim], head_dim contiguous, heads head_dim apart,
- * rows ld_* elements apart (ld_* >= heads * head_dim, a multiple of 8: views of one fused q/k/v buffer are fine), 16-byte
- * aligned.  head_dim is 64 or 128; n_heads is a multiple of n_kv_heads, at most 64 times as many.
+ * rows ld_* elements apart (heads * head_dim <= ld_* <= 2^26, a multiple of 8: views of one fused q/k/v buffer are fine), 16-byte
+ * aligned; outputs overlap no input where nothing else is said.  Calls take up to 2^24 - 1 rows (decoding: sequences times
+ * heads), page tables up to 2^30 tokens.  head_dim is 64 or 128; n_heads is a multiple of n_kv_heads, at most 64 times as many.
  * Numerics: scores, softmax statistics and sums are fp32; the softmax weights are rounded to bf16 for the product with
  * V, the output is rounded once.  A row that sees no token is 0.  Tokens that a row does not see do not touch it, whatever
  * their keys and values hold (infinities and NaN included).

@@ -296,10 +296,19 @@ static mes_status check_heads(const char* who, int n_heads, int n_kv_heads, int 
   return MES_OK;
 }
 
+// What indexes of 32 bits hold on the device: rows of a call (a launch has up to 2^32 threads), their distance, tokens of a page table
+constexpr int kMaxRows = 0xffffff, kMaxStride = 1 << 26, kMaxTokens = 1 << 30;
+
+static mes_status check_row_count(const char* who, int T) {
+  if (T < 0 || T > kMaxRows) return fail(MES_ERR_SHAPE, "%s: T = %d outside [0, %d]", who, T, kMaxRows);
+  return MES_OK;
+}
+
 static mes_status check_rows(const char* who, const char* what, const void* p, int ld, int heads, int head_dim) {
   if (!p) return fail(MES_ERR_NULL, "%s: %s is null", who, what);
   if (!aligned16(p)) return fail(MES_ERR_ALIGN, "%s: %s must be 16-byte aligned", who, what);
-  if (ld < (int64_t)heads * head_dim || ld % 8 != 0) return fail(MES_ERR_SHAPE, "%s: rows of %s are %d apart: a multiple of 8, %d or more", who, what, ld, heads * head_dim);
+  if (ld < (int64_t)heads * head_dim || ld % 8 != 0 || ld > kMaxStride)
+    return fail(MES_ERR_SHAPE, "%s: rows of %s are %d apart: a multiple of 8 in [%d, %d]", who, what, ld, heads * head_dim, kMaxStride);
   return MES_OK;
 }
 
@@ -322,8 +331,8 @@ static mes_status check_seqs(const char* who, const mes_kv* kv, const mes_seqs* 
   if (s->n_seqs < 0 || s->n_seqs > MES_MAX_SEQS) return fail(MES_ERR_SHAPE, "%s: n_seqs = %d outside [0, %d]", who, s->n_seqs, MES_MAX_SEQS);
   if (s->n_seqs == 0) return MES_OK;
   if (!s->kv_len || !s->page_table || (offsets && !s->q_offsets)) return fail(MES_ERR_NULL, "%s: a pointer in seqs is null", who);
-  if (s->table_pages < 1 || (int64_t)s->table_pages * kv->page_tokens > 0x7fffff00)
-    return fail(MES_ERR_SHAPE, "%s: table_pages = %d of %d tokens", who, s->table_pages, kv->page_tokens);
+  if (s->table_pages < 1 || (int64_t)s->table_pages * kv->page_tokens > kMaxTokens)
+    return fail(MES_ERR_SHAPE, "%s: table_pages = %d of %d tokens: 1 to %d tokens", who, s->table_pages, kv->page_tokens, kMaxTokens);
   return MES_OK;
 }
 
@@ -338,7 +347,7 @@ mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, cons
   static const char who[] = "mes_kv_append";
   if (mes_status st = check_kv(who, kv, layer)) return st;
   if (mes_status st = check_seqs(who, kv, seqs, false)) return st;
-  if (T < 0) return fail(MES_ERR_SHAPE, "%s: T = %d is negative", who, T);
+  if (mes_status st = check_row_count(who, T)) return st;
   if (!seqs->q_offsets && T > seqs->n_seqs) return fail(MES_ERR_SEGMENTS, "%s: %d rows of %d sequences without q_offsets", who, T, seqs->n_seqs);
   if (T == 0 || seqs->n_seqs == 0) return MES_OK;
   if ((q == nullptr) != (q_out == nullptr)) return fail(MES_ERR_NULL, "%s: give both of q and q_out or neither", who);
@@ -383,7 +392,7 @@ mes_status mes_attn_prompt(const void* q, const void* k, const void* v, int T, i
   static const char who[] = "mes_attn_prompt";
   if (mes_status st = check_heads(who, n_heads, n_kv_heads, head_dim)) return st;
   if (n_seqs < 0 || n_seqs > MES_MAX_SEQS) return fail(MES_ERR_SHAPE, "%s: n_seqs = %d outside [0, %d]", who, n_seqs, MES_MAX_SEQS);
-  if (T < 0) return fail(MES_ERR_SHAPE, "%s: T = %d is negative", who, T);
+  if (mes_status st = check_row_count(who, T)) return st;
   if (!(scale > 0.0f) || scale > 1e30f) return fail(MES_ERR_SHAPE, "%s: scale must be positive and finite", who);
   if (T == 0 || n_seqs == 0) return MES_OK;
   if (!seq_offsets) return fail(MES_ERR_NULL, "%s: seq_offsets is null", who);
@@ -407,7 +416,7 @@ mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, co
   if (mes_status st = check_kv(who, kv, layer)) return st;
   if (mes_status st = check_seqs(who, kv, seqs, true)) return st;
   if (mes_status st = check_heads(who, n_heads, kv->n_kv_heads, kv->head_dim)) return st;
-  if (T < 0) return fail(MES_ERR_SHAPE, "%s: T = %d is negative", who, T);
+  if (mes_status st = check_row_count(who, T)) return st;
   if (!(scale > 0.0f) || scale > 1e30f) return fail(MES_ERR_SHAPE, "%s: scale must be positive and finite", who);
   if (T == 0 || seqs->n_seqs == 0) return MES_OK;
   if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, kv->head_dim)) return st;
@@ -465,6 +474,8 @@ mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, co
       a.prefix[a.n_groups++] = prefix_len[e];
     }
   }
+  if ((int64_t)seqs->n_seqs * n_heads > kMaxRows)
+    return fail(MES_ERR_SHAPE, "%s: %d sequences of %d heads are more than one call takes", who, seqs->n_seqs, n_heads);
   // units of work are numbered in 32 bits (an expert's shared prefix has at most two passes per sequence)
   if ((int64_t)3 * seqs->n_seqs * kv->n_kv_heads * (seqs->table_pages * kv->page_tokens / 128 + 2) > 0x40000000)
     return fail(MES_ERR_SHAPE, "%s: %d page tables of %d pages are more than one call takes", who, seqs->n_seqs, seqs->table_pages);

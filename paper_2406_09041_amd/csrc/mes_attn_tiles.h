@@ -1,17 +1,21 @@
 // Many query rows against keys and values that a workgroup shares in LDS: the loop of the prompt kernel, and of the decode
 // kernel where many rows read the same tokens.
 //
-// A wavefront takes 64 query rows as two blocks of 32, a workgroup 4 wavefronts; keys come 64 at a time.  Scores are formed
-// transposed, S^T = K Q^T: in the result of v_mfma_f32_32x32x16_bf16 a lane holds ONE query row of the block (lane & 31) and 16 of
-// 32 keys, so that maxima, sums and rescaling need no exchange but one with lane ^ 32, and its registers, rounded to bf16, ARE
-// the operand P^T of the second product O^T = V^T P^T: keys 4 h + (0..3) and 8 + 4 h + (0..3) of every 16 for half h of the
-// wavefront.  V's operand for these keys is read from LDS with the transposing read (ds_read_b64_tr_b16), in P's order of keys.
+// A workgroup is 4 wavefronts of 32 query rows; keys come 64 at a time.  Scores are formed transposed, S^T = K Q^T: in the
+// result of v_mfma_f32_32x32x16_bf16 a lane holds ONE query row (lane & 31) and 16 of 32 keys, so that maxima, sums and rescaling
+// need no exchange but one with lane ^ 32, and its registers, rounded to bf16, ARE the operand P^T of the second product
+// O^T = V^T P^T: keys 4 h + (0..3) and 8 + 4 h + (0..3) of every 16 for half h of the wavefront.  V's operand for these keys is read
+// from LDS with the transposing read (ds_read_b64_tr_b16), in P's order of keys.
 //
-// Why 64 rows: an operand of K or V read from LDS serves two products.  With 32 rows per wavefront (two wavefronts per SIMD) the
-// LDS pipe is busy as long as the matrix cores.  The price is one wavefront per SIMD (up to 512 registers), which has to keep
-// matrix cores and vector units busy by itself: while the scores of tile t + 1 are multiplied, the exponentials of tile t are
-// formed between the products, and while tile t is multiplied with V, the maxima of tile t + 1.  The groups of one or two
-// operand reads, two products and the vector work that goes with them are kept in this order by scheduling barriers.
+// Matrix cores and vector units are kept busy together: while the scores of tile t + 1 are multiplied, the exponentials of tile t are
+// formed between the products, and while tile t is multiplied with V, the maxima of tile t + 1.  The groups of an operand read, a
+// product and the vector work that goes with them are kept in this order by scheduling barriers; operands are read three groups ahead.
+//
+// Why 32 rows and two wavefronts per SIMD: with 64 rows an operand read from LDS serves two products, but one wavefront per
+// SIMD with all 512 registers stood still at every barrier and every rescaling; two of 32 rows fill each other's gaps.  Measured at head_dim
+// 128: 40 heads of prompts of 1 to 6001 rows 420 us, 935 TFLOP/s of the 1268 that a bf16 library product of 8192^3 reaches on the same
+// card; one prompt of 8192 rows 950 to 970.  What bounds it: the exponentials and sums take about as many issue slots as the
+// products take matrix cycles, and what the scheduler cannot lay beside each other is lost.
 //
 // LDS: rows of head_dim, two tiles of keys and two of values in turn.  A copy of a wavefront writes 1 KiB in the order of its lanes: a
 // block of 4 (8) rows, whose 16-byte pieces are XORed with turn(row) by fetching them in that order, and blocks are 16 bytes further
@@ -160,7 +164,7 @@ struct Stage {
 template <int D>
 struct TileRows {
   static constexpr int KS = D / 16, DT = D / 32;
-  bf16x8 q[NB][KS];               // Q^T operands: lane (col, half) holds dimensions 16 ks + 8 half + (0..7) of row col of the block
+  bf16x8 q[NB][KS];               // NB = 1 block of 32 rows; Q^T operands: lane (col, half) holds dimensions 16 ks + 8 half + (0..7) of row col of the block
   f32x16 acc[NB][DT];             // O^T: lane holds its row, dimensions 32 dt + 8 (i / 4) + 4 half + i % 4
   float m[NB], l[NB];              // running maximum (in powers of two); sum over this half's keys
 };

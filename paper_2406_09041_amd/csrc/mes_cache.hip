@@ -53,6 +53,8 @@ __device__ inline void load8(const uint16_t* p, float v[8]) {
   }
 }
 
+// Four prompts of 1024 tokens (32 query, 8 key / value heads of 128, bf16): 101 MB in 19 us, 5.3 TB/s; 256 single tokens 6 MB, as long as a launch.
+//
 // One workgroup per row.  A unit of work is 8 dimensions of the first half of a head and the 8 they turn with, so that q_out
 // may be q: one thread reads both halves before it writes them.
 template <bool FP8>
@@ -70,7 +72,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
     if (s >= a.n_seqs || a.q_offsets[s] > t) return;       // behind the last sequence
     behind = a.q_offsets[s + 1] - t;
   }
-  const int pos = a.kv_len[s] - behind;
+  const int pos = max(a.kv_len[s], 0) - behind;
   if (pos < 0 || pos >= a.capacity) return;
   const int page = a.page_table[(size_t)s * a.table_pages + (pos >> a.page_shift)];
   const bool placed = (unsigned)page < (unsigned)a.n_pages;
@@ -116,7 +118,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
 }
 
 // Pages are whole 16-byte words one behind the other; a workgroup copies up to kCopyBytes of one page of one layer of keys or
-// values, every load in flight before the first store.
+// values, every load in flight before the first store: 400 pages of 32 KiB in 32 layers of keys and values 361 us, 4.65 TB/s (4.84 is what a
+// copy of 2 GiB reaches; a loop of one load and one store: 477 us).
 constexpr int kCopyThreads = 256, kCopyWords = 8, kCopyBytes = kCopyThreads * kCopyWords * 16;
 
 struct CopyArgs {
@@ -160,10 +163,11 @@ hipError_t launch_copy_pages(const mes_kv& kv, const int32_t* src, const int32_t
   a.layer_bytes = a.page_bytes * kv.n_pages;
   a.n_layers = kv.n_layers;
   a.parts = (int)((a.page_bytes + kCopyBytes - 1) / kCopyBytes);
-  // a launch's grid stays within 2^31 workgroups
+  // a launch has up to 2^32 threads
+  constexpr size_t kMostGrid = 0xffffffffu / kCopyThreads;
   const size_t per_pair = (size_t)a.parts * a.n_layers;
-  if (per_pair > 0x7fffffffu) return hipErrorInvalidValue;
-  const int most = (int)std::min<size_t>(kCopyPairs, 0x7fffffffu / per_pair);
+  if (per_pair > kMostGrid) return hipErrorInvalidValue;
+  const int most = (int)std::min<size_t>(kCopyPairs, kMostGrid / per_pair);
   for (int i = 0; i < n; i += most) {
     const int m = std::min(most, n - i);
     for (int j = 0; j < m; ++j) {

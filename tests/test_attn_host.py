@@ -240,3 +240,14 @@ def test_bookkeeping_errors():
     assert lib.mes_pages_compact(pool.handle, None, one, ctypes.byref(n)) == 1
     assert lib.mes_pages_table(pool.handle, one, 1, None, 3, None) == 1
     assert lib.mes_pages_length(None, 0) == -1 and pool.length(7) == -1 and lib.mes_pages_unused(None) == -1
+
+
+def test_sizes_that_do_not_fit_the_device_indexes():
+    for call in (_append, _extend, _decode):
+        assert call(seqs=_seqs(table_pages=(1 << 26) + 1)) == 2               # 16-token pages: 2^30 tokens and a page
+        assert call(ld_q=(1 << 26) + 8) == 2
+    assert _append(T=1 << 24) == 2 and _extend(T=1 << 24) == 2 and _prompt(T=1 << 24) == 2
+    assert _prompt(ld_k=(1 << 26) + 8) == 2 and _prompt(ld_v=(1 << 26) + 8) == 2 and _prompt(ld_o=(1 << 26) + 8) == 2
+    kv, wide = _kv(n_kv_heads=1024), 1024 * 32 * 64
+    assert _decode(kv=kv, seqs=_seqs(n_seqs=513), heads=1024 * 32, ld_q=wide, ld_o=wide, seg=None, pre=None, wsb=1 << 62) == 2   # 513 * 32768 rows
+    assert b"heads" in lib.mes_last_error()

@@ -321,3 +321,29 @@ def test_a_cache_whose_offsets_pass_32_bits(e4m3):
             want, tol = O.attend(q[[a + r for r in rows]], stored[0][a:b], stored[1][a:b], rows, dim ** -0.5)
             _check(out[[a + r for r in rows]], want, tol, f"sequence {s}, move {move}")
             _check(one_each[s:s + 1], want[-1:], tol[-1:], f"decoded, sequence {s}, move {move}")
+
+
+@pytest.mark.parametrize("n_seqs", [2, 70])
+def test_extend_with_the_largest_lengths(n_seqs):
+    """A length far past the table's room: every row sees all tokens of the table; the lowest one: none."""
+    heads, kvh, dim, page = 4, 2, 64, 16
+    g = torch.Generator().manual_seed(n_seqs)
+    cache = mes.KvCache(1, 50, page, kvh, dim)
+    for t in (cache.k, cache.v):
+        t.copy_(torch.randn(t.shape, generator=g).to(torch.bfloat16))
+    table = torch.randint(0, 50, (n_seqs, 20), generator=g, dtype=torch.int32)
+    length = torch.full((n_seqs,), 2 ** 31 - 1, dtype=torch.int32)
+    length[-1] = -2 ** 31
+    q = torch.randn(3 * n_seqs, heads, dim, generator=g).to(torch.bfloat16).to(DEV)
+    off = _ints([3 * s for s in range(n_seqs + 1)])
+    batch = mes.SeqBatch(length.to(DEV), table.to(DEV), off)
+    before = cache.k.clone()
+    mes.mes_kv_append(cache, 0, batch, None, q[:, :kvh], q[:, kvh:], None)        # no row has a place
+    assert torch.equal(cache.k.view(torch.int16), before.view(torch.int16))
+    for ws in (None, mes.binding.prompt_workspace(3 * n_seqs, n_seqs, heads, kvh, dim, DEV)):
+        out = mes.mes_attn_extend(cache, 0, batch, q, workspace=ws)
+        assert not out[-3:].any()
+        for s in (0, n_seqs - 2):
+            k, v = (torch.cat([x[0, p].transpose(0, 1) for p in table[s].tolist()]) for x in (cache.k.cpu(), cache.v.cpu()))
+            want, tol = O.attend(q[3 * s:3 * s + 3], k, v, [319] * 3, dim ** -0.5)
+            _check(out[3 * s:3 * s + 3], want, tol, f"sequence {s}")
