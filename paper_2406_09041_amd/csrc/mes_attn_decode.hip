@@ -22,8 +22,8 @@
 //
 // Measured (head_dim 128, 32 heads over 8 key / value heads): 256 sequences of 0 to 8192 tokens 165 us, 4.9 TB/s of the 5.96 that a
 // pass that only reads reaches; 64 sequences of 512 tokens 23 us (5.9 TB/s); 64 of 16 experts with prompts of 512 to 1600 tokens 43 us, 106
-// MB; 96 behind 8200 shared tokens of an e4m3 cache 62 us, where 10 us are products and the rest short own pieces, 4 to 5 us each beside
-// registers that the larger body keeps in scratch (19 to 24 of them at head_dim 128 and e4m3); one sequence of 200 tokens 9.2 us.
+// MB; 96 behind 8200 shared tokens of an e4m3 cache 59 us, of which 10 us are products at the library's rate (own pieces cost 4 to 5 us each beside the
+// larger body, but a launch of their own for them made it 68 and the 64 sequences 51); one sequence of 200 tokens 9.2 us.
 #include "mes_attn_tiles.h"
 
 namespace mes {
@@ -417,6 +417,17 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     }
   }
   __syncthreads();
+  // lane g: the sequences and the prefix of group g, if it shares
+  int my_first = 0, my_behind = 0, my_prefix = 0;
+  if (lane < n_groups && sh.group_src[lane] >= 0) {
+    my_first = a.first[lane];
+    my_behind = a.behind[lane];
+    my_prefix = a.prefix[lane];
+  }
+  auto shared_by = [&](int s, int len) {            // the prefix that a sequence (the same in all lanes) shares with others
+    const uint64_t who = __ballot(my_first <= s && s < my_behind && len >= my_prefix);
+    return who ? __builtin_amdgcn_readlane(my_prefix, __builtin_ctzll(who)) : 0;
+  };
   // ---- exclusive sums, in place
   {
     const int per = (n_items + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * per, n_items), hi = min(lo + per, n_items);
@@ -482,10 +493,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
       g.seq = g.seq0 = s;
       g.rows = c.sh.group;
       g.to = uniform(length(s));
-      g.from = 0;
-      for (int k = 0; k < n_groups; ++k)
-        if (s >= a.first[k] && s < a.behind[k] && sh.group_src[k] >= 0 && g.to >= a.prefix[k]) g.from = a.prefix[k];
-      g.from = uniform(g.from);
+      g.from = shared_by(s, g.to);
       const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
       p.direct = g.from == 0 && from_unit == 0 && to_unit == n;
       p.o = reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D;
