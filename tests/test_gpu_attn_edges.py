@@ -1,0 +1,124 @@
+"""Attention calls where values or scales are out of the ordinary: scales of the caller's own, values that are not finite behind rows that do
+not see them.  References and tolerances: oracle/attn_oracle.py."""
+import pytest
+import torch
+
+import paper_2406_09041_amd as mes
+from oracle import attn_oracle as O
+from test_gpu_attn import DEV, INF, NAN, Paged, _check, _ints, _rows
+
+pytestmark = pytest.mark.gpu
+
+
+def _offsets(counts):
+    off = [0]
+    for n in counts:
+        off.append(off[-1] + n)
+    return off
+
+
+# ------------------------------------------------------------------------------------------------- a scale of the caller's
+
+@pytest.mark.parametrize("scale", [0.004, 0.31, 3.0])
+def test_scales_of_the_callers_own(scale):
+    g = torch.Generator().manual_seed(12)
+    heads, kvh, dim, lens = 4, 2, 64, [150, 33]
+    q, k, v = _rows(g, 183, heads, dim), _rows(g, 183, kvh, dim), _rows(g, 183, kvh, dim)
+    out = mes.mes_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), _ints([0, 150, 183]), scale=scale)
+    for a, b in ((0, 150), (150, 183)):
+        want, tol = O.attend(q[a:b], k[a:b], v[a:b], range(b - a), scale)
+        _check(out[a:b], want, tol, f"prompt {a}..{b}")
+    for e4m3 in (False, True):
+        c = Paged(13, lens, kvh, dim, 16, e4m3)
+        out = mes.mes_attn_extend(c.cache, c.layer, c.batch([0, 20, 22]), q[:22].to(DEV), scale=scale)
+        each = mes.AttnDecode(c.cache, heads, 2)(c.layer, c.batch(), q[20:22].to(DEV), scale=scale)
+        for s, (a, b) in enumerate(((0, 20), (20, 22))):
+            want, tol = O.attend(q[a:b], c.k[s], c.v[s], range(lens[s] - (b - a), lens[s]), scale)
+            _check(out[a:b], want, tol, f"extend, sequence {s}")
+            want, tol = O.attend(q[20 + s:21 + s], c.k[s], c.v[s], [lens[s] - 1], scale)
+            _check(each[s:s + 1], want, tol, f"decode, sequence {s}")
+
+
+# --------------------------------------------------------------------------------------------- what is not finite, and not seen
+
+def _spoil(c, which, s, j, head, d, bad):
+    """Element d of token j of sequence s, in the cache only."""
+    x = c.cache.k if which == "k" else c.cache.v
+    if x.dtype == torch.float8_e4m3fn:
+        x, bad = x.view(torch.uint8), 0x7f                                 # the type's NaN: it has no infinities
+    x[c.layer, c.table[s][j // c.page], head, j % c.page, d] = bad
+
+
+def _check_around(out, q, k, v, positions, scale, d, what):
+    """Rows that see a value that is not finite in dimension d of v (a number in the reference): that dimension alone has it."""
+    out = out.cpu()
+    assert not torch.isfinite(out[:, :, d]).any(), what
+    keep = [x for x in range(out.shape[2]) if x != d]
+    want, tol = O.attend(q, k, v, positions, scale)
+    _check(out[:, :, keep], want[:, :, keep], tol[:, :, keep], what)
+
+
+@pytest.mark.parametrize("e4m3,bad", [(False, NAN), (False, INF), (False, -INF), (True, NAN)])
+@pytest.mark.parametrize("heads,kvh,dim,page", [(2, 2, 128, 16), (4, 2, 64, 32), (4, 1, 128, 64), (8, 2, 64, 16)])
+def test_extend_rows_are_not_touched_by_what_they_do_not_see(heads, kvh, dim, page, e4m3, bad):
+    """A value that is not finite in a new token: earlier rows of the same tile, other heads and other sequences as without it; a page
+    is missing before it."""
+    lens, news, at = [260, 150], [130, 140], 200
+    c = Paged(31, lens, kvh, dim, page, e4m3)
+    table = [list(r) for r in c.table]
+    table[0][64 // page] = -1
+    gone = range(64 // page * page, 64 // page * page + page)
+    off = _offsets(news)
+    q = _rows(torch.Generator().manual_seed(32), off[-1], heads, dim)
+    there = [j for j in range(lens[0]) if j not in gone]
+    k0, v0 = c.k[0][there], c.v[0][there]
+    group, scale, skip = heads // kvh, dim ** -0.5, lens[0] - len(there)
+    for which in ("k", "v"):
+        c = Paged(31, lens, kvh, dim, page, e4m3)
+        _spoil(c, which, 0, at, 0, 5, bad)
+        out = mes.mes_attn_extend(c.cache, c.layer, c.batch(off, None, table), q.to(DEV))
+        first = at - (lens[0] - news[0])                                   # the first row that sees it
+        want, tol = O.attend(q[:first], k0, v0, [130 + i - skip for i in range(first)], scale)
+        _check(out[:first], want, tol, f"rows before it, {which}")
+        want, tol = O.attend(q[130:], c.k[1], c.v[1], range(10, 150), scale)
+        _check(out[130:], want, tol, f"the other sequence, {which}")
+        rows = list(range(first, 130, 9))
+        after = [130 + i - skip for i in rows]
+        if kvh > 1:
+            want, tol = O.attend(q[rows, group:], k0[:, 1:], v0[:, 1:], after, scale)
+            _check(out[rows, group:], want, tol, f"other heads, {which}")
+        if which == "v":
+            _check_around(out[rows, :group], q[rows, :group], k0[:, :1], v0[:, :1], after, scale, 5, "rows that see it")
+        elif bad != bad:
+            assert torch.isnan(out[first:130, :group]).all()
+
+
+@pytest.mark.parametrize("e4m3,bad", [(False, NAN), (False, INF), (True, NAN)])
+@pytest.mark.parametrize("heads,dim", [(1, 128), (2, 64), (4, 128), (12, 64)])
+def test_extend_with_keys_shared_out_and_a_value_that_is_not_finite(heads, dim, e4m3, bad):
+    lens, news, at = [3000], [100], 2950
+    c = Paged(33, lens, 1, dim, 16, e4m3)
+    _spoil(c, "v", 0, at, 0, 5, bad)
+    q = _rows(torch.Generator().manual_seed(34), 100, heads, dim)
+    out = mes.mes_attn_extend(c.cache, c.layer, c.batch([0, 100]), q.to(DEV))
+    rows = [0, 1, 31, 32, 48, 49]
+    want, tol = O.attend(q[rows], c.k[0], c.v[0], [2900 + r for r in rows], dim ** -0.5)
+    _check(out[rows], want, tol, "rows before it")
+    rows = [50, 51, 63, 64, 99]
+    _check_around(out[rows], q[rows], c.k[0], c.v[0], [2900 + r for r in rows], dim ** -0.5, 5, "rows that see it")
+
+
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("heads,kvh,dim,T", [(2, 1, 128, 1700), (1, 1, 64, 2500), (4, 1, 128, 1100)])
+def test_prompt_with_keys_shared_out_and_a_value_that_is_not_finite(heads, kvh, dim, T, bad):
+    g = torch.Generator().manual_seed(35)
+    at = T - 200
+    q, k, v = _rows(g, T, heads, dim), _rows(g, T, kvh, dim), _rows(g, T, kvh, dim)
+    spoilt = v.clone()
+    spoilt[at, 0, 5] = bad
+    out = mes.mes_attn_prompt(q.to(DEV), k.to(DEV), spoilt.to(DEV), _ints([0, T]))
+    rows = [0, 63, 64, 700, at - 130, at - 1]
+    want, tol = O.attend(q[rows], k, v, rows, dim ** -0.5)
+    _check(out[rows], want, tol, "rows before it")
+    rows = [at, at + 1, at + 60, T - 1]
+    _check_around(out[rows], q[rows], k, v, rows, dim ** -0.5, 5, "rows that see it")
