@@ -321,7 +321,8 @@ mes_status mes_step_adamw(float* step, const float* grad, float* m, float* v, in
  *
  * The cache: k and v are [n_layers][n_pages][n_kv_heads][page_tokens][head_dim], page_tokens 16, 32, 64, 128 or 256, 16-byte
  * aligned.  MES_KV_BF16: bf16.  MES_KV_E4M3: 8-bit floating point (4 exponent, 3 mantissa bits, largest value 448), value =
- * code * scale with one fp32 scale per layer and head, k_scale and v_scale [n_layers][n_kv_heads] (NULL for bf16). */
+ * code * scale with one fp32 scale per layer and head, k_scale and v_scale [n_layers][n_kv_heads] (NULL for bf16): any finite
+ * numbers (the values of a head whose scale is 0 are 0). */
 enum { MES_KV_BF16 = 0, MES_KV_E4M3 = 1 };
 #define MES_MAX_SEQS 2048
 typedef struct {           /* HOST struct; pointers DEVICE, caller-owned */

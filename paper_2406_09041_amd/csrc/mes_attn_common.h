@@ -53,6 +53,23 @@ __device__ __forceinline__ u32x2 widen4(uint32_t w) {
   return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
+// The factor of scores that come from 8-bit codes holds the head's k_scale, which may have any sign.  Masked scores are -inf before it is
+// multiplied in, and maxima are taken before it, so it has to be above 0: its sign, or all of it where it is 0 or NaN, goes to
+// the query instead (exactly: bf16 times +-1, 0 or NaN).
+__device__ __forceinline__ float factor_of_scores(float f) { return f > 0.0f ? f : f < 0.0f ? -f : 1.0f; }
+template <class V, int N>
+__device__ __forceinline__ void factor_to_query(V (&q)[N], float f) {
+  if (f > 0.0f) return;
+  const float by = f < 0.0f ? -1.0f : f;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    u32x4 w = __builtin_bit_cast(u32x4, q[c]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) w[x] = pack2(bf16_at(w[x], 0) * by, bf16_at(w[x], 1) * by);
+    q[c] = __builtin_bit_cast(V, w);
+  }
+}
+
 // Over the lanes of a wavefront, without LDS.  scan: the sum up to and with the lane; max: of values that are not negative.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int from_below(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }

@@ -188,7 +188,8 @@ struct Few {
   // a step is then there before the loads of a whole chip are on their way, behind which it would be fetched (3 to 8 us).
   template <class SH>
   __device__ __forceinline__ void run(const Segment& g, bool fresh, bool ahead, const Segment& then, SH& sh, bool direct, float* o, float2* ml_out) {
-  const float scale = a.scale * kLog2e * (FP8 ? a.k_scale[g.kvh] : 1.0f);
+  const float factor = a.scale * kLog2e * (FP8 ? a.k_scale[g.kvh] : 1.0f), scale = FP8 ? factor_of_scores(factor) : factor;
+  if constexpr (FP8) factor_to_query(q, factor);
   f32x4 acc[VD];
   float m = -INFINITY, l = 0.0f;
 #pragma unroll
@@ -350,13 +351,15 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const S
   const uint16_t* src = a.q + (size_t)(g.seq0 + there / group) * a.ld_q + (size_t)(kvh * group + there % group) * D + 8 * half;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) w.q[0][ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
+  const float factor = a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f);
+  if constexpr (FP8) factor_to_query(w.q[0], factor);
   w.m[0] = -INFINITY;
   w.l[0] = 0.0f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) w.acc[0][dt] = f32x16{};
   const int last[NB] = {0x7fffffff}, first = g.t0 / kTile, n = (g.t1 - g.t0 + kTile - 1) / kTile;
   __syncthreads();                                  // the last piece's reads of LDS are over
-  attend_tiles<D, SRC>(w, stage, first, kWaveRows * wave < g.rows ? n : 0, n, 0x7fffffff, last, a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f));
+  attend_tiles<D, SRC>(w, stage, first, kWaveRows * wave < g.rows ? n : 0, n, 0x7fffffff, last, FP8 ? factor_of_scores(factor) : factor);
   const float l = w.l[0] + other_half(w.l[0]);
   if (row >= g.rows) return;
   if (direct) {

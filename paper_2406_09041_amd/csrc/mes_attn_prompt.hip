@@ -275,18 +275,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
     stage.n_pages = a.n_pages;
     stage.n_kv_heads = a.n_kv_heads;
   }
+  const float factor = a.scale * kLog2e * (SRC == KV_PAGED_E4M3 ? a.k_scale[kvh] : 1.0f), scale = SRC == KV_PAGED_E4M3 ? factor_of_scores(factor) : factor;
   TileRows<D> w;
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const uint16_t* src = a.q + (size_t)(it.row0 + min(wave_row + 32 * b + col, it.rows - 1)) * a.ld_q + (size_t)head * D + 8 * half;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) w.q[b][ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
+    if constexpr (SRC == KV_PAGED_E4M3) factor_to_query(w.q[b], factor);
     w.m[b] = -INFINITY;
     w.l[b] = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) w.acc[b][dt] = f32x16{};
   }
-  const float scale = a.scale * kLog2e * (SRC == KV_PAGED_E4M3 ? a.k_scale[kvh] : 1.0f);
   if (threadIdx.x == 0) lds_again = 0;
   if (n_all > 0) {
     attend_tiles<D, SRC>(w, stage, first, n, n_all, it.before + wave_row, last, scale);

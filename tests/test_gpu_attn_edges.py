@@ -1,5 +1,5 @@
-"""Attention calls where values or scales are out of the ordinary: scales of the caller's own, values that are not finite behind rows that do
-not see them.  References and tolerances: oracle/attn_oracle.py."""
+"""Attention calls where values or scales are out of the ordinary: scales of the caller's own, an 8-bit cache's scales of any sign, values
+that are not finite behind rows that do not see them.  References and tolerances: oracle/attn_oracle.py."""
 import pytest
 import torch
 
@@ -37,6 +37,56 @@ def test_scales_of_the_callers_own(scale):
             _check(out[a:b], want, tol, f"extend, sequence {s}")
             want, tol = O.attend(q[20 + s:21 + s], c.k[s], c.v[s], [lens[s] - 1], scale)
             _check(each[s:s + 1], want, tol, f"decode, sequence {s}")
+
+
+# ----------------------------------------------------------------------------------- an 8-bit cache's scales: any finite number
+
+def _rescaled(c, k_scale, v_scale):
+    """The same codes under other scales, one per key / value head."""
+    for x, old, new, there in ((c.k, c.scales[0], k_scale, c.cache.k_scale), (c.v, c.scales[1], v_scale, c.cache.v_scale)):
+        new = torch.tensor(new, dtype=torch.float32)
+        for s, n in enumerate(c.lens):
+            code = (x[s] / old[c.layer][:, None].double()).float().to(torch.float8_e4m3fn).double()
+            x[s] = code * new[:, None].double()
+        there[c.layer] = new.to(DEV)
+
+
+# scales of keys and of values (two heads), and of the scores: 0, negative, and a product that is 0 in fp32
+SCALES = [([0.0, -0.013], [0.02, -0.01], 0.125), ([-0.02, 0.015], [0.0, 0.02], 0.125), ([1e-30, -1e-30], [0.01, 0.02], 1e-20)]
+
+
+@pytest.mark.parametrize("k_scale,v_scale,scale", SCALES)
+@pytest.mark.parametrize("lens,news,heads,dim,page", [([300, 64, 17], [130, 64, 1], 4, 64, 16), ([129, 0, 77], [1, 0, 70], 2, 128, 64),
+                                                      ([3000], [70], 8, 128, 16)])
+def test_extend_with_scales_of_any_sign(lens, news, heads, dim, page, k_scale, v_scale, scale):
+    c = Paged(21, lens, 2, dim, page, True)
+    _rescaled(c, k_scale, v_scale)
+    off = _offsets(news)
+    q = _rows(torch.Generator().manual_seed(22), off[-1], heads, dim, 2.0)
+    out = mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q.to(DEV), scale=scale)
+    for s in range(len(lens)):
+        if news[s]:
+            rows = sorted(set(range(0, news[s], 7)) | {news[s] - 1})
+            pick = [off[s] + r for r in rows]
+            want, tol = O.attend(q[pick], c.k[s], c.v[s], [lens[s] - news[s] + r for r in rows], scale)
+            _check(out[pick], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("k_scale,v_scale,scale", SCALES)
+@pytest.mark.parametrize("lens,heads,dim,prefix", [
+    ([127, 33, 0, 400], 8, 128, None),                     # one workgroup per sequence
+    ([127, 128, 0, 1000], 4, 64, None),                    # pieces
+    ([90, 300], 34, 128, None),                            # more than 16 rows
+    ([300] * 8 + [170, 3], 8, 128, 150)])                  # a shared prefix
+def test_decode_with_scales_of_any_sign(lens, heads, dim, prefix, k_scale, v_scale, scale):
+    n = len(lens)
+    c = Paged(23, lens, 2, dim, 16, True, share=[(0 if m >= prefix else s, prefix) for s, m in enumerate(lens)] if prefix else None)
+    _rescaled(c, k_scale, v_scale)
+    q = _rows(torch.Generator().manual_seed(24), n, heads, dim, 2.0)
+    out = mes.AttnDecode(c.cache, heads, n)(c.layer, c.batch(), q.to(DEV), [0, n] if prefix else None, [prefix] if prefix else None, scale=scale)
+    for s, m in enumerate(lens):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [m - 1], scale)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
 
 
 # --------------------------------------------------------------------------------------------- what is not finite, and not seen
