@@ -352,7 +352,7 @@ typedef struct {
  * rotary: fp32 [n_positions][2][head_dim / 2], cosines then sines, n_positions >= table_pages * page_tokens; element i of
  * the first half turns with element i of the second: (a c - b s, b c + a s), every product and sum rounded to fp32, the
  * result once to bf16 (q_out; may be q) or to the cache's type (e4m3: after division by the scale, to nearest even,
- * clamped to +-448).  rotary NULL: keys are written as they are and q must be NULL.
+ * clamped to +-448; 0 stays 0 where the scale is 0).  rotary NULL: keys are written as they are and q must be NULL.
  * Rows without a place (see mes_seqs) are left out.  Two rows of one call must not share a place. */
 mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
                          int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,

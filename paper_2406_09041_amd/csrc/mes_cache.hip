@@ -20,9 +20,10 @@ __device__ inline uint32_t pack_bf16(float a, float b) {
 }
 
 // x / scale to e4m3: a true division, so that the nearest code is that of the quotient; clamped before the conversion (which
-// would make NaN of what is too large), NaN stays NaN.
+// would make NaN of what is too large), NaN stays NaN.  0 stays 0 also where the scale is 0: a head that is
+// always 0 has such a scale, and 0 / 0 would leave a NaN in the cache.
 __device__ inline float to_grid(float x, float scale) {
-  const float v = x / scale;
+  const float v = x == 0.0f && scale == 0.0f ? 0.0f : x / scale;
   return v > 448.0f ? 448.0f : v < -448.0f ? -448.0f : v;
 }
 __device__ inline uint32_t pack_e4m3(float a, float b, float c, float d) {

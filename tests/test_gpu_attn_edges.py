@@ -89,6 +89,27 @@ def test_decode_with_scales_of_any_sign(lens, heads, dim, prefix, k_scale, v_sca
         _check(out[s:s + 1], want, tol, f"sequence {s}")
 
 
+def test_append_under_a_scale_of_zero():
+    """What is 0 stays 0 (0 / 0 has no code), the rest is clamped: a head whose scale is 0 holds zeros, and rows that see it are finite."""
+    heads, kvh, dim, n = 4, 2, 64, 40
+    scale = [torch.tensor([[0.0, 0.02]], device=DEV) for _ in range(2)]
+    cache = mes.KvCache(1, 4, 16, kvh, dim, mes.KV_E4M3, *scale)
+    g = torch.Generator().manual_seed(25)
+    q, k, v = (_rows(g, n, h, dim) for h in (heads, kvh, kvh))
+    k[:, 0, ::2], v[:, 0, 1::2], k[3, 1, :], k[:, 0, 4] = 0.0, 0.0, 0.0, -0.0
+    batch = mes.SeqBatch(_ints([n]), _ints([[2, 0, 1, 3]]), _ints([0, n]))
+    mes.mes_kv_append(cache, 0, batch, None, k.to(DEV), v.to(DEV), None)
+    kept = []
+    for x, got in ((k, cache.k), (v, cache.v)):
+        code = torch.where(x.float() == 0, torch.zeros(()), x.float() / scale[0].cpu()[0][None, :, None]).clamp(-448, 448).to(torch.float8_e4m3fn).float()
+        got = got[0, [2, 0, 1]].cpu().float().transpose(1, 2).reshape(48, kvh, dim)[:n]
+        assert torch.equal(got, code)
+        kept.append(code.double() * scale[0].cpu()[0][None, :, None].double())
+    out = mes.mes_attn_extend(cache, 0, batch, q.to(DEV))
+    want, tol = O.attend(q, kept[0], kept[1], range(n), dim ** -0.5)
+    _check(out, want, tol)
+
+
 # --------------------------------------------------------------------------------------------- what is not finite, and not seen
 
 def _spoil(c, which, s, j, head, d, bad):
