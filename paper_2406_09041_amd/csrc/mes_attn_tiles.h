@@ -56,8 +56,12 @@ static __device__ const u32x4 g_zeros[16] = {};
 __device__ __forceinline__ void copy_to_lds(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(to) : "memory", "m0");
 }
-__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {   // base: the same in all lanes
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(to) : "memory", "m0");
+// base: the same in all lanes.  A vector instruction may have written its registers just before (a value that was kept in a lane), and a
+// vector memory instruction must not read such a register for 5 wait states, which the compiler does not look after in here: a scalar
+// copy of it may be read at once, and takes the place of the wait that M0 needs.
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t offset, uint32_t to) {
+  const void* at;
+  asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(at) : "v"(offset), "s"(base), "s"(to) : "memory", "m0");
 }
 
 // LDS accesses of the wavefront are done, then everybody's; copies into LDS are waited for apart.
