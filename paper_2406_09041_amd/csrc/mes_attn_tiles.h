@@ -47,8 +47,8 @@ struct TileLds {
   char kv[2][kRing][kTileBytes];      // keys, values
 };
 
-// What an absent token (behind the sequence's end, or on a page that does not exist) is read from: its value row must
-// not be able to turn a weight of 0 into NaN.
+// What an absent token (behind the sequence's end, before the first that is seen, or on a page that does not exist) is read from: its value
+// row must not be able to turn a weight of 0 into NaN.
 static __device__ const u32x4 g_zeros[16] = {};
 
 // 16 bytes per lane, lane l's to LDS address `to` + 16 l.  Written as instructions: for its builtin the compiler would make every
@@ -129,23 +129,26 @@ struct Stage {
       if (!real) page = 0;
       base += ((((int64_t)page * n_kv_heads + kvh) << page_shift) + (token0 & ((1 << page_shift) - 1))) * step;
     }
+    const bool lead = from > 0 && token0 < from;                      // never in the prompt kernel, where `from` is 0
     if constexpr (SRC != KV_PAGED_E4M3) {
       const uint32_t at = (uint32_t)(uintptr_t)slot(tile, kv) + Row<D>::at(kPart * wave);
-      if (real && token0 + kPart <= to) {
+      if (real && !lead && token0 + kPart <= to) {
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) copy_to_lds(base + (int64_t)i * kRowsCopy * step, offset[kv], at + i * kBlock);
       } else {
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-          const bool there = real && token0 + i * kRowsCopy + lane / kPieces < to;
+          const int token = token0 + i * kRowsCopy + lane / kPieces;
+          const bool there = real && token < to && !(lead && token < from);
           copy_to_lds(there ? (const void*)(base + (int64_t)i * kRowsCopy * step + offset[kv]) : (const void*)&g_zeros[lane % kPieces], at + i * kBlock);
         }
       }
     } else {
       const int r = lane / kLanes;
-      const char* from = base + (uint32_t)(r * D + lane % kLanes * (D / kLanes));
+      const char* codes = base + (uint32_t)(r * D + lane % kLanes * (D / kLanes));
+      const bool there = real && token0 + r < to && !(lead && token0 + r < from);
 #pragma unroll
-      for (int i = 0; i < kWords / 4; ++i) raw[i] = real && token0 + r < to ? *reinterpret_cast<const u32x4*>(from + 16 * i) : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < kWords / 4; ++i) raw[i] = there ? *reinterpret_cast<const u32x4*>(codes + 16 * i) : u32x4{0, 0, 0, 0};
     }
   }
   // all of this wavefront's copies but the last `younger`

@@ -193,3 +193,19 @@ def test_prompt_with_keys_shared_out_and_a_value_that_is_not_finite(heads, kvh, 
     _check(out[rows], want, tol, "rows before it")
     rows = [at, at + 1, at + 60, T - 1]
     _check_around(out[rows], q[rows], k, v, rows, dim ** -0.5, 5, "rows that see it")
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("heads,kvh,dim", [(4, 2, 128), (34, 2, 64), (17, 1, 128), (64, 1, 64)])
+def test_decode_does_not_see_its_own_copy_of_a_shared_prefix(heads, kvh, dim, e4m3):
+    """The prefix is read through the first sequence's pages: what the others hold in its place does not touch them (the last tokens of the
+    prefix lie in the tile that their own part begins in)."""
+    lens, prefix = [200, 210, 160, 170], 100
+    c = Paged(36, lens, kvh, dim, 16, e4m3, share=[(0, prefix)] * 4)
+    for s, which, j in ((1, "v", 64), (2, "v", 99), (3, "k", 97)):
+        _spoil(c, which, s, j, 0, 7, NAN)
+    q = _rows(torch.Generator().manual_seed(37), 4, heads, dim)
+    out = mes.AttnDecode(c.cache, heads, 4)(c.layer, c.batch(), q.to(DEV), [0, 4], [prefix])
+    for s, n in enumerate(lens):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [n - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
