@@ -608,16 +608,15 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
         const int k = min(k0 + W * b, count - 1), p = i0 + k;
-        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), k));
-        f[b] = k0 + W * b < count ? w : 0.0f;
+        f[b] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), k));
         const float* o = p < n_pre ? pre_o + (size_t)p * kRowsPass * D : own_o + (size_t)(p - n_pre) * group * D;
 #pragma unroll
         for (int e = 0; e < E; ++e) v[b][e] = o[E * lane + e];
       }
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b)
+      for (int b = 0; b < kBatch; ++b)            // behind the last piece it is read again, and left out: its values may be infinite
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf(f[b], v[b][e], x[e]);
+        for (int e = 0; e < E; ++e) x[e] = k0 + W * b < count ? fmaf(f[b], v[b][e], x[e]) : x[e];
     }
   }
   if constexpr (W == 4) {                            // all four have the same maximum and sum

@@ -1,5 +1,5 @@
 """Attention calls where values or scales are out of the ordinary: scales of the caller's own, an 8-bit cache's scales of any sign, values
-that are not finite behind rows that do not see them.  References and tolerances: oracle/attn_oracle.py."""
+that are not finite behind rows that do not see them, and in front of rows that do.  References and tolerances: oracle/attn_oracle.py."""
 import pytest
 import torch
 
@@ -208,4 +208,23 @@ def test_decode_does_not_see_its_own_copy_of_a_shared_prefix(heads, kvh, dim, e4
     out = mes.AttnDecode(c.cache, heads, 4)(c.layer, c.batch(), q.to(DEV), [0, 4], [prefix])
     for s, n in enumerate(lens):
         want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [n - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("lens,heads,kvh,prefix,at", [([2000], 4, 2, None, 1990), ([2000, 1900], 34, 2, None, 1890), ([3000] * 3, 8, 8, None, 2999),
+                                                      ([200, 210, 160], 34, 2, 100, 80), ([200, 210, 160], 34, 2, 100, 150), ([1200, 1300], 8, 2, 1000, 990)])
+def test_decode_rows_that_see_an_infinite_value_are_infinite(lens, heads, kvh, prefix, at):
+    """sum w_j v_j with one v_j = inf and weights above 0 is inf, not NaN, however the tokens are cut into pieces."""
+    dim, n = 128, len(lens)
+    c = Paged(38, lens, kvh, dim, 16, share=[(0, prefix)] * n if prefix else None)
+    for s in range(n):
+        _spoil(c, "v", s, at, 0, 7, INF)
+    q = _rows(torch.Generator().manual_seed(39), n, heads, dim, 0.5)
+    out = mes.AttnDecode(c.cache, heads, n)(c.layer, c.batch(), q.to(DEV), [0, n] if prefix else None, [prefix] if prefix else None).cpu()
+    group = heads // kvh
+    assert (out[:, :group, 7] == INF).all()
+    out[:, :group, 7] = 0.0
+    for s, m in enumerate(lens):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [m - 1], dim ** -0.5)
+        want[:, :group, 7] = 0.0
         _check(out[s:s + 1], want, tol, f"sequence {s}")
