@@ -353,10 +353,15 @@ typedef struct {
  * the first half turns with element i of the second: (a c - b s, b c + a s), every product and sum rounded to fp32, the
  * result once to bf16 (q_out; may be q) or to the cache's type (e4m3: after division by the scale, to nearest even,
  * clamped to +-448; 0 stays 0 where the scale is 0).  rotary NULL: keys are written as they are and q must be NULL.
- * Rows without a place (see mes_seqs) are left out.  Two rows of one call must not share a place. */
+ * Rows without a place (see mes_seqs) are left out: nothing is written for rows before position 0, past the table's room
+ * or behind the last sequence; on a page outside the cache only q_out is.  Two rows of one call must not share a place. */
 mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
                          int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
                          int ld_q_out, void* stream);
+/* The same for a q_out (neither NULL nor q) whose memory holds nothing yet: rows of it that would be left out are 0. */
+mes_status mes_kv_append_fresh(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                               int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
+                               int ld_q_out, void* stream);
 
 /* Attention over whole prompts: n_seqs sequences packed one after the other, rows seq_offsets[s] .. seq_offsets[s+1]
  * (DEVICE int32 [n_seqs + 1], 0 = o[0] <= ... <= o[n_seqs] <= T; rows behind are left as they are), every row sees the

@@ -39,7 +39,7 @@ EXPORTS = ["mes_base_bytes", "mes_codes_bytes", "mes_salient_bytes", "mes_pack_w
            "mes_gated_workspace_bytes", "mes_delta_linear_gated",
            "mes_step_grad_workspace_bytes", "mes_step_grad", "mes_step_adamw", "mes_noalloc_scratch_bytes",
            "mes_delta_linear_noalloc", "mes_long_segment_tokens",
-           "mes_kv_append", "mes_attn_prompt", "mes_attn_prompt_workspace_bytes", "mes_attn_extend", "mes_attn_decode_workspace_bytes", "mes_attn_decode",
+           "mes_kv_append", "mes_kv_append_fresh", "mes_attn_prompt", "mes_attn_prompt_workspace_bytes", "mes_attn_extend", "mes_attn_decode_workspace_bytes", "mes_attn_decode",
            "mes_kv_copy_pages", "mes_pages_create", "mes_pages_destroy", "mes_pages_grow", "mes_pages_fork", "mes_pages_free",
            "mes_pages_compact", "mes_pages_table", "mes_pages_length", "mes_pages_unused"]
 
@@ -165,8 +165,8 @@ def _load() -> ctypes.CDLL:
     lib.mes_pool_stats.restype = c_int
     lib.mes_pool_stats.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
     kvp, sqp, fl = ctypes.POINTER(mes_kv), ctypes.POINTER(mes_seqs), ctypes.c_float
-    lib.mes_kv_append.restype = c_int
-    lib.mes_kv_append.argtypes = [kvp, c_int, sqp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, c_int, vp, c_int, vp]
+    lib.mes_kv_append.restype = lib.mes_kv_append_fresh.restype = c_int
+    lib.mes_kv_append.argtypes = lib.mes_kv_append_fresh.argtypes = [kvp, c_int, sqp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, c_int, vp, c_int, vp]
     lib.mes_attn_prompt.restype = c_int
     lib.mes_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, c_int, c_int, c_int, c_int, c_int, fl, vp, c_int, vp, c_sz, vp]
     lib.mes_attn_prompt_workspace_bytes.restype = c_sz
@@ -664,8 +664,9 @@ def rotary_table(n_positions: int, head_dim: int, base: float = 10000.0, device=
 
 def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                   rotary: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
-    """Rotates the new rows' queries (returned; q_out may be q) and keys and puts keys and values into the cache's pages."""
-    index = cache.index
+    """Rotates the new rows' queries (returned; q_out may be q) and keys and puts keys and values into the cache's pages.  Rows without a
+    position are left as they are in a q_out that is given, and 0 where it is allocated."""
+    index, entry = cache.index, lib.mes_kv_append
     T, kv_heads, dim, ld_k = _rows("k", k, index)
     rows_v = _rows("v", v, index)
     assert batch.index == index and rows_v[:3] == (T, kv_heads, dim) == (T, cache.n_kv_heads, cache.head_dim), "k, v: [T, n_kv_heads, head_dim] of the cache"
@@ -678,11 +679,11 @@ def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch
         n, heads, d, ld_q = _rows("q", q, index)
         assert n == T and d == dim
         if q_out is None:
-            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            q_out, entry = torch.empty_like(q, memory_format=torch.contiguous_format), lib.mes_kv_append_fresh
         n, h, d, ld_o = _rows("q_out", q_out, index)
         assert (n, h, d) == (T, heads, dim)
         src, dst = q.data_ptr(), q_out.data_ptr()
-    _call_on(index, lib.mes_kv_append, cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3], rot, n_pos, dst, ld_o)
+    _call_on(index, entry, cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3], rot, n_pos, dst, ld_o)
     return q_out if q is not None else None
 
 

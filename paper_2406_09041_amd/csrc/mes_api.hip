@@ -341,15 +341,16 @@ static size_t kv_layer_bytes(const mes_kv& kv) {
 }
 static int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
 
-mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+static mes_status append(const char* who, bool fresh, const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
                          int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
                          int ld_q_out, void* stream) {
-  static const char who[] = "mes_kv_append";
   if (mes_status st = check_kv(who, kv, layer)) return st;
   if (mes_status st = check_seqs(who, kv, seqs, false)) return st;
   if (mes_status st = check_row_count(who, T)) return st;
   if (!seqs->q_offsets && T > seqs->n_seqs) return fail(MES_ERR_SEGMENTS, "%s: %d rows of %d sequences without q_offsets", who, T, seqs->n_seqs);
-  if (T == 0 || seqs->n_seqs == 0) return MES_OK;
+  if (T == 0 || (seqs->n_seqs == 0 && !fresh)) return MES_OK;
+  if (fresh && (!q || !q_out)) return fail(MES_ERR_NULL, "%s: q / q_out is null", who);
+  if (fresh && q == q_out) return fail(MES_ERR_SHAPE, "%s: q_out is q", who);
   if ((q == nullptr) != (q_out == nullptr)) return fail(MES_ERR_NULL, "%s: give both of q and q_out or neither", who);
   if (q && !rotary) return fail(MES_ERR_NULL, "%s: q needs rotary", who);
   if (mes_status st = check_rows(who, "k", k, ld_k, kv->n_kv_heads, kv->head_dim)) return st;
@@ -360,15 +361,27 @@ mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, cons
     if (mes_status st = check_rows(who, "q_out", q_out, ld_q_out, n_heads, kv->head_dim)) return st;
     if (q == q_out && ld_q != ld_q_out) return fail(MES_ERR_SHAPE, "%s: q_out is q with rows %d apart instead of %d", who, ld_q_out, ld_q);
   }
-  const int capacity = seqs->table_pages * kv->page_tokens;
+  const int capacity = seqs->n_seqs ? seqs->table_pages * kv->page_tokens : 0;   // no sequences: the table is not looked at
   if (rotary) {
     if (!aligned16(rotary)) return fail(MES_ERR_ALIGN, "%s: rotary must be 16-byte aligned", who);
     if (n_positions < capacity) return fail(MES_ERR_SHAPE, "%s: rotary has %d positions, the page table has room for %d", who, n_positions, capacity);
   }
   AppendArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, rotary, (uint16_t*)q_out, kv->k, kv->v, kv->k_scale, kv->v_scale,
                seqs->q_offsets, seqs->kv_len, seqs->page_table, layer, kv->n_pages, log2_of(kv->page_tokens), n_heads, kv->n_kv_heads,
-               kv->head_dim, seqs->n_seqs, seqs->table_pages, capacity, ld_q, ld_k, ld_v, ld_q_out};
+               kv->head_dim, seqs->n_seqs, seqs->table_pages, capacity, ld_q, ld_k, ld_v, ld_q_out, fresh};
   return check_hip(launch_append(a, T, kv->dtype == MES_KV_E4M3, (hipStream_t)stream), who);
+}
+
+mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                         int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
+                         int ld_q_out, void* stream) {
+  return append("mes_kv_append", false, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, rotary, n_positions, q_out, ld_q_out, stream);
+}
+
+mes_status mes_kv_append_fresh(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                               int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
+                               int ld_q_out, void* stream) {
+  return append("mes_kv_append_fresh", true, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, rotary, n_positions, q_out, ld_q_out, stream);
 }
 
 size_t mes_attn_prompt_workspace_bytes(int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim) {

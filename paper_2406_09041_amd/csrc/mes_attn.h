@@ -20,6 +20,7 @@ struct AppendArgs {
   const int32_t *q_offsets, *kv_len, *page_table;
   int layer, n_pages, page_shift, n_heads, n_kv_heads, head_dim, n_seqs, table_pages, capacity;
   int ld_q, ld_k, ld_v, ld_q_out;
+  bool fresh;                          // rows of q_out that get nothing are set to 0
 };
 hipError_t launch_append(const AppendArgs& a, int T, bool fp8, hipStream_t s);
 hipError_t launch_copy_pages(const mes_kv& kv, const int32_t* src, const int32_t* dst, int n, hipStream_t s);

@@ -70,11 +70,16 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
       if (a.q_offsets[mid + 1] > t) hi = mid; else lo = mid + 1;
     }
     s = lo;
-    if (s >= a.n_seqs || a.q_offsets[s] > t) return;       // behind the last sequence
-    behind = a.q_offsets[s + 1] - t;
+    if (s >= a.n_seqs || a.q_offsets[s] > t) s = -1;       // behind the last sequence
+    else behind = a.q_offsets[s + 1] - t;
   }
-  const int pos = max(a.kv_len[s], 0) - behind;
-  if (pos < 0 || pos >= a.capacity) return;
+  const int pos = s < 0 ? -1 : max(a.kv_len[s], 0) - behind;
+  if (pos < 0 || pos >= a.capacity) {
+    if (a.fresh)
+      for (int i = threadIdx.x * 8; i < a.n_heads * a.head_dim; i += kAppendThreads * 8)
+        *reinterpret_cast<uint4*>(a.q_out + (size_t)t * a.ld_q_out + i) = make_uint4(0, 0, 0, 0);
+    return;
+  }
   const int page = a.page_table[(size_t)s * a.table_pages + (pos >> a.page_shift)];
   const bool placed = (unsigned)page < (unsigned)a.n_pages;
   const int d = a.head_dim, half = d >> 1, per = half >> 3;   // per: units of a head

@@ -1,5 +1,6 @@
-"""Attention calls where values or scales are out of the ordinary: scales of the caller's own, an 8-bit cache's scales of any sign, values
-that are not finite behind rows that do not see them, and in front of rows that do.  References and tolerances: oracle/attn_oracle.py."""
+"""Attention calls where values, scales or places are out of the ordinary: scales of the caller's own, an 8-bit cache's scales of any sign,
+values that are not finite behind rows that do not see them and in front of rows that do, rows without a place.  References and
+tolerances: oracle/attn_oracle.py."""
 import pytest
 import torch
 
@@ -228,3 +229,28 @@ def test_decode_rows_that_see_an_infinite_value_are_infinite(lens, heads, kvh, p
         want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [m - 1], dim ** -0.5)
         want[:, :group, 7] = 0.0
         _check(out[s:s + 1], want, tol, f"sequence {s}")
+
+
+# ------------------------------------------------------------------------------------------------------ rows without a place
+
+def test_turned_queries_of_rows_without_a_position():
+    """A q_out that the call allocates holds zeros for rows that have no position or no sequence, whatever was in its memory; the other
+    rows are turned, also those whose page is outside the cache."""
+    heads, kvh, dim, page, T = 4, 2, 64, 16, 30
+    g = torch.Generator().manual_seed(40)
+    cache = mes.KvCache(1, 6, page, kvh, dim)
+    rotary = mes.rotary_table(2 * page, dim)
+    q, k, v = (_rows(g, T, h, dim).to(DEV) for h in (heads, kvh, kvh))
+    #  rows 0..9 of a sequence of 6 tokens (4 have no position), 10..19 of one longer than the table, 20..25 on no page; 26..29: no sequence
+    batch = mes.SeqBatch(_ints([6, 37, 6]), _ints([[0, 1], [2, 3], [-1, 6]]), _ints([0, 10, 20, 26]))
+    for _ in range(3):
+        stale = torch.full((T, heads, dim), NAN, dtype=torch.bfloat16, device=DEV)
+        del stale                                                      # its memory is the next tensor's
+        out = mes.mes_kv_append(cache, 0, batch, q, k, v, rotary).cpu()
+        pos = {**{4 + i: i for i in range(6)}, **{10 + i: 27 + i for i in range(5)}, **{20 + i: i for i in range(6)}}
+        rows = sorted(pos)
+        want = O.rotate(q.cpu()[rows], rotary.cpu(), torch.tensor([pos[r] for r in rows])).to(torch.bfloat16)
+        assert torch.equal(out[rows].view(torch.int16), want.view(torch.int16))
+        assert not out[[r for r in range(T) if r not in pos]].view(torch.int16).any()
+        none = mes.SeqBatch(_ints([]), torch.zeros(0, 2, dtype=torch.int32, device=DEV), _ints([0]))
+        assert not mes.mes_kv_append(cache, 0, none, q, k, v, rotary).view(torch.int16).any()            # no sequences at all
