@@ -9,5 +9,5 @@ from .binding import (  # noqa: F401
     mes_pack_delta, mes_select_salient, mes_unpack_base, mes_unpack_delta, salient_bytes, DeltaLinearMulti, KernelTimer,
     mes_copy_probe, ExpertPool, mes_delta_linear_descriptors, mes_delta_linear_multi_descriptors, StepGrad, mes_step_adamw,
     mes_delta_linear_noalloc, DeltaLinearGated, KV_BF16, KV_E4M3, AttnDecode, KvCache, PagePool, SeqBatch, mes_attn_extend,
-    mes_attn_prompt, mes_kv_append, mes_kv_copy_pages, rotary_table,
+    mes_attn_prompt, mes_kv_append, mes_kv_copy_pages, prompt_workspace, rotary_table,
 )

@@ -1,6 +1,9 @@
 """Attention and its cache, host side (no GPU): refusals beside those of test_attn_host.py."""
 import ctypes
 
+import torch
+
+import paper_2406_09041_amd as mes
 import paper_2406_09041_amd.binding as B
 from test_attn_host import FAKE, ODD, _kv, _seqs
 
@@ -20,3 +23,8 @@ def test_append_into_fresh_queries_errors():
     # the other checks are those of mes_kv_append
     assert _fresh(k=None) == 1 and _fresh(q_out=ODD) == 6 and _fresh(ld_o=255) == 2 and _fresh(n_pos=63) == 2 and _fresh(rotary=None) == 1 and _fresh(heads=0) == 2
     assert _fresh(seqs=_seqs(n_seqs=0, kv_len=None, page_table=None), q_out=ODD) == 6                  # no sequences: all rows are cleared
+
+
+def test_the_prompt_workspace_is_the_packages_own():
+    ws = mes.prompt_workspace(5, 1, 4, 2, 64, "cpu")
+    assert ws.dtype == torch.uint8 and ws.numel() == lib.mes_attn_prompt_workspace_bytes(5, 1, 4, 2, 64) > 0
