@@ -741,11 +741,14 @@ def mes_attn_extend(cache: KvCache, layer: int, batch: SeqBatch, q: torch.Tensor
 
 
 class AttnDecode:
-    """mes_attn_decode with its workspace, for up to max_seqs sequences; all layers of a model can share one."""
+    """mes_attn_decode with its workspace, for up to max_seqs sequences; all layers of a model can share one, and calls follow one another
+    on one stream (or wait for each other)."""
 
     def __init__(self, cache: KvCache, n_heads: int, max_seqs: int = 64, workspace: Optional[torch.Tensor] = None):
         self.cache, self.n_heads = cache, n_heads
-        n = max(lib.mes_attn_decode_workspace_bytes(max_seqs, n_heads, cache.n_kv_heads, cache.head_dim), 16)
+        assert 0 <= max_seqs <= MAX_SEQS, f"max_seqs = {max_seqs} outside [0, {MAX_SEQS}]"
+        n = lib.mes_attn_decode_workspace_bytes(max(max_seqs, 1), n_heads, cache.n_kv_heads, cache.head_dim)
+        assert n, f"n_heads = {n_heads} must be 1 to 64 times the cache's {cache.n_kv_heads}, head_dim 64 or 128 (got {cache.head_dim})"
         self.ws = workspace if workspace is not None else torch.empty(n, dtype=torch.uint8, device=cache.device)
         self.scratch = _scratch(self.ws, cache.index)
 

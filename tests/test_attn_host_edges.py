@@ -1,6 +1,8 @@
 """Attention and its cache, host side (no GPU): refusals beside those of test_attn_host.py."""
 import ctypes
+from types import SimpleNamespace
 
+import pytest
 import torch
 
 import paper_2406_09041_amd as mes
@@ -23,6 +25,16 @@ def test_append_into_fresh_queries_errors():
     # the other checks are those of mes_kv_append
     assert _fresh(k=None) == 1 and _fresh(q_out=ODD) == 6 and _fresh(ld_o=255) == 2 and _fresh(n_pos=63) == 2 and _fresh(rotary=None) == 1 and _fresh(heads=0) == 2
     assert _fresh(seqs=_seqs(n_seqs=0, kv_len=None, page_table=None), q_out=ODD) == 6                  # no sequences: all rows are cleared
+
+
+def test_the_decode_workspace_is_refused_where_no_call_could_use_it():
+    cache = lambda kvh=2, dim=64: SimpleNamespace(n_kv_heads=kvh, head_dim=dim, device="cpu", index=-1)  # noqa: E731
+    for heads, seqs, c, what in ((4, 2049, cache(), "max_seqs"), (4, -1, cache(), "max_seqs"), (5, 8, cache(), "n_heads"), (130, 8, cache(), "n_heads"),
+                                 (0, 8, cache(), "n_heads"), (4, 8, cache(dim=96), "head_dim")):
+        with pytest.raises(AssertionError, match=what):
+            mes.AttnDecode(c, heads, seqs)
+    for seqs in (0, 1, 2048):
+        assert mes.AttnDecode(cache(), 4, seqs).ws.numel() == lib.mes_attn_decode_workspace_bytes(max(seqs, 1), 4, 2, 64)
 
 
 def test_the_prompt_workspace_is_the_packages_own():
