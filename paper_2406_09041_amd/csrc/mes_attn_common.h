@@ -14,9 +14,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-// The running maximum of a row's scores (in powers of two) is raised only by a score more than this above it: weights up
-// to 2^kSlack stay far from the ends of fp32 and bf16, and the accumulators are rescaled a few times per row instead of at
-// almost every tile.
+// Weights are 2^(score - m) (scores in powers of two) with a running bound m of the row's scores.  Where a score passes it, it is raised to
+// this much above the largest, so that the accumulators are rescaled a few times per row instead of at almost every tile; no weight is
+// above 1 (a value of any size times its weight is finite), and the largest is at least 2^-kSlack, far from the ends of fp32 and bf16.
 constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32; -inf gives 0

@@ -5,7 +5,7 @@
 // prefixes (once per pass of up to 64 query rows), then what every sequence has of its own.  The line is cut into equal
 // chunks, one per workgroup, wherever that falls: the workgroups are equally busy however the lengths are spread, also for one long
 // sequence, and the launch does not depend on the lengths, which stay on the device (every workgroup adds them up for itself).  A
-// piece of the line that does not cover a sequence alone leaves (max, sum, weighted values) in the workspace, and k_join
+// piece of the line that does not cover a sequence alone leaves (bound, sum, weighted values) in the workspace, and k_join
 // adds the pieces of a row in their order.
 //
 // Up to 16 query rows (one sequence of a group of up to 16 heads, or few sequences' shared prefix): a wavefront takes 32 tokens at a
@@ -43,7 +43,7 @@ struct Shape {                       // what host and device derive alike
   int group, per_pass, n_passes;     // query heads per key / value head, sequences per pass, passes of all groups
 };
 
-// partial results: [slot][rows][D] floats, then [slot][rows] (max, sum)
+// partial results: [slot][rows][D] floats, then [slot][rows] (bound, sum)
 struct Partials {
   float* o;
   float2* ml;
@@ -229,10 +229,10 @@ struct Few {
             if (!seen(h, e)) s[h][e] = -INFINITY;
       }
       float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))) * scale;
-      if (__any(top > m + kSlack)) {
+      if (__any(top > m)) {
         top = fmaxf(top, other_row16(top));
         top = fmaxf(top, other_half(top));
-        const float raised = fmaxf(m, top);
+        const float raised = fmaxf(m, top + kSlack);
         const float shrink = exp2_fast(m - (raised == -INFINITY ? 0.0f : raised));
         l *= shrink;
 #pragma unroll
@@ -286,7 +286,7 @@ struct Few {
   pages[0] = pages_then[0];
   pages[1] = pages_then[1];
 
-  // ---- the four wavefronts' results on one maximum, added in their order
+  // ---- the four wavefronts' results on one bound, added in their order
   __syncthreads();                                  // the last piece's reads of LDS are over
   l += other_row16(l);
   l += other_half(l);
@@ -563,7 +563,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
   }
 }
 
-// One wavefront (W = 4: four, sharing out the pieces) per query row: the pieces of its prefix and its own, on one maximum.
+// One wavefront (W = 4: four, sharing out the pieces) per query row: the pieces of its prefix and its own, on one bound.
 template <int D, int W>
 __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
   constexpr int E = D / 64;                          // dimensions per lane
@@ -619,7 +619,7 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
         for (int e = 0; e < E; ++e) x[e] = k0 + W * b < count ? fmaf(f[b], v[b][e], x[e]) : x[e];
     }
   }
-  if constexpr (W == 4) {                            // all four have the same maximum and sum
+  if constexpr (W == 4) {                            // all four have the same bound and sum
 #pragma unroll
     for (int e = 0; e < E; ++e) part[wave][E * lane + e] = x[e];
     __syncthreads();

@@ -1,6 +1,6 @@
 // Causal attention over packed prompts, and over new tokens behind a paged cache.  Bound by the matrix cores (and the
 // exponentials between their products); the mathematics, per query row with scores s_j = scale * <q, k_j>:
-//   m = max s_j (kept within kSlack of it), p_j = 2^(s_j log2e - m), l = sum p_j, o = sum p_j v_j / l
+//   p_j = 2^(s_j log2e - m) with a bound m of the exponents, at most kSlack above the largest, l = sum p_j, o = sum p_j v_j / l
 // in one pass over the keys, 64 at a time, nothing of the scores in memory (mes_attn_tiles.h).
 //
 // A workgroup is 4 wavefronts of 32 query rows: of up to 4 heads that share keys and values (all of them then see as many keys,
@@ -142,7 +142,7 @@ __device__ bool item_number(const PromptArgs& a, const Lanes& y, int R, int j, i
   return it.tile >= 0 && it.tile < (it.rows + R - 1) / R;
 }
 
-// The parts' results, per part and head group: (max, sum) of the 128 rows of the wavefronts, and their weighted values in the order of the
+// The parts' results, per part and head group: (bound, sum) of the 128 rows of the wavefronts, and their weighted values in the order of the
 // accumulators: [wavefront][4 dimensions: 8 (i / 4) + half][32 rows] x 4.
 struct PieceLayout {
   size_t o, total;
@@ -193,7 +193,7 @@ __device__ __forceinline__ void attend_by_key(TileRows<D>& w, Stage<D, SRC>& sta
         }
         dot = (dot + other_half(dot)) * scale;
         const bool seen = t * kTile + r <= last[b];
-        const float raised = seen && dot > w.m[b] + kSlack ? dot : w.m[b];
+        const float raised = seen && dot > w.m[b] ? dot + kSlack : w.m[b];
         const float shrink = raised == w.m[b] ? 1.0f : exp2_fast(w.m[b] - raised);
         const float weight = bf16_at(pack2(exp2_fast(dot - (raised == -INFINITY ? 0.0f : raised)), 0.0f), 0);
         w.m[b] = raised;

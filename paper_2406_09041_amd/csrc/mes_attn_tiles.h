@@ -173,7 +173,7 @@ struct TileRows {
   static constexpr int KS = D / 16, DT = D / 32;
   bf16x8 q[NB][KS];               // NB = 1 block of 32 rows; Q^T operands: lane (col, half) holds dimensions 16 ks + 8 half + (0..7) of row col of the block
   f32x16 acc[NB][DT];             // O^T: lane holds its row, dimensions 32 dt + 8 (i / 4) + 4 half + i % 4
-  float m[NB], l[NB];              // running maximum (in powers of two); sum over this half's keys
+  float m[NB], l[NB];              // running bound of the scores (in powers of two); sum over this half's keys
 };
 
 // One tile's scores -> -inf where the row does not see the key.  `last[b]`: the last key that the lane's row of block b sees.
@@ -259,15 +259,15 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
   f32x16 s0[NB][2], s1[NB][2];                                        // scores [block][32 keys] of two tiles in turn
   float from[NB];
 
-  auto raise = [&](const float (&top)[NB]) {                          // the running maxima, seldom
+  auto raise = [&](const float (&top)[NB]) {                          // the bounds, seldom
     bool above = false;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) above |= top[b] * scale > w.m[b] + kSlack;
+    for (int b = 0; b < NB; ++b) above |= top[b] * scale > w.m[b];
     if (__any(above)) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const float t = fmaxf(top[b], other_half(top[b])) * scale;
-        const float raised = fmaxf(w.m[b], t);
+        const float raised = fmaxf(w.m[b], t + kSlack);
         const float shrink = exp2_fast(w.m[b] - (raised == -INFINITY ? 0.0f : raised));
         w.l[b] *= shrink;
 #pragma unroll

@@ -1,6 +1,6 @@
 """Attention calls where values, scales or places are out of the ordinary: scales of the caller's own, an 8-bit cache's scales of any sign,
-values that are not finite behind rows that do not see them and in front of rows that do, rows without a place.  References and
-tolerances: oracle/attn_oracle.py."""
+values that are not finite behind rows that do not see them and in front of rows that do, rows without a place, the type's largest
+values.  References and tolerances: oracle/attn_oracle.py."""
 import pytest
 import torch
 
@@ -254,3 +254,33 @@ def test_turned_queries_of_rows_without_a_position():
         assert not out[[r for r in range(T) if r not in pos]].view(torch.int16).any()
         none = mes.SeqBatch(_ints([]), torch.zeros(0, 2, dtype=torch.int32, device=DEV), _ints([0]))
         assert not mes.mes_kv_append(cache, 0, none, q, k, v, rotary).view(torch.int16).any()            # no sequences at all
+
+
+# ----------------------------------------------------------------------------------------------------------- the largest values
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_rows_that_see_the_largest_value_are_finite(dim):
+    """The type's largest number as a value, at a token whose score is above that of the tokens before it, but not by much: a sum of weights
+    that are at most 1 holds it."""
+    big, n, at, heads, kvh = 3.3895313892515355e38, 200, 150, 4, 2
+    g = torch.Generator().manual_seed(50)
+    k, v, q = torch.zeros(n, kvh, dim), _rows(g, n, kvh, dim), torch.zeros(n, heads, dim)
+    q[:, :, 0], k[at, :, 0] = 4.0, 1.0                                   # scores 0, and 4 for this token: 2^5.8 times their weight
+    q, k, scale = q.to(torch.bfloat16), k.to(torch.bfloat16), 1.0
+    v[at, 0, 5], v[at, 1, 6] = big, -big
+    want, tol = O.attend(q, k, v, range(n), scale)
+    assert bool(torch.isfinite(want).all()) and float(want.abs().max()) > 5e37
+    out = mes.mes_attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), _ints([0, n]), scale=scale)
+    _check(out, want, tol, "prompt")
+    cache = mes.KvCache(1, 13, 16, kvh, dim)
+    batch = mes.SeqBatch(_ints([n]), _ints([list(range(13))]), _ints([0, n]))
+    mes.mes_kv_append(cache, 0, batch, None, k.to(DEV), v.to(DEV), None)
+    _check(mes.mes_attn_extend(cache, 0, batch, q.to(DEV), scale=scale), want, tol, "extend")
+    one = mes.SeqBatch(_ints([n]), _ints([list(range(13))]))
+    _check(mes.AttnDecode(cache, heads, 1)(0, one, q[-1:].to(DEV), scale=scale), want[-1:], tol[-1:], "decode")
+    two = mes.SeqBatch(_ints([n, n]), _ints([list(range(13))] * 2))
+    order = torch.tensor([0, 1] * 10 + [2, 3] * 10)
+    wide = q[-1:][:, order].to(DEV)                                       # 20 heads per key / value head: rows share tiles
+    out = mes.AttnDecode(cache, 40, 2)(0, two, torch.cat([wide, wide]), [0, 2], [n - 10], scale=scale)
+    for row in out:
+        _check(row[None], want[-1:][:, order], tol[-1:][:, order], "decode, shared")
