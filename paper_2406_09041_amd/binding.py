@@ -23,7 +23,7 @@ MAX_EXPERTS = 64
 
 KV_BF16, KV_E4M3 = 0, 1
 MAX_SEQS = 2048
-SHORT_PROMPT = 704          # keys: rows that see no more are never shared out, and need no workspace
+SHORT_PROMPT = 704          # keys, 11 tiles of 64: the library never shares out rows that see no more, and needs no workspace for them
 
 STATUS_NAMES = {0: "MES_OK", 1: "MES_ERR_NULL", 2: "MES_ERR_SHAPE", 3: "MES_ERR_BITS", 4: "MES_ERR_SALIENT",
                 5: "MES_ERR_SEGMENTS", 6: "MES_ERR_ALIGN", 7: "MES_ERR_WORKSPACE", 8: "MES_ERR_DEVICE", 9: "MES_ERR_PAGES"}

@@ -2,7 +2,7 @@
 // every distinct cached token is read once, 2 head_dim values per key / value head, for 4 head_dim n_heads operations.
 //
 // Work is a flat line of units (kUnit = 128 tokens of one key / value head): per key / value head first the shared
-// prefixes (once per pass of up to 64 query rows), then what every sequence has of its own.  The line is cut into equal
+// prefixes (once per pass of up to 128 query rows), then what every sequence has of its own.  The line is cut into equal
 // chunks, one per workgroup, wherever that falls: the workgroups are equally busy however the lengths are spread, also for one long
 // sequence, and the launch does not depend on the lengths, which stay on the device (every workgroup adds them up for itself).  A
 // piece of the line that does not cover a sequence alone leaves (bound, sum, weighted values) in the workspace, and k_join
@@ -20,10 +20,15 @@
 // at 16 rows is where the small body would read the tokens a second time: 64 sequences of 16 experts (1 to 25 each) took 62 us by passes of
 // 16 rows and 47 through LDS, 96 behind one e4m3 prefix 94 and 60.
 //
-// Measured (head_dim 128, 32 heads over 8 key / value heads): 256 sequences of 0 to 8192 tokens 165 us, 4.9 TB/s of the 5.96 that a
-// pass that only reads reaches; 64 sequences of 512 tokens 23 us (5.9 TB/s); 64 of 16 experts with prompts of 512 to 1600 tokens 43 us, 106
-// MB; 96 behind 8200 shared tokens of an e4m3 cache 59 us, of which 10 us are products at the library's rate (own pieces cost 4 to 5 us each beside the
-// larger body, but a launch of their own for them made it 68 and the 64 sequences 51); one sequence of 200 tokens 9.2 us.
+// Weights are rounded to bf16 for the product with V, as the matrix cores take both operands alike, and summed as rounded: they still add up
+// to 1, and a row's error grows by at most 2^-8 of its weighted values' size (measured against 64 bits: 0.0020 of the rows' norm, 0.0017
+// with weights in fp32).
+//
+// Measured (head_dim 128, 32 heads over 8 key / value heads): 256 sequences of 0 to 8192 tokens 160 us, 5.0 TB/s of the 5.96 that a
+// pass that only reads reaches; the same at e4m3 99 us, 4.0 TB/s; 64 sequences of 512 tokens 26.5 us (5.1 TB/s); 64 of 16 experts with prompts of 512 to
+// 1600 tokens 42 us, 106 MB; 96 behind 8200 shared tokens of an e4m3 cache 54 us, of which 10 us are products at the library's rate; one sequence of
+// 200 tokens 8.3 us.  Own pieces cost 4 to 5 us each beside the larger body; in a launch of their own it was worse: 43 -> 51 us for the 64
+// sequences, 59 -> 68 for the shared prefix.
 #include "mes_attn_tiles.h"
 
 namespace mes {
@@ -31,11 +36,11 @@ namespace {
 
 constexpr int kThreads = 256, kUnit = 128, kRowsPass = 128, kFewRows = 16;
 // Workgroups of a launch: what the chip holds.  Without shared prefixes and with up to 16 heads per key / value head only the small body is
-// needed, which leaves room for three per compute unit (256 sequences of 0 to 8192 tokens: 168 us, as a part
+// needed, which leaves room for three per compute unit (256 sequences of 0 to 8192 tokens, when it was made: 168 us, as a part
 // of the larger kernel, two per compute unit, 186).
 constexpr int kWorkgroups = 512, kWorkgroupsFew = 768;
 // Up to this many tokens a sequence is one workgroup's, where nothing is shared: no second launch to add up pieces (one
-// sequence of 200 tokens: 9.2 us, 12.4 with it).
+// sequence of 200 tokens, when it was made: 9.2 us, 12.4 with it).
 constexpr int kWholeTokens = 512;
 static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
 
@@ -380,7 +385,7 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const S
   }
 }
 
-// MANY: pieces of more than 16 rows can occur.  WHOLE: workgroup i does sequence i % n_seqs alone, and there is nothing to join.
+// MANY: prefixes are shared, or more than 16 query heads a key / value head: both bodies are there, also where no pass has more than 16 rows.  WHOLE: workgroup i does sequence i % n_seqs alone, and there is nothing to join.
 template <int D, bool FP8, bool MANY, bool WHOLE>
 __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCall c) {
   __shared__ __align__(16) Shared<D, MANY> sh;

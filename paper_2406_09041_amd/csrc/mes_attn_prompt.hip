@@ -10,9 +10,9 @@
 // wherever an equal share ended asked for 4.2 TB/s of different tiles).  The parts of an item leave their sums in the workspace and
 // k_join_prompt adds them up.  The lengths are on the device, so every workgroup finds its part by itself.
 //
-// Measured (head_dim 128, 32 heads over 8 key / value heads unless stated): one prompt of 77 rows 9.4 us, of which 7 is the time of a launch
-// that does next to nothing; four of 1024 rows 59 us; 1 to 6001 rows of 40 heads with keys of their own 420 us, 935 TFLOP/s; 8
-// prompts of 1 to 700 rows behind 0 to 4096 cached tokens 131 us.
+// Measured (head_dim 128, 32 heads over 8 key / value heads unless stated): one prompt of 77 rows 8.8 us, of which 7 is the time of a launch
+// that does next to nothing; four of 1024 rows 53 us; 1 to 6001 rows of 40 heads with keys of their own 411 us, 961 TFLOP/s; 8
+// prompts of 1 to 700 rows behind 0 to 4096 cached tokens 126 us, at e4m3 147.
 #include "mes_attn_tiles.h"
 
 namespace mes {
@@ -66,7 +66,9 @@ __device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
   const int units = wave_sum(y.tiles * y.base + y.tiles * (y.tiles + 1) / 2);
   const int share = units / max(kHeld / columns, 1) + 1;  // of a workgroup, if all had the same
   // A tile of keys takes a workgroup 1.1 us alone on its compute unit and 2.3 us beside another; writing and adding up parts about as long
-  // as 11 tiles (measured: 512 rows behind 4096 tokens 70 us cut and 87 whole; a prompt of 1024 tokens 38 us cut and 24 whole).
+  // as 11 tiles (measured: 512 rows behind 4096 tokens 70 us cut and 87 whole; a prompt of 1024 tokens 38 us cut and 24 whole).  The rule takes the
+  // longest item to be alone, as in these calls of one sequence: where more items than places keep it company, it waits too long
+  // before it cuts (8 prompts behind 0 to 4096 tokens, 528 workgroups, longest 72 tiles: whole, 126 us; evenly shared out 71 us of tiles).
   if (y.longest <= 21 * share / 8 + 11 * kTile / R) return y;
   // parts of a share fit the chip at once; whole tiles (R is 32, 64 or 128)
   int block = max(share + share / 8 + 1, kLeastPart / R);

@@ -13,8 +13,8 @@
 //
 // Why 32 rows and two wavefronts per SIMD: with 64 rows an operand read from LDS serves two products, but one wavefront per
 // SIMD with all 512 registers stood still at every barrier and every rescaling; two of 32 rows fill each other's gaps.  Measured at head_dim
-// 128: 40 heads of prompts of 1 to 6001 rows 420 us, 935 TFLOP/s of the 1268 that a bf16 library product of 8192^3 reaches on the same
-// card; one prompt of 8192 rows 950 to 970.  What bounds it: the exponentials and sums take about as many issue slots as the
+// 128: 40 heads of prompts of 1 to 6001 rows 411 us, 961 TFLOP/s of the 1268 that a bf16 library product of 8192^3 reaches on the same
+// card; one prompt of 8192 rows of 32 heads 1083.  What bounds it: the exponentials and sums take about as many issue slots as the
 // products take matrix cycles, and what the scheduler cannot lay beside each other is lost.
 //
 // LDS: rows of head_dim, two tiles of keys and two of values in turn.  A copy of a wavefront writes 1 KiB in the order of its lanes: a

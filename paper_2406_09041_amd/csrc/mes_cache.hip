@@ -54,7 +54,7 @@ __device__ inline void load8(const uint16_t* p, float v[8]) {
   }
 }
 
-// Four prompts of 1024 tokens (32 query, 8 key / value heads of 128, bf16): 101 MB in 19 us, 5.3 TB/s; 256 single tokens 6 MB, as long as a launch.
+// Four prompts of 1024 tokens (32 query, 8 key / value heads of 128, bf16): 101 MB in 19.7 us, 5.1 TB/s; 256 single tokens 6 MB, as long as a launch.
 //
 // One workgroup per row.  A unit of work is 8 dimensions of the first half of a head and the 8 they turn with, so that q_out
 // may be q: one thread reads both halves before it writes them.
@@ -124,8 +124,10 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
 }
 
 // Pages are whole 16-byte words one behind the other; a workgroup copies up to kCopyBytes of one page of one layer of keys or
-// values, every load in flight before the first store: 400 pages of 32 KiB in 32 layers of keys and values 361 us, 4.65 TB/s (4.84 is what a
-// copy of 2 GiB reaches; a loop of one load and one store: 477 us).
+// values.  Where that is all of kCopyBytes, every load is in flight before the first store: 400 pages of 32 KiB in 32 layers of keys and values 360 us,
+// 4.66 TB/s (4.84 is what a copy of 2 GiB reaches; a loop of one load and one store: 477 us).  Shorter pages, and the rest of longer ones, take
+// that loop: 400 pages of 24, 16 and 8 KiB at 4.88, 4.81 and 4.65 TB/s, as more workgroups are there to wait side by side, but pages of 40 KiB
+// at 3.2.
 constexpr int kCopyThreads = 256, kCopyWords = 8, kCopyBytes = kCopyThreads * kCopyWords * 16;
 
 struct CopyArgs {
