@@ -322,15 +322,23 @@ mes_status mes_step_adamw(float* step, const float* grad, float* m, float* v, in
  * The cache: k and v are [n_layers][n_pages][n_kv_heads][page_tokens][head_dim], page_tokens 16, 32, 64, 128 or 256, 16-byte
  * aligned.  MES_KV_BF16: bf16.  MES_KV_E4M3: 8-bit floating point (4 exponent, 3 mantissa bits, largest value 448), value =
  * code * scale with one fp32 scale per layer and head, k_scale and v_scale [n_layers][n_kv_heads] (NULL for bf16): any finite
- * numbers (the values of a head whose scale is 0 are 0). */
-enum { MES_KV_BF16 = 0, MES_KV_E4M3 = 1 };
+ * numbers (the values of a head whose scale is 0 are 0).
+ * MES_KV_E4M3_BLOCKS: the same codes, value = code * 2^(x - 127) with one byte x per block of MES_KV_BLOCK tokens of a page and head,
+ * k_exponent and v_exponent [n_layers][n_pages][n_kv_heads][page_tokens / MES_KV_BLOCK].  mes_kv_append finds and writes it: nothing has to
+ * be known about the values beforehand, and none is clamped because another was smaller.  Bytes that it writes lie in
+ * [MES_KV_LEAST_EXPONENT, MES_KV_MOST_EXPONENT], so that every value but the largest codes of the largest exponent is a normal bf16; others
+ * count as the nearer end. */
+enum { MES_KV_BF16 = 0, MES_KV_E4M3 = 1, MES_KV_E4M3_BLOCKS = 3 };
 #define MES_MAX_SEQS 2048
+#define MES_KV_BLOCK 16
+#define MES_KV_LEAST_EXPONENT 10
+#define MES_KV_MOST_EXPONENT 247
 typedef struct {           /* HOST struct; pointers DEVICE, caller-owned */
   int32_t n_layers, n_pages, page_tokens, n_kv_heads, head_dim, dtype;
   void* k;
   void* v;
-  const float* k_scale;
-  const float* v_scale;
+  union { const float* k_scale; uint8_t* k_exponent; };   /* MES_KV_E4M3; MES_KV_E4M3_BLOCKS */
+  union { const float* v_scale; uint8_t* v_exponent; };
 } mes_kv;
 
 /* The sequences of a call (HOST struct; pointers DEVICE, so that a captured graph can be replayed while they grow).
@@ -353,6 +361,10 @@ typedef struct {
  * the first half turns with element i of the second: (a c - b s, b c + a s), every product and sum rounded to fp32, the
  * result once to bf16 (q_out; may be q) or to the cache's type (e4m3: after division by the scale, to nearest even,
  * clamped to +-448; 0 stays 0 where the scale is 0).  rotary NULL: keys are written as they are and q must be NULL.
+ * MES_KV_E4M3_BLOCKS: a block gets the least exponent under which the finite ones of its new values are at most 448 codes; where it holds
+ * tokens of the sequence before the call's first, their exponent, if that is larger, and where it is smaller their codes
+ * are rounded to the new one (exactly, but for codes that become subnormal).  What is infinite becomes the largest code
+ * (240 under the largest exponent, so that its value is finite), NaN stays NaN.  What a block held behind the new tokens is lost.
  * Rows without a place (see mes_seqs) are left out: nothing is written for rows before position 0, past the table's room
  * or behind the last sequence; on a page outside the cache only q_out is.  Two rows of one call must not share a place. */
 mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
@@ -362,6 +374,51 @@ mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, cons
 mes_status mes_kv_append_fresh(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
                                int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
                                int ld_q_out, void* stream);
+
+/* Rotary positions in their other forms.  Position p turns pair i of the first `dims` dimensions of a head by the angle that row p of the table
+ * has the cosine and sine of: (a c - b s, b c + a s); the dimensions behind are left as they are.  MES_ROTARY_HALVES: pair i is
+ * (i, i + dims / 2), as in mes_kv_append; MES_ROTARY_PAIRS: neighbours, (2 i, 2 i + 1).  dims: a multiple of 16, at most head_dim. */
+enum { MES_ROTARY_HALVES = 0, MES_ROTARY_PAIRS = 1 };
+typedef struct {           /* HOST struct */
+  const float* table;      /* DEVICE fp32 [n_positions][2][dims / 2], cosines then sines, 16-byte aligned */
+  int32_t n_positions, dims, layout;
+} mes_angles;
+
+/* mes_kv_append with angles of any form (NULL: keys are written as they are, q must be NULL).  fresh: 0, or 1 as in mes_kv_append_fresh. */
+mes_status mes_kv_append_angles(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                                int n_heads, int ld_q, int ld_k, int ld_v, const mes_angles* angles, void* q_out, int ld_q_out,
+                                int fresh, void* stream);
+
+/* Fills a table: row p has cos(p f_i) and sin(p f_i), i < dims / 2, times magnitude; angles in fp64, rounded once.  f_i = base^(-2 i / dims),
+ * for contexts longer than those trained at (factor >= 1) changed to
+ *   MES_SCALING_LINEAR  f_i / factor: positions are interpolated
+ *   MES_SCALING_BASE    that of the base base * factor^(dims / (dims - 2)): the slowest dimension as with LINEAR, the fastest unchanged
+ *   MES_SCALING_BANDS   f_i (g + (1 - g) / factor), g = (context f_i / 2 pi - low) / (high - low) inside [0, 1]: dimensions that turn `high`
+ *                       times or more over the trained context stay, those that turn `low` times or fewer are interpolated
+ * n_positions in [0, 2^26], dims a multiple of 16 up to 512, base > 0, magnitude finite; factor >= 1 where it is used; BANDS: context >= 1,
+ * 0 <= low < high. */
+enum { MES_SCALING_NONE = 0, MES_SCALING_LINEAR = 1, MES_SCALING_BASE = 2, MES_SCALING_BANDS = 3 };
+mes_status mes_rotary_table(float* table, int n_positions, int dims, double base, int scaling, double factor, int context, double low,
+                            double high, double magnitude, void* stream);
+
+/* Turns rows outside a cache (what mes_attn_prompt takes): q [T][n_heads][head_dim] to q_out and, where k is not NULL, k
+ * [T][n_kv_heads][head_dim] to k_out, row t by the angles of positions[t] (DEVICE int32 [T]).  Every product and sum is rounded to fp32, the result
+ * once to the rows' type: MES_ROWS_BF16 or MES_ROWS_FP32.  transpose: 1 turns back by the same cosines and sines, (a c + b s, b c - a s): the
+ * gradient of the rows where `q` and `k` are those of the turned rows.  q_out may be q, k_out k (rows as far apart).
+ * head_dim: a multiple of 16 up to 512.  Rows ld_* elements apart, 16-byte aligned, as for the attention calls.
+ * Rows whose position is outside the table (-1: one that pads the batch) are left as they are in q_out / k_out, with fresh = 1 (outputs that
+ * are not the inputs and whose memory holds nothing yet) set to 0. */
+enum { MES_ROWS_BF16 = 0, MES_ROWS_FP32 = 1 };
+mes_status mes_rotary(const mes_angles* angles, const int32_t* positions, const void* q, const void* k, int T, int n_heads, int n_kv_heads,
+                      int head_dim, int ld_q, int ld_k, int dtype, int transpose, void* q_out, int ld_q_out, void* k_out, int ld_k_out,
+                      int fresh, void* stream);
+
+/* Reads tokens back: row t of sequence s, numbered as in mes_kv_append, gets the keys and values of its position in bf16
+ * (e4m3: code times scale, rounded once; blocks: the value itself) in k, v [T][n_kv_heads][head_dim], rows ld_* apart, which overlap
+ * neither each other nor the cache.  Either may be NULL.  Rows of a sequence whose token is absent (see mes_seqs) or before position 0 are set
+ * to 0; rows behind the last sequence are left as they are, with fresh = 1 set to 0. */
+mes_status mes_kv_read(const mes_kv* kv, int layer, const mes_seqs* seqs, int T, void* k, void* v, int ld_k, int ld_v, int fresh,
+                       void* stream);
 
 /* Attention over whole prompts: n_seqs sequences packed one after the other, rows seq_offsets[s] .. seq_offsets[s+1]
  * (DEVICE int32 [n_seqs + 1], 0 = o[0] <= ... <= o[n_seqs] <= T; rows behind are left as they are), every row sees the
@@ -395,7 +452,7 @@ mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, co
                            int n_experts, const int32_t* seg_offsets, const int32_t* prefix_len, float scale, void* out,
                            int ld_out, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Copies n pages, page src[i] to page dst[i], in all layers of keys and values.  src, dst: HOST int32 [n], inside [0,
+/* Copies n pages, page src[i] to page dst[i], in all layers of keys and values (their blocks' exponents with them).  src, dst: HOST int32 [n], inside [0,
  * n_pages); no page may be written twice, or both read and written (MES_ERR_PAGES). */
 mes_status mes_kv_copy_pages(const mes_kv* kv, const int32_t* src, const int32_t* dst, int n, void* stream);
 

@@ -8,6 +8,6 @@ from .binding import (  # noqa: F401
     base_bytes, codes_bytes, linear_workspace_bytes, make_workspace, mes_delta_linear, mes_pack_base,
     mes_pack_delta, mes_select_salient, mes_unpack_base, mes_unpack_delta, salient_bytes, DeltaLinearMulti, KernelTimer,
     mes_copy_probe, ExpertPool, mes_delta_linear_descriptors, mes_delta_linear_multi_descriptors, StepGrad, mes_step_adamw,
-    mes_delta_linear_noalloc, DeltaLinearGated, KV_BF16, KV_E4M3, AttnDecode, KvCache, PagePool, SeqBatch, mes_attn_extend,
-    mes_attn_prompt, mes_kv_append, mes_kv_copy_pages, prompt_workspace, rotary_table,
+    mes_delta_linear_noalloc, DeltaLinearGated, KV_BF16, KV_E4M3, KV_E4M3_BLOCKS, Angles, AttnDecode, KvCache, PagePool, SeqBatch, mes_attn_extend,
+    mes_attn_prompt, mes_kv_append, mes_kv_copy_pages, mes_kv_read, mes_rotary, mes_rotary_table, prompt_workspace, rotary_table,
 )

@@ -21,7 +21,10 @@ GRID_SYM, GRID_EQ1 = 0, 1
 STEP_GIVEN, STEP_MAXABS, STEP_MEANABS = 0, 1, 2
 MAX_EXPERTS = 64
 
-KV_BF16, KV_E4M3 = 0, 1
+KV_BF16, KV_E4M3, KV_E4M3_BLOCKS = 0, 1, 3
+KV_BLOCK, LEAST_EXPONENT = 16, 10      # tokens of a block; the least exponent byte that is written
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+SCALINGS = {None: 0, "linear": 1, "base": 2, "bands": 3}
 MAX_SEQS = 2048
 SHORT_PROMPT = 704          # keys, 11 tiles of 64: the library never shares out rows that see no more, and needs no workspace for them
 
@@ -40,7 +43,7 @@ EXPORTS = ["mes_base_bytes", "mes_codes_bytes", "mes_salient_bytes", "mes_pack_w
            "mes_step_grad_workspace_bytes", "mes_step_grad", "mes_step_adamw", "mes_noalloc_scratch_bytes",
            "mes_delta_linear_noalloc", "mes_long_segment_tokens",
            "mes_kv_append", "mes_kv_append_fresh", "mes_attn_prompt", "mes_attn_prompt_workspace_bytes", "mes_attn_extend", "mes_attn_decode_workspace_bytes", "mes_attn_decode",
-           "mes_kv_copy_pages", "mes_pages_create", "mes_pages_destroy", "mes_pages_grow", "mes_pages_fork", "mes_pages_free",
+           "mes_kv_append_angles", "mes_rotary_table", "mes_rotary", "mes_kv_read", "mes_kv_copy_pages", "mes_pages_create", "mes_pages_destroy", "mes_pages_grow", "mes_pages_fork", "mes_pages_free",
            "mes_pages_compact", "mes_pages_table", "mes_pages_length", "mes_pages_unused"]
 
 
@@ -64,6 +67,10 @@ class mes_linear(ctypes.Structure):
 class mes_kv(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_pages", "page_tokens", "n_kv_heads", "head_dim", "dtype")] + \
                [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class mes_angles(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("n_positions", "dims", "layout")]
 
 
 class mes_seqs(ctypes.Structure):
@@ -167,6 +174,12 @@ def _load() -> ctypes.CDLL:
     kvp, sqp, fl = ctypes.POINTER(mes_kv), ctypes.POINTER(mes_seqs), ctypes.c_float
     lib.mes_kv_append.restype = lib.mes_kv_append_fresh.restype = c_int
     lib.mes_kv_append.argtypes = lib.mes_kv_append_fresh.argtypes = [kvp, c_int, sqp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, vp, c_int, vp, c_int, vp]
+    anp, db = ctypes.POINTER(mes_angles), ctypes.c_double
+    lib.mes_kv_append_angles.restype = lib.mes_rotary_table.restype = lib.mes_rotary.restype = lib.mes_kv_read.restype = c_int
+    lib.mes_kv_append_angles.argtypes = [kvp, c_int, sqp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, anp, vp, c_int, c_int, vp]
+    lib.mes_rotary_table.argtypes = [vp, c_int, c_int, db, c_int, db, c_int, db, db, db, vp]
+    lib.mes_rotary.argtypes = [anp, vp, vp, vp, c_int, c_int, c_int, c_int, c_int, c_int, c_int, c_int, vp, c_int, vp, c_int, c_int, vp]
+    lib.mes_kv_read.argtypes = [kvp, c_int, sqp, c_int, vp, vp, c_int, c_int, c_int, vp]
     lib.mes_attn_prompt.restype = c_int
     lib.mes_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, vp, c_int, c_int, c_int, c_int, c_int, c_int, fl, vp, c_int, vp, c_sz, vp]
     lib.mes_attn_prompt_workspace_bytes.restype = c_sz
@@ -592,13 +605,13 @@ def _call_on(index: int, entry, *args) -> None:
         _check(status)
 
 
-def _rows(name: str, t: torch.Tensor, index: int):
-    """Checks rows [T, heads, head_dim] of bf16 on device `index` whose heads lie one behind the other: T, heads, head_dim, and how
-    far rows are apart."""
+def _rows(name: str, t: torch.Tensor, index: int, dtype: torch.dtype = _BF16):
+    """Checks rows [T, heads, head_dim] of bf16 (or another type) on device `index` whose heads lie one behind the other: T, heads,
+    head_dim, and how far rows are apart."""
     n, heads, dim = t.shape
     step, head, one = t.stride()
-    assert t.dtype is _BF16 and t.get_device() == index and (one == 1 or dim == 1) and (head == dim or heads == 1), \
-        f"{name}: bf16 [T, heads, head_dim] on device {index}, the heads of a row one behind the other"
+    assert t.dtype is dtype and t.get_device() == index and (one == 1 or dim == 1) and (head == dim or heads == 1), \
+        f"{name}: {dtype} [T, heads, head_dim] on device {index}, the heads of a row one behind the other"
     return n, heads, dim, step if n > 1 else heads * dim
 
 
@@ -608,14 +621,19 @@ def _int32_on(name: str, t: torch.Tensor, index: int) -> None:
 
 class KvCache:
     """A paged cache of keys and values for all layers of a model (mes_kv in mes.h): k and v are
-    [n_layers, n_pages, n_kv_heads, page_tokens, head_dim], bf16, or float8_e4m3fn with one fp32 scale per layer and head."""
+    [n_layers, n_pages, n_kv_heads, page_tokens, head_dim], bf16, or float8_e4m3fn with k_scale and v_scale: one fp32 scale per layer and
+    head (KV_E4M3), or exponents of blocks of 16 tokens, float8_e8m0fnu [n_layers, n_pages, n_kv_heads, page_tokens / 16]
+    (KV_E4M3_BLOCKS), which mes_kv_append finds."""
 
     def __init__(self, n_layers: int, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, dtype: int = KV_BF16,
                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, device="cuda:0"):
         shape = (n_layers, n_pages, n_kv_heads, page_tokens, head_dim)
-        kind = torch.float8_e4m3fn if dtype == KV_E4M3 else torch.bfloat16
-        self._set(torch.zeros(shape, dtype=torch.uint8 if dtype == KV_E4M3 else kind, device=device).view(kind),
-                  torch.zeros(shape, dtype=torch.uint8 if dtype == KV_E4M3 else kind, device=device).view(kind), k_scale, v_scale)
+        if dtype == KV_E4M3_BLOCKS:
+            assert k_scale is None and v_scale is None, "a cache of blocks finds its exponents itself"
+            k_scale, v_scale = (torch.full((*shape[:3], page_tokens // KV_BLOCK), LEAST_EXPONENT, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+                                for _ in range(2))
+        kind = torch.bfloat16 if dtype == KV_BF16 else torch.float8_e4m3fn
+        self._set(*(torch.zeros(shape, dtype=kind if dtype == KV_BF16 else torch.uint8, device=device).view(kind) for _ in range(2)), k_scale, v_scale)
 
     @classmethod
     def over(cls, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
@@ -628,12 +646,15 @@ class KvCache:
         assert k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous() and k.is_cuda and k.device == v.device
         assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn), "a cache is bf16 or float8_e4m3fn"
         fp8 = k.dtype == torch.float8_e4m3fn
+        blocks = fp8 and k_scale is not None and k_scale.dtype == torch.float8_e8m0fnu
         for t in (k_scale, v_scale):
             assert (t is not None) == fp8, "scales belong to an e4m3 cache"
-            assert t is None or (t.dtype == torch.float32 and t.shape == (k.shape[0], k.shape[2]) and t.is_contiguous() and t.device == k.device)
+            kind, shape = (torch.float8_e8m0fnu, (*k.shape[:3], k.shape[3] // KV_BLOCK)) if blocks else (torch.float32, (k.shape[0], k.shape[2]))
+            assert t is None or (t.dtype == kind and t.shape == shape and t.is_contiguous() and t.device == k.device)
         self.k, self.v, self.k_scale, self.v_scale, self.device, self.index = k, v, k_scale, v_scale, k.device, k.get_device()
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
-        self.desc = mes_kv(self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, KV_E4M3 if fp8 else KV_BF16,
+        self.dtype = KV_E4M3_BLOCKS if blocks else KV_E4M3 if fp8 else KV_BF16
+        self.desc = mes_kv(self.n_layers, self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.dtype,
                            k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if fp8 else None, v_scale.data_ptr() if fp8 else None)
         self.ref = ctypes.byref(self.desc)
 
@@ -662,29 +683,110 @@ def rotary_table(n_positions: int, head_dim: int, base: float = 10000.0, device=
     return torch.stack([angle.cos(), angle.sin()], 1).to(device=device, dtype=torch.float32)
 
 
+def mes_rotary_table(n_positions: int, dims: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, context: int = 0,
+                     low: float = 1.0, high: float = 32.0, magnitude: float = 1.0, device="cuda:0", out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Cosines and sines [n_positions, 2, dims / 2], fp32, made on the GPU (mes_rotary_table in mes.h).  scaling, for contexts `factor` times
+    as long as trained at: None, "linear", "base", or "bands" (dimensions that turn `high` times or more over the trained `context` stay as
+    they are, those that turn `low` times or fewer are stretched).  magnitude: multiplies all of it."""
+    assert scaling in SCALINGS, f"scaling = {scaling!r}: None, 'linear', 'base' or 'bands'"
+    if out is None:
+        out = torch.empty((max(n_positions, 0), 2, max(dims, 0) // 2), dtype=torch.float32, device=device)
+    assert out.is_cuda and out.dtype is torch.float32 and out.is_contiguous() and out.shape == (n_positions, 2, dims // 2)
+    _call_on(out.get_device(), lib.mes_rotary_table, out.data_ptr(), n_positions, dims, base, SCALINGS[scaling], factor, context, low, high, magnitude)
+    return out
+
+
+class Angles:
+    """Rotary angles (mes_angles in mes.h): table fp32 [n_positions, 2, dims / 2] as from mes_rotary_table or rotary_table, dims of them turned, where
+    dimension i turns with i + dims / 2, or (interleaved) 2 i with 2 i + 1."""
+
+    def __init__(self, table: torch.Tensor, interleaved: bool = False):
+        assert table.is_cuda and table.dtype is torch.float32 and table.is_contiguous() and table.dim() == 3 and table.shape[1] == 2
+        self.table, self.index, self.dims = table, table.get_device(), 2 * table.shape[2]
+        self.desc = mes_angles(table.data_ptr(), table.shape[0], self.dims, ROTARY_PAIRS if interleaved else ROTARY_HALVES)
+        self.ref = ctypes.byref(self.desc)
+
+
+def mes_rotary(angles: Angles, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               k_out: Optional[torch.Tensor] = None, transpose: bool = False):
+    """Turns rows q [T, heads, d] and k [T, kv heads, d], bf16 or fp32, by the angles of positions int32 [T]; returns (q_out, k_out), or q_out
+    where there is no k (q_out may be q, k_out k).  transpose: turns back, which takes gradients of turned rows to those of the rows.
+    Rows whose position is outside the table (-1) are left as they are in outputs that are given, and 0 where these are allocated."""
+    index, kind = q.get_device(), q.dtype
+    assert kind in (_BF16, torch.float32) and q.is_cuda and angles.index == index, "rows are bf16 or fp32, on the angles' device"
+    T, heads, dim, ld_q = _rows("q", q, index, kind)
+    _int32_on("positions", positions, index)
+    assert positions.shape == (T,), f"positions: int32 [{T}]"
+    assert (k is None) <= (k_out is None) and (k is None or (q_out is None) == (k_out is None)), "give both of q_out and k_out or neither"
+    kv_heads = ld_k = ld_ko = 0
+    fresh = q_out is None
+    if fresh:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    n, h, d, ld_qo = _rows("q_out", q_out, index, kind)
+    assert (n, h, d) == (T, heads, dim)
+    if k is not None:
+        n, kv_heads, d, ld_k = _rows("k", k, index, kind)
+        assert (n, d) == (T, dim), "k: as many rows as q"
+        if fresh:
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        n, h, d, ld_ko = _rows("k_out", k_out, index, kind)
+        assert (n, h, d) == (T, kv_heads, dim)
+    _call_on(index, lib.mes_rotary, angles.ref, positions.data_ptr(), q.data_ptr(), None if k is None else k.data_ptr(), T, heads, kv_heads, dim, ld_q, ld_k,
+             0 if kind is _BF16 else 1, int(transpose), q_out.data_ptr(), ld_qo, None if k is None else k_out.data_ptr(), ld_ko, int(fresh))
+    return q_out if k is None else (q_out, k_out)
+
+
 def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
-                  rotary: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
-    """Rotates the new rows' queries (returned; q_out may be q) and keys and puts keys and values into the cache's pages.  Rows without a
-    position are left as they are in a q_out that is given, and 0 where it is allocated."""
-    index, entry = cache.index, lib.mes_kv_append
+                  rotary=None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Rotates the new rows' queries (returned; q_out may be q) and keys and puts keys and values into the cache's pages.  rotary: a table
+    [n, 2, head_dim / 2] (rotary_table), Angles of any form, or None.  Rows without a position are left as they are in a q_out that is given, and 0
+    where it is allocated."""
+    index = cache.index
     T, kv_heads, dim, ld_k = _rows("k", k, index)
     rows_v = _rows("v", v, index)
     assert batch.index == index and rows_v[:3] == (T, kv_heads, dim) == (T, cache.n_kv_heads, cache.head_dim), "k, v: [T, n_kv_heads, head_dim] of the cache"
     heads = ld_q = ld_o = n_pos = 0
     rot = src = dst = None
-    if rotary is not None:
+    fresh = False
+    if isinstance(rotary, Angles):
+        assert rotary.index == index, f"angles on device {index}"
+        rot = rotary.ref
+    elif rotary is not None:
         assert rotary.dtype is torch.float32 and rotary.is_contiguous() and rotary.get_device() == index and rotary.shape[1:] == (2, dim // 2)
         n_pos, rot = rotary.shape[0], rotary.data_ptr()
     if q is not None:
         n, heads, d, ld_q = _rows("q", q, index)
         assert n == T and d == dim
         if q_out is None:
-            q_out, entry = torch.empty_like(q, memory_format=torch.contiguous_format), lib.mes_kv_append_fresh
+            q_out, fresh = torch.empty_like(q, memory_format=torch.contiguous_format), True
         n, h, d, ld_o = _rows("q_out", q_out, index)
         assert (n, h, d) == (T, heads, dim)
         src, dst = q.data_ptr(), q_out.data_ptr()
-    _call_on(index, entry, cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3], rot, n_pos, dst, ld_o)
+    rows = (cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3])
+    if isinstance(rotary, Angles):
+        _call_on(index, lib.mes_kv_append_angles, *rows, rot, dst, ld_o, int(fresh))
+    else:
+        _call_on(index, lib.mes_kv_append_fresh if fresh else lib.mes_kv_append, *rows, rot, n_pos, dst, ld_o)
     return q_out if q is not None else None
+
+
+def mes_kv_read(cache: KvCache, layer: int, batch: SeqBatch, T: int, k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """Reads the tokens of the batch's T rows (the last tokens of their sequences, as in mes_kv_append) back: k, v bf16 [T, kv heads, head_dim].  Given
+    one of k_out and v_out, only that is read.  Rows of a sequence whose token is absent are 0; rows behind the last
+    sequence are left as they are in outputs that are given, and 0 where these are allocated."""
+    index = cache.index
+    assert batch.index == index
+    fresh = k_out is None and v_out is None
+    if fresh:
+        k_out, v_out = (torch.empty((max(T, 0), cache.n_kv_heads, cache.head_dim), dtype=_BF16, device=cache.device) for _ in range(2))
+    ld = [0, 0]
+    for i, t in enumerate((k_out, v_out)):
+        if t is not None:
+            *shape, ld[i] = _rows("k_out / v_out", t, index)
+            assert shape == [T, cache.n_kv_heads, cache.head_dim], "k_out, v_out: [T, n_kv_heads, head_dim] of the cache"
+    _call_on(index, lib.mes_kv_read, cache.ref, layer, batch.ref, T, None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(),
+             *ld, int(fresh))
+    return k_out, v_out
 
 
 def _scratch(workspace: Optional[torch.Tensor], index: int):

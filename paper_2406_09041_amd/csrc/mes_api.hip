@@ -314,7 +314,7 @@ static mes_status check_rows(const char* who, const char* what, const void* p, i
 
 static mes_status check_kv(const char* who, const mes_kv* kv, int layer) {
   if (!kv) return fail(MES_ERR_NULL, "%s: kv is null", who);
-  if (kv->dtype != MES_KV_BF16 && kv->dtype != MES_KV_E4M3) return fail(MES_ERR_BITS, "%s: unknown cache type %d", who, kv->dtype);
+  if (kv->dtype != MES_KV_BF16 && kv->dtype != MES_KV_E4M3 && kv->dtype != MES_KV_E4M3_BLOCKS) return fail(MES_ERR_BITS, "%s: unknown cache type %d", who, kv->dtype);
   if (kv->n_layers < 1 || kv->n_pages < 1) return fail(MES_ERR_SHAPE, "%s: n_layers = %d, n_pages = %d must be positive", who, kv->n_layers, kv->n_pages);
   if (kv->page_tokens < 16 || kv->page_tokens > 256 || (kv->page_tokens & (kv->page_tokens - 1)))
     return fail(MES_ERR_SHAPE, "%s: page_tokens must be 16, 32, 64, 128 or 256 (got %d)", who, kv->page_tokens);
@@ -322,6 +322,7 @@ static mes_status check_kv(const char* who, const mes_kv* kv, int layer) {
   if (!kv->k || !kv->v) return fail(MES_ERR_NULL, "%s: the cache's k / v is null", who);
   if (!aligned16(kv->k) || !aligned16(kv->v)) return fail(MES_ERR_ALIGN, "%s: the cache must be 16-byte aligned", who);
   if (kv->dtype == MES_KV_E4M3 && (!kv->k_scale || !kv->v_scale)) return fail(MES_ERR_NULL, "%s: an e4m3 cache needs k_scale and v_scale", who);
+  if (kv->dtype == MES_KV_E4M3_BLOCKS && (!kv->k_exponent || !kv->v_exponent)) return fail(MES_ERR_NULL, "%s: a cache of blocks needs k_exponent and v_exponent", who);
   if (layer < 0 || layer >= kv->n_layers) return fail(MES_ERR_SHAPE, "%s: layer %d outside [0, %d)", who, layer, kv->n_layers);
   return MES_OK;
 }
@@ -337,13 +338,27 @@ static mes_status check_seqs(const char* who, const mes_kv* kv, const mes_seqs* 
 }
 
 static size_t kv_layer_bytes(const mes_kv& kv) {
-  return (size_t)kv.n_pages * kv.n_kv_heads * kv.page_tokens * kv.head_dim * (kv.dtype == MES_KV_E4M3 ? 1 : 2);
+  return (size_t)kv.n_pages * kv.n_kv_heads * kv.page_tokens * kv.head_dim * (kv.dtype == MES_KV_BF16 ? 2 : 1);
 }
+// first exponent of a layer, of k_exponent or v_exponent
+static uint8_t* layer_exponents(const mes_kv& kv, uint8_t* of, int layer) {
+  return of + (size_t)layer * kv.n_pages * kv.n_kv_heads * (kv.page_tokens / MES_KV_BLOCK);
+}
+static int source_of(const mes_kv& kv) { return kv.dtype == MES_KV_BF16 ? KV_PAGED : kv.dtype == MES_KV_E4M3 ? KV_PAGED_E4M3 : KV_PAGED_BLOCKS; }
 static int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
 
+static mes_status check_angles(const char* who, const mes_angles& g, int head_dim) {
+  if (!g.table) return fail(MES_ERR_NULL, "%s: the table of angles is null", who);
+  if (!aligned16(g.table)) return fail(MES_ERR_ALIGN, "%s: the table of angles must be 16-byte aligned", who);
+  if (g.dims < 16 || g.dims % 16 || g.dims > head_dim) return fail(MES_ERR_SHAPE, "%s: dims = %d: a multiple of 16 up to head_dim = %d", who, g.dims, head_dim);
+  if (g.n_positions < 0) return fail(MES_ERR_SHAPE, "%s: n_positions = %d", who, g.n_positions);
+  if (g.layout != MES_ROTARY_HALVES && g.layout != MES_ROTARY_PAIRS) return fail(MES_ERR_SHAPE, "%s: unknown layout %d", who, g.layout);
+  return MES_OK;
+}
+
 static mes_status append(const char* who, bool fresh, const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
-                         int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
-                         int ld_q_out, void* stream) {
+                         int n_heads, int ld_q, int ld_k, int ld_v, const mes_angles* angles, void* q_out, int ld_q_out, void* stream) {
+  const float* rotary = angles ? angles->table : nullptr;
   if (mes_status st = check_kv(who, kv, layer)) return st;
   if (mes_status st = check_seqs(who, kv, seqs, false)) return st;
   if (mes_status st = check_row_count(who, T)) return st;
@@ -362,26 +377,142 @@ static mes_status append(const char* who, bool fresh, const mes_kv* kv, int laye
     if (q == q_out && ld_q != ld_q_out) return fail(MES_ERR_SHAPE, "%s: q_out is q with rows %d apart instead of %d", who, ld_q_out, ld_q);
   }
   const int capacity = seqs->n_seqs ? seqs->table_pages * kv->page_tokens : 0;   // no sequences: the table is not looked at
-  if (rotary) {
-    if (!aligned16(rotary)) return fail(MES_ERR_ALIGN, "%s: rotary must be 16-byte aligned", who);
-    if (n_positions < capacity) return fail(MES_ERR_SHAPE, "%s: rotary has %d positions, the page table has room for %d", who, n_positions, capacity);
+  if (angles) {
+    if (mes_status st = check_angles(who, *angles, kv->head_dim)) return st;
+    if (angles->n_positions < capacity)
+      return fail(MES_ERR_SHAPE, "%s: rotary has %d positions, the page table has room for %d", who, angles->n_positions, capacity);
   }
-  AppendArgs a{(const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, rotary, (uint16_t*)q_out, kv->k, kv->v, kv->k_scale, kv->v_scale,
-               seqs->q_offsets, seqs->kv_len, seqs->page_table, layer, kv->n_pages, log2_of(kv->page_tokens), n_heads, kv->n_kv_heads,
-               kv->head_dim, seqs->n_seqs, seqs->table_pages, capacity, ld_q, ld_k, ld_v, ld_q_out, fresh};
-  return check_hip(launch_append(a, T, kv->dtype == MES_KV_E4M3, (hipStream_t)stream), who);
+  AppendArgs a{};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.q_out = (uint16_t*)q_out;
+  a.rotary = rotary;
+  if (angles) { a.dims = angles->dims; a.pairs = angles->layout == MES_ROTARY_PAIRS; }
+  a.k_cache = kv->k; a.v_cache = kv->v;
+  if (kv->dtype == MES_KV_E4M3) { a.k_scale = kv->k_scale; a.v_scale = kv->v_scale; }
+  if (kv->dtype == MES_KV_E4M3_BLOCKS) { a.k_exponent = layer_exponents(*kv, kv->k_exponent, layer); a.v_exponent = layer_exponents(*kv, kv->v_exponent, layer); }
+  a.q_offsets = seqs->q_offsets; a.kv_len = seqs->kv_len; a.page_table = seqs->page_table;
+  a.layer = layer; a.n_pages = kv->n_pages; a.page_shift = log2_of(kv->page_tokens); a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads;
+  a.head_dim = kv->head_dim; a.n_seqs = seqs->n_seqs; a.table_pages = seqs->table_pages; a.capacity = capacity;
+  a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_q_out = ld_q_out;
+  a.fresh = fresh;
+  return check_hip(launch_append(a, T, kv->dtype, (hipStream_t)stream), who);
 }
 
 mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
                          int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
                          int ld_q_out, void* stream) {
-  return append("mes_kv_append", false, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, rotary, n_positions, q_out, ld_q_out, stream);
+  const mes_angles angles = {rotary, n_positions, kv ? kv->head_dim : 0, MES_ROTARY_HALVES};
+  return append("mes_kv_append", false, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, rotary ? &angles : nullptr, q_out, ld_q_out, stream);
 }
 
 mes_status mes_kv_append_fresh(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
                                int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
                                int ld_q_out, void* stream) {
-  return append("mes_kv_append_fresh", true, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, rotary, n_positions, q_out, ld_q_out, stream);
+  const mes_angles angles = {rotary, n_positions, kv ? kv->head_dim : 0, MES_ROTARY_HALVES};
+  return append("mes_kv_append_fresh", true, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, rotary ? &angles : nullptr, q_out, ld_q_out, stream);
+}
+
+mes_status mes_kv_append_angles(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
+                                int n_heads, int ld_q, int ld_k, int ld_v, const mes_angles* angles, void* q_out, int ld_q_out,
+                                int fresh, void* stream) {
+  if (fresh != 0 && fresh != 1) return fail(MES_ERR_SHAPE, "mes_kv_append_angles: fresh = %d", fresh);
+  return append("mes_kv_append_angles", fresh == 1, kv, layer, seqs, q, k, v, T, n_heads, ld_q, ld_k, ld_v, angles, q_out, ld_q_out, stream);
+}
+
+mes_status mes_rotary_table(float* table, int n_positions, int dims, double base, int scaling, double factor, int context, double low,
+                            double high, double magnitude, void* stream) {
+  static const char who[] = "mes_rotary_table";
+  if (n_positions < 0 || n_positions > 1 << 26) return fail(MES_ERR_SHAPE, "%s: n_positions = %d outside [0, %d]", who, n_positions, 1 << 26);
+  if (dims < 16 || dims % 16 || dims > kMostTurned) return fail(MES_ERR_SHAPE, "%s: dims = %d: a multiple of 16 up to %d", who, dims, kMostTurned);
+  if (scaling < MES_SCALING_NONE || scaling > MES_SCALING_BANDS) return fail(MES_ERR_SHAPE, "%s: unknown scaling %d", who, scaling);
+  if (!(base > 0.0) || !std::isfinite(base)) return fail(MES_ERR_SHAPE, "%s: base must be positive and finite", who);
+  if (!std::isfinite(magnitude)) return fail(MES_ERR_SHAPE, "%s: magnitude must be finite", who);
+  if (scaling != MES_SCALING_NONE && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(MES_ERR_SHAPE, "%s: factor must be at least 1 and finite", who);
+  if (scaling == MES_SCALING_BANDS && (context < 1 || !(low >= 0.0) || !(high > low) || !std::isfinite(high)))
+    return fail(MES_ERR_SHAPE, "%s: context must be positive and 0 <= low < high", who);
+  if (n_positions == 0) return MES_OK;
+  if (!table) return fail(MES_ERR_NULL, "%s: table is null", who);
+  if (!aligned16(table)) return fail(MES_ERR_ALIGN, "%s: table must be 16-byte aligned", who);
+  TableArgs a{};
+  a.table = table;
+  a.n_positions = n_positions;
+  a.dims = dims;
+  a.magnitude = magnitude;
+  if (scaling == MES_SCALING_BASE) base *= std::pow(factor, dims / (dims - 2.0));
+  for (int i = 0; i < dims / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / dims);
+    if (scaling == MES_SCALING_LINEAR) f /= factor;
+    if (scaling == MES_SCALING_BANDS) {
+      const double keep = std::min(std::max((context * f / 6.283185307179586 - low) / (high - low), 0.0), 1.0);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    // a frequency that is not finite (a base near 0, to a power) has no angles
+    if (!std::isfinite(f) || f > 1e6) return fail(MES_ERR_SHAPE, "%s: base %g gives dimension %d the frequency %g", who, base, i, f);
+    a.frequency[i] = f;
+  }
+  return check_hip(launch_rotary_table(a, (hipStream_t)stream), who);
+}
+
+mes_status mes_rotary(const mes_angles* angles, const int32_t* positions, const void* q, const void* k, int T, int n_heads, int n_kv_heads,
+                      int head_dim, int ld_q, int ld_k, int dtype, int transpose, void* q_out, int ld_q_out, void* k_out, int ld_k_out,
+                      int fresh, void* stream) {
+  static const char who[] = "mes_rotary";
+  if (!angles) return fail(MES_ERR_NULL, "%s: angles is null", who);
+  if (dtype != MES_ROWS_BF16 && dtype != MES_ROWS_FP32) return fail(MES_ERR_BITS, "%s: unknown type of rows %d", who, dtype);
+  if (transpose != 0 && transpose != 1) return fail(MES_ERR_SHAPE, "%s: transpose = %d", who, transpose);
+  if (fresh != 0 && fresh != 1) return fail(MES_ERR_SHAPE, "%s: fresh = %d", who, fresh);
+  if (head_dim < 16 || head_dim % 16 || head_dim > kMostTurned) return fail(MES_ERR_SHAPE, "%s: head_dim = %d: a multiple of 16 up to %d", who, head_dim, kMostTurned);
+  if (n_heads < 1 || n_heads > 65535 || (k && (n_kv_heads < 1 || n_kv_heads > 65535)))
+    return fail(MES_ERR_SHAPE, "%s: n_heads = %d, n_kv_heads = %d: 1 to 65535", who, n_heads, n_kv_heads);
+  if (mes_status st = check_angles(who, *angles, head_dim)) return st;
+  if (mes_status st = check_row_count(who, T)) return st;
+  if (T == 0) return MES_OK;
+  if (!positions) return fail(MES_ERR_NULL, "%s: positions is null", who);
+  if ((k == nullptr) != (k_out == nullptr)) return fail(MES_ERR_NULL, "%s: give both of k and k_out or neither", who);
+  if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, head_dim)) return st;
+  if (mes_status st = check_rows(who, "q_out", q_out, ld_q_out, n_heads, head_dim)) return st;
+  if (q == q_out && ld_q != ld_q_out) return fail(MES_ERR_SHAPE, "%s: q_out is q with rows %d apart instead of %d", who, ld_q_out, ld_q);
+  if (k) {
+    if (mes_status st = check_rows(who, "k", k, ld_k, n_kv_heads, head_dim)) return st;
+    if (mes_status st = check_rows(who, "k_out", k_out, ld_k_out, n_kv_heads, head_dim)) return st;
+    if (k == k_out && ld_k != ld_k_out) return fail(MES_ERR_SHAPE, "%s: k_out is k with rows %d apart instead of %d", who, ld_k_out, ld_k);
+  }
+  if (fresh && (q == q_out || (k && k == k_out))) return fail(MES_ERR_SHAPE, "%s: fresh outputs are not the inputs", who);
+  RotaryArgs a{};
+  a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out;
+  a.positions = positions; a.table = angles->table;
+  a.T = T; a.n_heads = n_heads; a.n_kv_heads = k ? n_kv_heads : 0; a.head_dim = head_dim;
+  a.ld_q = ld_q; a.ld_k = ld_k; a.ld_q_out = ld_q_out; a.ld_k_out = ld_k_out;
+  a.n_positions = angles->n_positions; a.dims = angles->dims; a.pairs = angles->layout == MES_ROTARY_PAIRS;
+  a.sign = transpose ? -1.0f : 1.0f;
+  a.fresh = fresh == 1;
+  return check_hip(launch_rotary(a, dtype == MES_ROWS_FP32, (hipStream_t)stream), who);
+}
+
+mes_status mes_kv_read(const mes_kv* kv, int layer, const mes_seqs* seqs, int T, void* k, void* v, int ld_k, int ld_v, int fresh,
+                       void* stream) {
+  static const char who[] = "mes_kv_read";
+  if (mes_status st = check_kv(who, kv, layer)) return st;
+  if (mes_status st = check_seqs(who, kv, seqs, false)) return st;
+  if (mes_status st = check_row_count(who, T)) return st;
+  if (fresh != 0 && fresh != 1) return fail(MES_ERR_SHAPE, "%s: fresh = %d", who, fresh);
+  if (!seqs->q_offsets && T > seqs->n_seqs) return fail(MES_ERR_SEGMENTS, "%s: %d rows of %d sequences without q_offsets", who, T, seqs->n_seqs);
+  if (T == 0 || (seqs->n_seqs == 0 && !fresh)) return MES_OK;
+  if (!k && !v) return fail(MES_ERR_NULL, "%s: k and v are null", who);
+  if (k) if (mes_status st = check_rows(who, "k", k, ld_k, kv->n_kv_heads, kv->head_dim)) return st;
+  if (v) if (mes_status st = check_rows(who, "v", v, ld_v, kv->n_kv_heads, kv->head_dim)) return st;
+  if (k == v) return fail(MES_ERR_SHAPE, "%s: k is v", who);
+  ReadArgs a{};
+  a.k_cache = (const char*)kv->k + layer * kv_layer_bytes(*kv);
+  a.v_cache = (const char*)kv->v + layer * kv_layer_bytes(*kv);
+  if (kv->dtype == MES_KV_E4M3) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  if (kv->dtype == MES_KV_E4M3_BLOCKS) { a.k_exponent = layer_exponents(*kv, kv->k_exponent, layer); a.v_exponent = layer_exponents(*kv, kv->v_exponent, layer); }
+  a.k = (uint16_t*)k; a.v = (uint16_t*)v;
+  a.q_offsets = seqs->q_offsets; a.kv_len = seqs->kv_len; a.page_table = seqs->page_table;
+  a.T = T; a.n_pages = kv->n_pages; a.page_shift = log2_of(kv->page_tokens); a.n_kv_heads = kv->n_kv_heads; a.head_dim = kv->head_dim;
+  a.n_seqs = seqs->n_seqs; a.table_pages = seqs->table_pages; a.capacity = seqs->n_seqs ? seqs->table_pages * kv->page_tokens : 0;
+  a.ld_k = ld_k; a.ld_v = ld_v;
+  a.fresh = fresh == 1;
+  return check_hip(launch_read(a, kv->dtype, (hipStream_t)stream), who);
 }
 
 size_t mes_attn_prompt_workspace_bytes(int T, int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
@@ -434,20 +565,20 @@ mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, co
   if (T == 0 || seqs->n_seqs == 0) return MES_OK;
   if (mes_status st = check_rows(who, "q", q, ld_q, n_heads, kv->head_dim)) return st;
   if (mes_status st = check_rows(who, "out", out, ld_out, n_heads, kv->head_dim)) return st;
-  const bool fp8 = kv->dtype == MES_KV_E4M3;
   if (mes_status st = check_prompt_workspace(who, T, seqs->n_seqs, n_heads, kv->n_kv_heads, kv->head_dim, workspace, workspace_bytes)) return st;
   PromptArgs a{};
   a.ws = workspace;
   a.q = (const uint16_t*)q; a.out = (uint16_t*)out;
   a.k = (const uint16_t*)((const char*)kv->k + layer * kv_layer_bytes(*kv));
   a.v = (const uint16_t*)((const char*)kv->v + layer * kv_layer_bytes(*kv));
-  if (fp8) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  if (kv->dtype == MES_KV_E4M3) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  if (kv->dtype == MES_KV_E4M3_BLOCKS) { a.k_exponent = layer_exponents(*kv, kv->k_exponent, layer); a.v_exponent = layer_exponents(*kv, kv->v_exponent, layer); }
   a.q_offsets = seqs->q_offsets; a.kv_len = seqs->kv_len; a.page_table = seqs->page_table;
   a.T = T; a.n_seqs = seqs->n_seqs; a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads; a.head_dim = kv->head_dim;
   a.n_pages = kv->n_pages; a.page_shift = log2_of(kv->page_tokens); a.table_pages = seqs->table_pages;
   a.capacity = seqs->table_pages * kv->page_tokens;
   a.ld_q = ld_q; a.ld_out = ld_out; a.scale = scale;
-  return check_hip(launch_attn_prompt(a, fp8 ? KV_PAGED_E4M3 : KV_PAGED, (hipStream_t)stream), who);
+  return check_hip(launch_attn_prompt(a, source_of(*kv), (hipStream_t)stream), who);
 }
 
 size_t mes_attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim) {
@@ -495,16 +626,16 @@ mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, co
   const size_t need = attn_decode_workspace_bytes(seqs->n_seqs, n_heads, kv->n_kv_heads, kv->head_dim);
   if (!workspace || workspace_bytes < need) return fail(MES_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, need);
   if (!aligned16(workspace)) return fail(MES_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
-  const bool fp8 = kv->dtype == MES_KV_E4M3;
   a.q = (const uint16_t*)q; a.out = (uint16_t*)out;
   a.k = (const char*)kv->k + layer * kv_layer_bytes(*kv);
   a.v = (const char*)kv->v + layer * kv_layer_bytes(*kv);
-  if (fp8) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  if (kv->dtype == MES_KV_E4M3) { a.k_scale = kv->k_scale + (size_t)layer * kv->n_kv_heads; a.v_scale = kv->v_scale + (size_t)layer * kv->n_kv_heads; }
+  if (kv->dtype == MES_KV_E4M3_BLOCKS) { a.k_exponent = layer_exponents(*kv, kv->k_exponent, layer); a.v_exponent = layer_exponents(*kv, kv->v_exponent, layer); }
   a.kv_len = seqs->kv_len; a.page_table = seqs->page_table; a.ws = workspace;
   a.n_seqs = seqs->n_seqs; a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads; a.head_dim = kv->head_dim; a.n_pages = kv->n_pages;
   a.page_shift = log2_of(kv->page_tokens); a.table_pages = seqs->table_pages; a.capacity = seqs->table_pages * kv->page_tokens;
   a.ld_q = ld_q; a.ld_out = ld_out; a.scale = scale;
-  return check_hip(launch_attn_decode(a, fp8, (hipStream_t)stream), who);
+  return check_hip(launch_attn_decode(a, source_of(*kv), (hipStream_t)stream), who);
 }
 
 mes_status mes_kv_copy_pages(const mes_kv* kv, const int32_t* src, const int32_t* dst, int n, void* stream) {

@@ -46,10 +46,10 @@ __device__ __forceinline__ float other_row16(float v) {
   return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
 }
 
-// four e4m3 codes of a word -> four bf16 (exact)
-__device__ __forceinline__ u32x2 widen4(uint32_t w) {
-  const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-  const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+// four e4m3 codes of a word times a power of two -> four bf16 (exact: a block's exponent costs nothing here)
+__device__ __forceinline__ u32x2 widen4(uint32_t w, float power = 1.0f) {
+  const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false);
+  const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true);
   return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 

@@ -81,17 +81,20 @@ struct DecodeCall {
   int pass_base[MES_MAX_EXPERTS];
 };
 
-template <int D, bool FP8>
+constexpr bool has_codes(int source) { return source != KV_PAGED; }
+
+template <int D, int SRC>
 struct Raw {                                        // 32 tokens of keys and values on their way
+  static constexpr bool FP8 = has_codes(SRC);
   static constexpr int VD = D / 16, KC = FP8 ? D / 64 : D / 32, VW = VD * (FP8 ? 1 : 2) / 4;
   u32x4 k[2][KC];
   uint32_t v[8][VW];
 };
 
 // first dimension of the 8 that a lane holds in product c of K Q^T
-template <int D, bool FP8>
+template <int D, int SRC>
 __device__ __forceinline__ int dim_of(int c, int g) {
-  return FP8 ? 64 * (c / 2) + 16 * g + 8 * (c % 2) : 32 * c + 8 * g;
+  return has_codes(SRC) ? 64 * (c / 2) + 16 * g + 8 * (c % 2) : 32 * c + 8 * g;
 }
 
 struct Segment {                                    // a piece of the line
@@ -116,16 +119,18 @@ struct Shared {
 
 // The weighted sum over a piece with up to 16 query rows.  Pieces follow one another without a pause: a wavefront asks for the next piece's
 // first tokens where it would ask for more of this one's, and knows their pages by then.
-template <int D, bool FP8>
+template <int D, int SRC>
 struct Few {
+  static constexpr bool FP8 = has_codes(SRC), SCALED = SRC == KV_PAGED_E4M3, BLOCKS = SRC == KV_PAGED_BLOCKS;
   static constexpr int VD = D / 16, KS = D / 32;
-  typedef Raw<D, FP8> R;
+  typedef Raw<D, SRC> R;
   const DecodeArgs& a;
   int group, lane, wave, col, quad;
   u32x4 q[KS];                                      // Q^T operands
   R raw;                                            // the step that comes next
   int there[2];                                     // its pages
   int pages[2];                                     // of 64 steps of the piece, one step per lane
+  int exponents[2][2];                              // blocks: of keys and values on these pages
 
   __device__ Few(const DecodeArgs& args, int g) : a(args), group(g), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), col(lane & 15), quad(lane >> 4) {}
 
@@ -139,12 +144,25 @@ struct Few {
       pg[h] = first + lane < mine && t < g.to ? table[t >> a.page_shift] : -1;
     }
   }
+  // asked for with the tokens themselves: the pages have to be there
+  __device__ __forceinline__ void look_up_exponents(const Segment& g, int first, const int (&pg)[2]) {
+    if constexpr (BLOCKS) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int t = g.t0 + (4 * (first + lane) + wave) * 32 + 16 * h;
+        const size_t at = block_at((unsigned)pg[h] < (unsigned)a.n_pages ? pg[h] : 0, g.kvh, a.n_kv_heads, a.page_shift, t & ((1 << a.page_shift) - 1));
+        exponents[h][0] = a.k_exponent[at];
+        exponents[h][1] = a.v_exponent[at];
+      }
+    }
+  }
+  __device__ __forceinline__ float power(int h, int kv, int i) const { return power_of(exponent_of(__builtin_amdgcn_readlane(exponents[h][kv], i & 63))); }
   __device__ __forceinline__ void load_q(const Segment& g) {
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
       q[c] = u32x4{0, 0, 0, 0};
       if (col < g.rows)
-        q[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(g.kvh * group + col % group) * D + dim_of<D, FP8>(c, quad));
+        q[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(g.kvh * group + col % group) * D + dim_of<D, SRC>(c, quad));
     }
   }
   __device__ __forceinline__ size_t row_of(const Segment& g, int t, int page) const {   // first element of token t's row
@@ -184,6 +202,7 @@ struct Few {
   __device__ __forceinline__ void start(const Segment& g) {   // a piece that nobody has asked for
     look_up(g, 0, pages);
     load_q(g);
+    look_up_exponents(g, 0, pages);
     raw = R{};
     there[0] = there[1] = -1;
   }
@@ -193,8 +212,8 @@ struct Few {
   // a step is then there before the loads of a whole chip are on their way, behind which it would be fetched (3 to 8 us).
   template <class SH>
   __device__ __forceinline__ void run(const Segment& g, bool fresh, bool ahead, const Segment& then, SH& sh, bool direct, float* o, float2* ml_out) {
-  const float factor = a.scale * kLog2e * (FP8 ? a.k_scale[g.kvh] : 1.0f), scale = FP8 ? factor_of_scores(factor) : factor;
-  if constexpr (FP8) factor_to_query(q, factor);
+  const float factor = a.scale * kLog2e * (SCALED ? a.k_scale[g.kvh] : 1.0f), scale = SCALED ? factor_of_scores(factor) : factor;
+  if constexpr (SCALED) factor_to_query(q, factor);
   f32x4 acc[VD];
   float m = -INFINITY, l = 0.0f;
 #pragma unroll
@@ -211,6 +230,14 @@ struct Few {
       const int tok = t + 16 * h + 4 * quad + e;
       return (h ? ok1 : ok0) && tok >= g.from && tok < g.to;
     };
+    float power_k[2] = {1.0f, 1.0f}, power_v[2] = {1.0f, 1.0f};
+    if constexpr (BLOCKS) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        power_k[h] = power(h, 0, i);
+        power_v[h] = power(h, 1, i);
+      }
+    }
     u32x4 p;
     {
       f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
@@ -220,7 +247,7 @@ struct Few {
         for (int h = 0; h < 2; ++h) {
           u32x4 kc;
           if constexpr (FP8) {
-            const u32x2 x = widen4(raw.k[h][c / 2][2 * (c % 2)]), y = widen4(raw.k[h][c / 2][2 * (c % 2) + 1]);
+            const u32x2 x = widen4(raw.k[h][c / 2][2 * (c % 2)], power_k[h]), y = widen4(raw.k[h][c / 2][2 * (c % 2) + 1], power_k[h]);
             kc = u32x4{x[0], x[1], y[0], y[1]};
           } else kc = raw.k[h][c];
           s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kc), __builtin_bit_cast(bf16x8, q[c]), s[h], 0, 0, 0);
@@ -254,9 +281,13 @@ struct Few {
     int next[2] = {-1, -1};
     const bool more = i + 1 < mine;
     if (more) {
-      if (((i + 1) & 63) == 0 && i > 0) look_up(g, i + 1, pages);
+      if (((i + 1) & 63) == 0 && i > 0) {
+        look_up(g, i + 1, pages);
+        look_up_exponents(g, i + 1, pages);
+      }
       request_k(g, i + 1, pages, next);
     } else if (ahead) {
+      look_up_exponents(then, 0, pages_then);
       request_k(then, 0, pages_then, next);
     }
     if (!whole) {                                   // what no row sees must not turn a weight of 0 into NaN
@@ -271,7 +302,7 @@ struct Few {
       uint32_t pair[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (FP8) pair[e] = widen4(raw.v[e][jw / 2])[jw % 2];
+        if constexpr (FP8) pair[e] = widen4(raw.v[e][jw / 2], power_v[e / 4])[jw % 2];
         else pair[e] = raw.v[e][jw];
       }
 #pragma unroll
@@ -320,7 +351,7 @@ struct Few {
 #pragma unroll
       for (int j = 0; j < VD; ++j) x[j] = sh.merge[0][row][d0 + j] + sh.merge[1][row][d0 + j] + sh.merge[2][row][d0 + j] + sh.merge[3][row][d0 + j];
       if (direct) {
-        const float inv = lr == 0.0f ? 0.0f : (FP8 ? a.v_scale[g.kvh] : 1.0f) / lr;
+        const float inv = lr == 0.0f ? 0.0f : (SCALED ? a.v_scale[g.kvh] : 1.0f) / lr;
         uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(g.kvh * group + row % group) * D + d0;
 #pragma unroll
         for (int j = 0; j < VD; j += 4)
@@ -336,14 +367,17 @@ struct Few {
 };
 
 // The same for up to 128 rows: 32 per wavefront.
-template <int D, bool FP8>
+template <int D, int SRC>
 __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const Segment& g, Shared<D, true>& sh, bool direct, float* o, float2* ml_out) {
-  constexpr int KS = D / 16, DT = D / 32, SRC = FP8 ? KV_PAGED_E4M3 : KV_PAGED;
+  constexpr int KS = D / 16, DT = D / 32;
+  constexpr bool SCALED = SRC == KV_PAGED_E4M3;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, row = kWaveRows * wave + (lane & 31);
   const int kvh = g.kvh;
   Stage<D, SRC> stage(sh.tiles);
   stage.k = static_cast<const char*>(a.k);
   stage.v = static_cast<const char*>(a.v);
+  stage.exponents[0] = a.k_exponent;
+  stage.exponents[1] = a.v_exponent;
   stage.kvh = kvh;
   stage.from = g.from;
   stage.to = g.t1;
@@ -356,19 +390,19 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const S
   const uint16_t* src = a.q + (size_t)(g.seq0 + there / group) * a.ld_q + (size_t)(kvh * group + there % group) * D + 8 * half;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) w.q[0][ks] = *reinterpret_cast<const bf16x8*>(src + 16 * ks);
-  const float factor = a.scale * kLog2e * (FP8 ? a.k_scale[kvh] : 1.0f);
-  if constexpr (FP8) factor_to_query(w.q[0], factor);
+  const float factor = a.scale * kLog2e * (SCALED ? a.k_scale[kvh] : 1.0f);
+  if constexpr (SCALED) factor_to_query(w.q[0], factor);
   w.m[0] = -INFINITY;
   w.l[0] = 0.0f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) w.acc[0][dt] = f32x16{};
   const int last[NB] = {0x7fffffff}, first = g.t0 / kTile, n = (g.t1 - g.t0 + kTile - 1) / kTile;
   __syncthreads();                                  // the last piece's reads of LDS are over
-  attend_tiles<D, SRC>(w, stage, first, kWaveRows * wave < g.rows ? n : 0, n, 0x7fffffff, last, FP8 ? factor_of_scores(factor) : factor);
+  attend_tiles<D, SRC>(w, stage, first, kWaveRows * wave < g.rows ? n : 0, n, 0x7fffffff, last, SCALED ? factor_of_scores(factor) : factor);
   const float l = w.l[0] + other_half(w.l[0]);
   if (row >= g.rows) return;
   if (direct) {
-    const float inv = l == 0.0f ? 0.0f : (FP8 ? a.v_scale[kvh] : 1.0f) / l;
+    const float inv = l == 0.0f ? 0.0f : (SCALED ? a.v_scale[kvh] : 1.0f) / l;
     uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(kvh * group + row % group) * D + 4 * half;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -386,7 +420,7 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const S
 }
 
 // MANY: prefixes are shared, or more than 16 query heads a key / value head: both bodies are there, also where no pass has more than 16 rows.  WHOLE: workgroup i does sequence i % n_seqs alone, and there is nothing to join.
-template <int D, bool FP8, bool MANY, bool WHOLE>
+template <int D, int SRC, bool MANY, bool WHOLE>
 __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCall c) {
   __shared__ __align__(16) Shared<D, MANY> sh;
   const DecodeArgs& a = c.a;
@@ -396,7 +430,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
   auto units = [](int from, int to) { return to > from ? (to - (from & ~63) + kUnit - 1) / kUnit : 0; };
 
   if constexpr (WHOLE) {
-    Few<D, FP8> few(a, c.sh.group);
+    Few<D, SRC> few(a, c.sh.group);
     const int s = blockIdx.x % a.n_seqs;
     const Segment g = {(int)blockIdx.x / a.n_seqs, s, s, c.sh.group, 0, uniform(length(s)), 0, uniform(length(s))};
     few.start(g);
@@ -520,7 +554,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     for (int u = begin; u < end;) {
       const Piece p = piece_at(u);
       u += p.units;
-      if (p.g.rows > kFewRows) run_many<D, FP8>(a, c.sh.group, p.g, sh, p.direct, p.o, p.ml);
+      if (p.g.rows > kFewRows) run_many<D, SRC>(a, c.sh.group, p.g, sh, p.direct, p.o, p.ml);
     }
     asm volatile("" ::: "memory");
   }
@@ -534,7 +568,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     return false;
   };
   Piece p, then;
-  Few<D, FP8> few(a, c.sh.group);
+  Few<D, SRC> few(a, c.sh.group);
   for (int round = 0;; ++round) {
     const bool more = next_few(then);               // while the first tokens of piece p are on their way
     if (round) few.run(p.g, round == 1, more, then.g, sh, p.direct, p.o, p.ml);
@@ -570,7 +604,7 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
 
 // One wavefront (W = 4: four, sharing out the pieces) per query row: the pieces of its prefix and its own, on one bound.
 template <int D, int W>
-__global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
+__global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool scaled) {
   constexpr int E = D / 64;                          // dimensions per lane
   __shared__ float part[4][D];
   const DecodeArgs& a = c.a;
@@ -632,36 +666,33 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool fp8) {
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = part[0][E * lane + e] + part[1][E * lane + e] + part[2][E * lane + e] + part[3][E * lane + e];
   }
-  const float inv = l == 0.0f ? 0.0f : (fp8 ? a.v_scale[h] : 1.0f) / l;
+  const float inv = l == 0.0f ? 0.0f : (scaled ? a.v_scale[h] : 1.0f) / l;
   uint16_t* dst = a.out + (size_t)s * a.ld_out + (size_t)head * D + E * lane;
   if constexpr (E == 2) *reinterpret_cast<uint32_t*>(dst) = pack2(x[0] * inv, x[1] * inv);
   else *dst = (uint16_t)pack2(x[0] * inv, 0.0f);
 }
 
-template <int D>
-hipError_t launch(const DecodeCall& c, bool fp8, hipStream_t s) {
+template <int D, int SRC>
+hipError_t launch(const DecodeCall& c, hipStream_t s) {
   const bool many = c.sh.group > kFewRows || c.a.n_groups > 0;
   if (!many && c.a.capacity <= kWholeTokens) {
-    const unsigned items = (unsigned)(c.a.n_kv_heads * c.a.n_seqs);
-    if (fp8) k_attn_decode<D, true, false, true><<<items, kThreads, 0, s>>>(c);
-    else k_attn_decode<D, false, false, true><<<items, kThreads, 0, s>>>(c);
+    k_attn_decode<D, SRC, false, true><<<(unsigned)(c.a.n_kv_heads * c.a.n_seqs), kThreads, 0, s>>>(c);
     return hipGetLastError();
   }
   // never more workgroups than units there can be
   const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kUnit - 1) / kUnit + 1);
   const unsigned grid = (unsigned)std::min<int64_t>(many ? kWorkgroups : kWorkgroupsFew, most);
-  if (many) {
-    if (fp8) k_attn_decode<D, true, true, false><<<grid, kThreads, 0, s>>>(c);
-    else k_attn_decode<D, false, true, false><<<grid, kThreads, 0, s>>>(c);
-  } else {
-    if (fp8) k_attn_decode<D, true, false, false><<<grid, kThreads, 0, s>>>(c);
-    else k_attn_decode<D, false, false, false><<<grid, kThreads, 0, s>>>(c);
-  }
+  if (many) k_attn_decode<D, SRC, true, false><<<grid, kThreads, 0, s>>>(c);
+  else k_attn_decode<D, SRC, false, false><<<grid, kThreads, 0, s>>>(c);
   if (hipError_t e = hipGetLastError()) return e;
   const int rows = c.a.n_seqs * c.a.n_heads;
-  if (rows <= 1024) k_join<D, 4><<<rows, kThreads, 0, s>>>(c, fp8);
-  else k_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(c, fp8);
+  if (rows <= 1024) k_join<D, 4><<<rows, kThreads, 0, s>>>(c, SRC == KV_PAGED_E4M3);
+  else k_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(c, SRC == KV_PAGED_E4M3);
   return hipGetLastError();
+}
+template <int D>
+hipError_t launch_of(const DecodeCall& c, int source, hipStream_t s) {
+  return source == KV_PAGED ? launch<D, KV_PAGED>(c, s) : source == KV_PAGED_E4M3 ? launch<D, KV_PAGED_E4M3>(c, s) : launch<D, KV_PAGED_BLOCKS>(c, s);
 }
 
 }  // namespace
@@ -673,7 +704,7 @@ size_t attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int 
   return layout(n_seqs, n_kv_heads, group, most, head_dim).total;
 }
 
-hipError_t launch_attn_decode(const DecodeArgs& a, bool fp8, hipStream_t s) {
+hipError_t launch_attn_decode(const DecodeArgs& a, int source, hipStream_t s) {
   DecodeCall c;
   c.a = a;
   c.sh.group = a.n_heads / a.n_kv_heads;
@@ -683,7 +714,7 @@ hipError_t launch_attn_decode(const DecodeArgs& a, bool fp8, hipStream_t s) {
     c.pass_base[g] = c.sh.n_passes;
     c.sh.n_passes += (a.behind[g] - a.first[g] + c.sh.per_pass - 1) / c.sh.per_pass;
   }
-  return a.head_dim == 128 ? launch<128>(c, fp8, s) : launch<64>(c, fp8, s);
+  return a.head_dim == 128 ? launch_of<128>(c, source, s) : launch_of<64>(c, source, s);
 }
 
 }  // namespace mes

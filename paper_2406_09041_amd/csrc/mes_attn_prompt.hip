@@ -274,6 +274,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
     stage.v = reinterpret_cast<const char*>(a.v);
     stage.table = a.page_table + (size_t)it.seq * a.table_pages;
     stage.page_shift = a.page_shift;
+    stage.exponents[0] = a.k_exponent;
+    stage.exponents[1] = a.v_exponent;
     stage.n_pages = a.n_pages;
     stage.n_kv_heads = a.n_kv_heads;
   }
@@ -445,7 +447,8 @@ hipError_t launch(const PromptArgs& a, int source, hipStream_t s) {
   };
   if (source == KV_PACKED) go(std::integral_constant<int, KV_PACKED>{});
   else if (source == KV_PAGED) go(std::integral_constant<int, KV_PAGED>{});
-  else go(std::integral_constant<int, KV_PAGED_E4M3>{});
+  else if (source == KV_PAGED_E4M3) go(std::integral_constant<int, KV_PAGED_E4M3>{});
+  else go(std::integral_constant<int, KV_PAGED_BLOCKS>{});
   return hipGetLastError();
 }
 

@@ -80,9 +80,12 @@ struct Stage {
   TileLds<D>& lds;
   int lane, wave;
   uint32_t offset[2];             // of a lane's 16 bytes from the first row of its copy
+  static constexpr bool kCodes = SRC == KV_PAGED_E4M3 || SRC == KV_PAGED_BLOCKS;
   int pages[4], batch;            // pages of the 16-token parts of tiles batch .. batch + 63, one tile per lane
-  static constexpr int kLanes = 64 / kPart, kWords = D / kLanes / 4;   // e4m3: lanes per key, words of codes of a lane
-  u32x4 raw[kWords / 4];          // e4m3: codes on their way
+  const uint8_t* exponents[2];    // blocks: of the cache's layer, keys and values
+  int exponent[2];                // of the wavefront's part, one tile per lane
+  static constexpr int kLanes = 64 / kPart, kWords = D / kLanes / 4;   // codes: lanes per key, words of codes of a lane
+  u32x4 raw[kWords / 4];          // codes on their way
 
   __device__ Stage(TileLds<D>& l) : ld_k(D), ld_v(D), from(0), lds(l), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), batch(-64) {}
   __device__ __forceinline__ void begin(int tile) {
@@ -103,6 +106,14 @@ struct Stage {
         const int64_t token = (int64_t)(batch + lane) * kTile + 16 * i;
         pages[i] = token < to ? table[token >> page_shift] : -1;
       }
+      if constexpr (SRC == KV_PAGED_BLOCKS) {
+        static_assert(kPart == MES_KV_BLOCK && kTileWaves == 4, "a wavefront's part of a tile is a block");
+        const int page = wave == 0 ? pages[0] : wave == 1 ? pages[1] : wave == 2 ? pages[2] : pages[3];
+        const int slot = (int)((int64_t)(batch + lane) * kTile + kPart * wave) & ((1 << page_shift) - 1);
+        const size_t at = block_at((unsigned)page < (unsigned)n_pages ? page : 0, kvh, n_kv_heads, page_shift, slot);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) exponent[i] = exponent_of(exponents[i][at]);
+      }
     }
   }
   __device__ __forceinline__ int page_of(int tile, int part) { return __builtin_amdgcn_readlane(pages[part], tile - batch); }
@@ -118,7 +129,7 @@ struct Stage {
   __device__ __forceinline__ void request(int tile, int kv) {
     const int token0 = tile * kTile + kPart * wave;
     const char* base = kv ? v : k;
-    const int step = (SRC == KV_PACKED ? (kv ? ld_v : ld_k) : D) * (SRC == KV_PAGED_E4M3 ? 1 : 2);   // bytes between rows
+    const int step = (SRC == KV_PACKED ? (kv ? ld_v : ld_k) : D) * (kCodes ? 1 : 2);   // bytes between rows
     bool real = true;
     if constexpr (SRC == KV_PACKED) {
       base += (int64_t)token0 * step;
@@ -130,7 +141,7 @@ struct Stage {
       base += ((((int64_t)page * n_kv_heads + kvh) << page_shift) + (token0 & ((1 << page_shift) - 1))) * step;
     }
     const bool lead = from > 0 && token0 < from;                      // never in the prompt kernel, where `from` is 0
-    if constexpr (SRC != KV_PAGED_E4M3) {
+    if constexpr (!kCodes) {
       const uint32_t at = (uint32_t)(uintptr_t)slot(tile, kv) + Row<D>::at(kPart * wave);
       if (real && !lead && token0 + kPart <= to) {
 #pragma unroll
@@ -154,14 +165,15 @@ struct Stage {
   // all of this wavefront's copies but the last `younger`
   template <int younger>
   __device__ __forceinline__ void arrive() {
-    if constexpr (SRC != KV_PAGED_E4M3) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(younger) : "memory");
+    if constexpr (!kCodes) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(younger) : "memory");
   }
-  __device__ __forceinline__ void deposit(int tile, int kv) {        // e4m3: codes -> bf16 rows in LDS
-    if constexpr (SRC == KV_PAGED_E4M3) {
+  __device__ __forceinline__ void deposit(int tile, int kv) {        // codes -> bf16 rows in LDS
+    if constexpr (kCodes) {
+      const float power = SRC == KV_PAGED_BLOCKS ? power_of(__builtin_amdgcn_readlane(exponent[kv], tile - batch)) : 1.0f;
       const int r = kPart * wave + lane / kLanes, piece = lane % kLanes * (kWords / 2);
 #pragma unroll
       for (int i = 0; i < kWords / 2; ++i) {
-        const u32x2 x = widen4(raw[i / 2][2 * (i % 2)]), y = widen4(raw[i / 2][2 * (i % 2) + 1]);
+        const u32x2 x = widen4(raw[i / 2][2 * (i % 2)], power), y = widen4(raw[i / 2][2 * (i % 2) + 1], power);
         *reinterpret_cast<u32x4*>(slot(tile, kv) + Row<D>::at(r) + (((piece + i) ^ Row<D>::turn(r)) * 16)) = u32x4{x[0], x[1], y[0], y[1]};
       }
     }
@@ -286,7 +298,7 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
   // three tiles and 8 wavefronts, which ask for them a tile earlier, measured the same).  Codes of an 8-bit cache pass through registers:
   // keys t + 2 during the first half of the work on tile t, values t + 1 during the second.
   const int end_all = first + n_all, end = first + n;
-  constexpr bool kDirect = SRC != KV_PAGED_E4M3;
+  constexpr bool kDirect = !Stage<D, SRC>::kCodes;
   auto before = [&](int t) {
     stage.template arrive<0>();
     barrier();                                                       // nobody reads keys t and values t - 1 any more
@@ -310,7 +322,7 @@ __device__ __forceinline__ void attend_tiles(TileRows<D>& w, Stage<D, SRC>& stag
     next_k(t + 1);
     if (t > first) next_v(t);
     u32x4 p[NB][4];
-    constexpr int kAhead = SRC == KV_PAGED_E4M3 ? 2 : 3;            // operands on their way; codes of the 8-bit cache need the registers
+    constexpr int kAhead = kDirect ? 3 : 2;            // operands on their way; codes of the 8-bit cache need the registers
     bf16x8 ring[kAhead + 1];
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) ring[g] = k_operand(g);

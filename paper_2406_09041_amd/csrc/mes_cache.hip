@@ -1,23 +1,12 @@
 // Writing to the paged cache (rotary embedding of new queries and keys, keys and values to their pages) and copying its
 // pages.  Both move bytes and are bound by HBM where there are many, by a launch where there are few.
 #include "mes_attn.h"
+#include "mes_rows.h"
 
 namespace mes {
 namespace {
 
 constexpr int kAppendThreads = 256;
-
-__device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
-// two floats -> packed bf16, round to nearest even (v_cvt_pk_bf16_f32)
-__device__ inline uint32_t pack_bf16(float a, float b) {
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  b2 r;
-  r[0] = (__bf16)a;
-  r[1] = (__bf16)b;
-  return __builtin_bit_cast(uint32_t, r);
-}
 
 // x / scale to e4m3: a true division, so that the nearest code is that of the quotient; clamped before the conversion (which
 // would make NaN of what is too large), NaN stays NaN.  0 stays 0 also where the scale is 0: a head that is
@@ -31,38 +20,46 @@ __device__ inline uint32_t pack_e4m3(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
+// 8 values times a power of two -> codes, what is past the limit to the limit, NaN stays NaN
+__device__ inline uint2 codes8(const float v[8], float by, float limit) {
+  float t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = v[i] * by;
+    t[i] = x > limit ? limit : x < -limit ? -limit : x;
+  }
+  return make_uint2(pack_e4m3(t[0], t[1], t[2], t[3]), pack_e4m3(t[4], t[5], t[6], t[7]));
+}
+template <int I>
+__device__ inline float code_at(uint32_t w) { return __builtin_amdgcn_cvt_f32_fp8(w, I); }
+// four codes to those of a larger exponent
+__device__ inline uint32_t scaled4(uint32_t w, float by) { return pack_e4m3(code_at<0>(w) * by, code_at<1>(w) * by, code_at<2>(w) * by, code_at<3>(w) * by); }
+// two codes of a word times a power of two -> bf16
+template <bool HIGH>
+__device__ inline uint32_t widen2(uint32_t w, float power) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, HIGH)); }
+
 template <bool FP8>
-__device__ inline void store8(void* base, size_t element, const float v[8], float scale) {
+__device__ inline void put8(void* base, size_t element, const float v[8], float scale) {
   if constexpr (FP8) {
     float t[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = to_grid(v[i], scale);
     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(base) + element) = make_uint2(pack_e4m3(t[0], t[1], t[2], t[3]), pack_e4m3(t[4], t[5], t[6], t[7]));
   } else {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + element) =
-        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-  }
-}
-
-__device__ inline void load8(const uint16_t* p, float v[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = bf16_lo(u[i]);
-    v[2 * i + 1] = bf16_hi(u[i]);
+    store8(static_cast<uint16_t*>(base) + element, v);
   }
 }
 
 // Four prompts of 1024 tokens (32 query, 8 key / value heads of 128, bf16): 101 MB in 19.7 us, 5.1 TB/s; 256 single tokens 6 MB, as long as a launch.
 //
-// One workgroup per row.  A unit of work is 8 dimensions of the first half of a head and the 8 they turn with, so that q_out
-// may be q: one thread reads both halves before it writes them.
-template <bool FP8>
-__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
-#pragma clang fp contract(off)   // products and sums are rounded one by one: the same bits as an elementwise program
-  const int t = blockIdx.x;
-  int s = t, behind = 1;                                   // sequence of the row, rows from it to the sequence's end
+// Which token a row of the call is.
+struct Place {
+  int seq, pos;                                            // -1: behind the last sequence; < 0 or past the capacity: none
+  int from, to;                                            // positions [from, to) of the sequence's rows
+};
+template <class A>
+__device__ __forceinline__ Place place_of(const A& a, int t) {
+  int s = t, begin = t, end = t + 1;                       // the sequence's rows
   if (a.q_offsets) {
     int lo = 0, hi = a.n_seqs;                             // first s with q_offsets[s + 1] > t
     while (lo < hi) {
@@ -70,56 +67,228 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
       if (a.q_offsets[mid + 1] > t) hi = mid; else lo = mid + 1;
     }
     s = lo;
-    if (s >= a.n_seqs || a.q_offsets[s] > t) s = -1;       // behind the last sequence
-    else behind = a.q_offsets[s + 1] - t;
+    if (s < a.n_seqs) {
+      begin = a.q_offsets[s];
+      end = a.q_offsets[s + 1];
+    }
+    if (begin > t) s = a.n_seqs;
   }
-  const int pos = s < 0 ? -1 : max(a.kv_len[s], 0) - behind;
-  if (pos < 0 || pos >= a.capacity) {
+  if (s >= a.n_seqs) return {-1, -1, 0, 0};
+  const int len = max(a.kv_len[s], 0);
+  return {s, len - (end - t), max(len - (end - begin), 0), min(len, a.capacity)};
+}
+
+// q's part of a row: turned, rounded once, to q_out; 0 where the row has no place and nothing is there yet
+__device__ __forceinline__ void append_queries(const AppendArgs& a, int t, const float* turn, bool real) {
+  const int d = a.head_dim, per = d >> 4, units = a.n_heads * per;
+  if (!real) {
     if (a.fresh)
-      for (int i = threadIdx.x * 8; i < a.n_heads * a.head_dim; i += kAppendThreads * 8)
-        *reinterpret_cast<uint4*>(a.q_out + (size_t)t * a.ld_q_out + i) = make_uint4(0, 0, 0, 0);
+      for (int i = threadIdx.x * 8; i < a.n_heads * d; i += kAppendThreads * 8) *reinterpret_cast<uint4*>(a.q_out + (size_t)t * a.ld_q_out + i) = make_uint4(0, 0, 0, 0);
     return;
   }
+  for (int w = threadIdx.x; w < units; w += kAppendThreads) {
+    const int h = w / per, u = w % per;
+    int i, j;
+    chunks_of(u, a.dims, a.pairs, i, j);
+    float x[8], y[8];
+    load8(a.q + (size_t)t * a.ld_q + (size_t)h * d + i, x);
+    load8(a.q + (size_t)t * a.ld_q + (size_t)h * d + j, y);
+    if (u < a.dims >> 4) turn_unit(x, y, turn, u, a.dims, a.pairs, 1.0f);
+    store8(a.q_out + (size_t)t * a.ld_q_out + (size_t)h * d + i, x);
+    store8(a.q_out + (size_t)t * a.ld_q_out + (size_t)h * d + j, y);
+  }
+}
+
+// One workgroup per row.  A unit of work is 8 dimensions of the first half of a head and the 8 they turn with, so that q_out
+// may be q: one thread reads both halves before it writes them.
+template <bool FP8>
+__global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
+  const int t = blockIdx.x;
+  const Place at = place_of(a, t);
+  const int s = at.seq, pos = at.pos;
+  if (pos < 0 || pos >= a.capacity) return append_queries(a, t, nullptr, false);
   const int page = a.page_table[(size_t)s * a.table_pages + (pos >> a.page_shift)];
   const bool placed = (unsigned)page < (unsigned)a.n_pages;
-  const int d = a.head_dim, half = d >> 1, per = half >> 3;   // per: units of a head
+  const int d = a.head_dim, per = d >> 4;                  // per: units of a head
   const size_t slot = (size_t)(pos & ((1 << a.page_shift) - 1)) * d;
   const size_t head_step = (size_t)d << a.page_shift;
   const size_t page_at = ((size_t)a.layer * a.n_pages + (placed ? page : 0)) * a.n_kv_heads * head_step + slot;
-  const float* turn = a.rotary ? a.rotary + (size_t)pos * d : nullptr;
+  const float* turn = a.rotary ? a.rotary + (size_t)pos * a.dims : nullptr;
   const int nq = a.q ? a.n_heads * per : 0, nk = a.n_kv_heads * per;
-  for (int u = threadIdx.x; u < nq + 2 * nk; u += kAppendThreads) {
-    const int w = u < nq ? u : u < nq + nk ? u - nq : u - nq - nk;
-    const int h = w / per, i = (w % per) * 8;
-    const uint16_t* row = u < nq ? a.q + (size_t)t * a.ld_q : u < nq + nk ? a.k + (size_t)t * a.ld_k : a.v + (size_t)t * a.ld_v;
+  for (int w = threadIdx.x; w < nq + 2 * nk; w += kAppendThreads) {
+    const int z = w < nq ? w : w < nq + nk ? w - nq : w - nq - nk;
+    const int h = z / per, u = z % per;
+    const uint16_t* row = w < nq ? a.q + (size_t)t * a.ld_q : w < nq + nk ? a.k + (size_t)t * a.ld_k : a.v + (size_t)t * a.ld_v;
+    int i, j;
+    chunks_of(u, a.dims, a.pairs, i, j);
     float x[8], y[8];
     load8(row + (size_t)h * d + i, x);
-    load8(row + (size_t)h * d + half + i, y);
-    if (u < nq + nk && turn) {
-      float c[8], sn[8];
-#pragma unroll
-      for (int j = 0; j < 8; j += 4) {
-        *reinterpret_cast<float4*>(c + j) = *reinterpret_cast<const float4*>(turn + i + j);
-        *reinterpret_cast<float4*>(sn + j) = *reinterpret_cast<const float4*>(turn + half + i + j);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float p = x[j] * c[j], q = y[j] * sn[j], r = y[j] * c[j], o = x[j] * sn[j];
-        x[j] = p - q;
-        y[j] = r + o;
-      }
-    }
-    if (u < nq) {
-      store8<false>(a.q_out, (size_t)t * a.ld_q_out + (size_t)h * d + i, x, 1.0f);
-      store8<false>(a.q_out, (size_t)t * a.ld_q_out + (size_t)h * d + half + i, y, 1.0f);
+    load8(row + (size_t)h * d + j, y);
+    if (w < nq + nk && turn && u < a.dims >> 4) turn_unit(x, y, turn, u, a.dims, a.pairs, 1.0f);
+    if (w < nq) {
+      put8<false>(a.q_out, (size_t)t * a.ld_q_out + (size_t)h * d + i, x, 1.0f);
+      put8<false>(a.q_out, (size_t)t * a.ld_q_out + (size_t)h * d + j, y, 1.0f);
     } else if (placed) {
-      const bool key = u < nq + nk;
+      const bool key = w < nq + nk;
       void* base = key ? a.k_cache : a.v_cache;
       const float scale = FP8 ? (key ? a.k_scale : a.v_scale)[(size_t)a.layer * a.n_kv_heads + h] : 1.0f;
-      const size_t at = page_at + h * head_step;
-      store8<FP8>(base, at + i, x, scale);
-      store8<FP8>(base, at + half + i, y, scale);
+      const size_t to = page_at + h * head_step;
+      put8<FP8>(base, to + i, x, scale);
+      put8<FP8>(base, to + j, y, scale);
     }
+  }
+}
+
+// The same to a cache of blocks.  A block of a head's keys or values is one wavefront's work, from the largest of its values to its codes: it
+// holds all of them in registers, or, where the call has few tokens for the block, several heads of it.  One workgroup per row turns the row's queries
+// and takes its share of the heads of the block that the row is in, so that nothing has to be counted beforehand and a block's wavefronts are
+// on different compute units.
+template <int D>
+__global__ __launch_bounds__(kAppendThreads) void k_append_blocks(AppendArgs a) {
+  constexpr int kUnits = D / 16, kRowsPass = 64 / kUnits, kPasses = MES_KV_BLOCK / kRowsPass;
+  const int t = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Place at = place_of(a, t);
+  const int pos = at.pos;
+  const bool real = pos >= 0 && pos < a.capacity;
+  const float* turns = a.rotary;
+  if (a.q) append_queries(a, t, turns + (size_t)max(pos, 0) * a.dims, real);
+  if (!real) return;
+  const int page = a.page_table[(size_t)at.seq * a.table_pages + (pos >> a.page_shift)];
+  if ((unsigned)page >= (unsigned)a.n_pages) return;
+  // the block's rows in this call: positions [from, to), rows of the call from row0
+  const int begin = pos & -MES_KV_BLOCK, from = max(begin, at.from), rows = min(begin + MES_KV_BLOCK, at.to) - from, row0 = t - (pos - from);
+  const int older = from - begin, slot = begin & ((1 << a.page_shift) - 1);
+  // lanes of a (head, keys or values), and how many of these a wavefront does at a time
+  int lanes = kUnits;
+  while (lanes < 64 && lanes < kUnits * rows) lanes <<= 1;
+  const int together = 64 / lanes, l = lane & (lanes - 1), u = l % kUnits, r0 = l / kUnits, tasks = 2 * a.n_kv_heads;
+  int i, j;
+  chunks_of(u, a.dims, a.pairs, i, j);
+  const bool turning = turns && u < a.dims >> 4;
+  for (int group = wave * rows + (pos - from); group * together < tasks; group += kAppendThreads / 64 * rows) {
+    const int task = group * together + lane / lanes;
+    const bool mine = task < tasks, key = task < a.n_kv_heads;
+    const int h = key ? task : task - a.n_kv_heads;
+    float x[kPasses][8], y[kPasses][8], top = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const int r = r0 + p * kRowsPass;
+      if (!mine || r >= rows) continue;
+      const uint16_t* row = (key ? a.k + (size_t)(row0 + r) * a.ld_k : a.v + (size_t)(row0 + r) * a.ld_v) + (size_t)h * D;
+      load8(row + i, x[p]);
+      load8(row + j, y[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const int r = r0 + p * kRowsPass;
+      if (!mine || r >= rows) continue;
+      if (key && turning) turn_unit(x[p], y[p], turns + (size_t)(from + r) * a.dims, u, a.dims, a.pairs, 1.0f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float s = fabsf(x[p][e]), w = fabsf(y[p][e]);
+        top = fmaxf(top, s <= 3.402823466e38f ? s : 0.0f);   // what is not finite does not count
+        top = fmaxf(top, w <= 3.402823466e38f ? w : 0.0f);
+      }
+    }
+    for (int m = 1; m < lanes; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if (!mine) continue;
+    uint8_t* exponents = key ? a.k_exponent : a.v_exponent;
+    uint8_t* codes = static_cast<uint8_t*>(key ? a.k_cache : a.v_cache) + ((((size_t)a.layer * a.n_pages + page) * a.n_kv_heads + h) << a.page_shift) * D;
+    const size_t block = block_at(page, h, a.n_kv_heads, a.page_shift, slot);
+    // the least with top <= 448 2^e, 448 = 1.75 2^8: 8 below top's own exponent, 7 where its mantissa is above 1.75
+    int exponent = max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8, MES_KV_LEAST_EXPONENT);
+    if (older) {
+      const int was = exponent_of(exponents[block]);
+      if (exponent > was) {                                  // seldom: a sequence's scale is found by its first tokens
+        const float by = ldexpf(1.0f, was - exponent);
+        for (int w = l; w < older * (D / 8); w += lanes) {
+          uint2* p = reinterpret_cast<uint2*>(codes + (size_t)slot * D + w * 8);
+          const uint2 c = *p;
+          *p = make_uint2(scaled4(c.x, by), scaled4(c.y, by));
+        }
+      } else exponent = was;
+    }
+    if (l == 0) exponents[block] = (uint8_t)exponent;
+    const float by = power_of(254 - exponent), limit = exponent == MES_KV_MOST_EXPONENT ? 240.0f : 448.0f;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const int r = r0 + p * kRowsPass;
+      if (r >= rows) continue;
+      uint8_t* row = codes + (size_t)(slot + older + r) * D;
+      *reinterpret_cast<uint2*>(row + i) = codes8(x[p], by, limit);
+      *reinterpret_cast<uint2*>(row + j) = codes8(y[p], by, limit);
+    }
+  }
+}
+
+// Reading back: a thread 16 dimensions of a token.  Workgroups take kReadRows rows; keys and values of a head are read in the order of the page.
+constexpr int kReadThreads = 256, kReadRows = 16;
+
+template <int DTYPE>
+__device__ __forceinline__ void read16(const void* base, size_t element, float scale, uint16_t* to) {
+  if constexpr (DTYPE == MES_KV_BF16) {
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + element);
+    const uint4 x = p[0], y = p[1];
+    reinterpret_cast<uint4*>(to)[0] = x;
+    reinterpret_cast<uint4*>(to)[1] = y;
+  } else {
+    const uint4 c = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + element);
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (DTYPE == MES_KV_E4M3_BLOCKS) {
+        v[2 * i] = widen2<false>(w[i], scale);
+        v[2 * i + 1] = widen2<true>(w[i], scale);
+      } else {
+        v[2 * i] = pack_bf16(code_at<0>(w[i]) * scale, code_at<1>(w[i]) * scale);
+        v[2 * i + 1] = pack_bf16(code_at<2>(w[i]) * scale, code_at<3>(w[i]) * scale);
+      }
+    }
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kReadThreads) void k_read(ReadArgs a) {
+  constexpr int kChunks = D / 16;
+  __shared__ int pages[kReadRows], slots[kReadRows];       // page -1: absent, -2: no row of a sequence
+  const int t0 = blockIdx.x * kReadRows;
+  if (threadIdx.x < kReadRows) {
+    const int t = t0 + threadIdx.x;
+    int page = -2, slot = 0;
+    if (t < a.T) {
+      const Place at = place_of(a, t);
+      if (at.seq >= 0) {
+        page = -1;
+        if (at.pos >= 0 && at.pos < a.capacity) {
+          const int p = a.page_table[(size_t)at.seq * a.table_pages + (at.pos >> a.page_shift)];
+          if ((unsigned)p < (unsigned)a.n_pages) page = p;
+          slot = at.pos & ((1 << a.page_shift) - 1);
+        }
+      }
+    }
+    pages[threadIdx.x] = page;
+    slots[threadIdx.x] = slot;
+  }
+  __syncthreads();
+  const int half = a.n_kv_heads * kReadRows * kChunks;
+  for (int w = threadIdx.x; w < 2 * half; w += kReadThreads) {
+    const bool key = w < half;
+    const int z = key ? w : w - half, c = z % kChunks, r = z / kChunks % kReadRows, h = z / (kChunks * kReadRows), page = pages[r], slot = slots[r];
+    uint16_t* out = key ? a.k : a.v;
+    if (!out || t0 + r >= a.T || (page == -2 && !a.fresh)) continue;
+    out += (size_t)(t0 + r) * (key ? a.ld_k : a.ld_v) + (size_t)h * D + c * 16;
+    if (page < 0) {
+      reinterpret_cast<uint4*>(out)[0] = make_uint4(0, 0, 0, 0);
+      reinterpret_cast<uint4*>(out)[1] = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    float scale = 1.0f;
+    if constexpr (DTYPE == MES_KV_E4M3) scale = (key ? a.k_scale : a.v_scale)[h];
+    if constexpr (DTYPE == MES_KV_E4M3_BLOCKS) scale = power_of(exponent_of((key ? a.k_exponent : a.v_exponent)[block_at(page, h, a.n_kv_heads, a.page_shift, slot)]));
+    read16<DTYPE>(key ? a.k_cache : a.v_cache, (((((size_t)page * a.n_kv_heads + h) << a.page_shift) + slot) * D) + c * 16, scale, out);
   }
 }
 
@@ -132,7 +301,9 @@ constexpr int kCopyThreads = 256, kCopyWords = 8, kCopyBytes = kCopyThreads * kC
 
 struct CopyArgs {
   char *k, *v;
+  uint8_t *k_exponent, *v_exponent;    // nullptr: the cache has none
   size_t page_bytes, layer_bytes;
+  int n_pages, page_exponents;
   int n_layers, parts;                 // parts: workgroups per page of a layer
   int32_t src[kCopyPairs], dst[kCopyPairs];
 };
@@ -141,6 +312,10 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(CopyArgs a) {
   const int part = blockIdx.x % a.parts, layer = (blockIdx.x / a.parts) % a.n_layers, pair = blockIdx.x / a.parts / a.n_layers;
   char* base = (blockIdx.y ? a.v : a.k) + layer * a.layer_bytes;
   const size_t at = (size_t)part * kCopyBytes + threadIdx.x * 16;
+  if (part == 0 && a.k_exponent) {
+    uint8_t* of = (blockIdx.y ? a.v_exponent : a.k_exponent) + (size_t)layer * a.n_pages * a.page_exponents;
+    for (int x = threadIdx.x; x < a.page_exponents; x += kCopyThreads) of[(size_t)a.dst[pair] * a.page_exponents + x] = of[(size_t)a.src[pair] * a.page_exponents + x];
+  }
   const char* from = base + a.src[pair] * a.page_bytes;
   char* to = base + a.dst[pair] * a.page_bytes;
   constexpr int kStep = kCopyThreads * 16;
@@ -157,9 +332,24 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(CopyArgs a) {
 
 }  // namespace
 
-hipError_t launch_append(const AppendArgs& a, int T, bool fp8, hipStream_t s) {
-  if (fp8) k_append<true><<<T, kAppendThreads, 0, s>>>(a);
-  else k_append<false><<<T, kAppendThreads, 0, s>>>(a);
+hipError_t launch_append(const AppendArgs& a, int T, int dtype, hipStream_t s) {
+  if (dtype == MES_KV_BF16) k_append<false><<<T, kAppendThreads, 0, s>>>(a);
+  else if (dtype == MES_KV_E4M3) k_append<true><<<T, kAppendThreads, 0, s>>>(a);
+  else if (a.head_dim == 128) k_append_blocks<128><<<T, kAppendThreads, 0, s>>>(a);
+  else k_append_blocks<64><<<T, kAppendThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_read(const ReadArgs& a, int dtype, hipStream_t s) {
+  const unsigned grid = (unsigned)((a.T + kReadRows - 1) / kReadRows);
+  auto go = [&](auto type) {
+    constexpr int DTYPE = decltype(type)::value;
+    if (a.head_dim == 128) k_read<DTYPE, 128><<<grid, kReadThreads, 0, s>>>(a);
+    else k_read<DTYPE, 64><<<grid, kReadThreads, 0, s>>>(a);
+  };
+  if (dtype == MES_KV_BF16) go(std::integral_constant<int, MES_KV_BF16>{});
+  else if (dtype == MES_KV_E4M3) go(std::integral_constant<int, MES_KV_E4M3>{});
+  else go(std::integral_constant<int, MES_KV_E4M3_BLOCKS>{});
   return hipGetLastError();
 }
 
@@ -167,7 +357,11 @@ hipError_t launch_copy_pages(const mes_kv& kv, const int32_t* src, const int32_t
   CopyArgs a;
   a.k = static_cast<char*>(kv.k);
   a.v = static_cast<char*>(kv.v);
-  a.page_bytes = (size_t)kv.n_kv_heads * kv.page_tokens * kv.head_dim * (kv.dtype == MES_KV_E4M3 ? 1 : 2);
+  a.page_bytes = (size_t)kv.n_kv_heads * kv.page_tokens * kv.head_dim * (kv.dtype == MES_KV_BF16 ? 2 : 1);
+  a.k_exponent = kv.dtype == MES_KV_E4M3_BLOCKS ? kv.k_exponent : nullptr;
+  a.v_exponent = kv.dtype == MES_KV_E4M3_BLOCKS ? kv.v_exponent : nullptr;
+  a.n_pages = kv.n_pages;
+  a.page_exponents = kv.n_kv_heads * kv.page_tokens / MES_KV_BLOCK;
   a.layer_bytes = a.page_bytes * kv.n_pages;
   a.n_layers = kv.n_layers;
   a.parts = (int)((a.page_bytes + kCopyBytes - 1) / kCopyBytes);
