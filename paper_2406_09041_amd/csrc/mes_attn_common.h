@@ -92,6 +92,7 @@ __device__ __forceinline__ int wave_max(int v) {
   v = max(v, from_below<0x143, 0xc>(v));
   return __builtin_amdgcn_readlane(v, 63);
 }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 }  // namespace mes

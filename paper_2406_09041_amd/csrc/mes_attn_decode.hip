@@ -1,12 +1,13 @@
 // One token of every sequence against the paged cache, prefixes that an expert's sequences share read once.  Bound by HBM:
 // every distinct cached token is read once, 2 head_dim values per key / value head, for 4 head_dim n_heads operations.
 //
-// Work is a flat line of units (kUnit = 128 tokens of one key / value head): per key / value head first the shared
-// prefixes (once per pass of up to 128 query rows), then what every sequence has of its own.  The line is cut into equal
-// chunks, one per workgroup, wherever that falls: the workgroups are equally busy however the lengths are spread, also for one long
-// sequence, and the launch does not depend on the lengths, which stay on the device (every workgroup adds them up for itself).  A
-// piece of the line that does not cover a sequence alone leaves (bound, sum, weighted values) in the workspace, and k_join
-// adds the pieces of a row in their order.
+// Work is a flat line of costs.  First, per key / value head, what many query rows read together: passes of up to 128 rows over a shared
+// prefix, in tiles of 64 tokens, which a workgroup's four wavefronts do together.  Then what every sequence has of its own, in steps of 32 tokens,
+// which a wavefront does alone and waits for nobody (in teams of four with their sums added up in LDS, sequences of 16 to 4096 tokens
+// took 104 us instead of 91, as beginning and ending a piece cost 4 us each).  The line is cut into equal chunks, wherever that falls: all wavefronts are
+// equally busy however the lengths are spread, also for one long sequence, and the launch does not depend on the lengths, which stay on
+// the device (every workgroup adds them up for itself).  A piece of the line that does not cover a sequence alone leaves (bound, sum,
+// weighted values) in the workspace, and k_join adds the pieces of a row in their order.
 //
 // Up to 16 query rows (one sequence of a group of up to 16 heads, or few sequences' shared prefix): a wavefront takes 32 tokens at a
 // time.  Scores are formed transposed, S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K's operand is 16 tokens x 8 dimensions per lane
@@ -16,9 +17,8 @@
 // is pairs of 16-bit halves put together, one v_perm each.  So neither keys nor values pass through LDS.  Of the 16 columns of a
 // tile 4 (n_heads / n_kv_heads) are used where nothing is shared: the matrix cores are idle most of the time anyway.
 //
-// More rows: up to 128 of them share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from about 100 rows on.  The crossover
-// at 16 rows is where the small body would read the tokens a second time: 64 sequences of 16 experts (1 to 25 each) took 62 us by passes of
-// 16 rows and 47 through LDS, 96 behind one e4m3 prefix 94 and 60.
+// More rows: up to 128 of them share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from about 100 rows on; also those of a
+// sequence alone where more than 16 query heads share a key / value head.
 //
 // Weights are rounded to bf16 for the product with V, as the matrix cores take both operands alike, and summed as rounded: they still add up
 // to 1, and a row's error grows by at most 2^-8 of its weighted values' size (measured against 64 bits: 0.0020 of the rows' norm, 0.0017
@@ -34,11 +34,17 @@
 namespace mes {
 namespace {
 
-constexpr int kThreads = 256, kUnit = 128, kRowsPass = 128, kFewRows = 16;
-// Workgroups of a launch: what the chip holds.  Without shared prefixes and with up to 16 heads per key / value head only the small body is
-// needed, which leaves room for three per compute unit (256 sequences of 0 to 8192 tokens, when it was made: 168 us, as a part
-// of the larger kernel, two per compute unit, 186).
-constexpr int kWorkgroups = 512, kWorkgroupsFew = 768;
+constexpr bool has_codes(int source) { return source != KV_PAGED; }
+
+constexpr int kThreads = 256, kWaves = kThreads / 64, kStep = 32, kRowsPass = 128, kFewRows = 16;
+// Costs on the line, in steps of a wavefront: of a tile of the larger body, of beginning and ending what a pass or a sequence does there, and
+// the same of a sequence's own part in the smaller one.
+template <int SRC>
+struct Cost {
+  static constexpr uint32_t kTile = has_codes(SRC) ? 7 : 4, kBegin = has_codes(SRC) ? 12 : 7, kOwn = has_codes(SRC) ? 3 : 2;
+};
+// Workgroups of a launch: what the chip holds.
+constexpr int kWorkgroups = 512;
 // Up to this many tokens a sequence is one workgroup's, where nothing is shared: no second launch to add up pieces (one
 // sequence of 200 tokens, when it was made: 9.2 us, 12.4 with it).
 constexpr int kWholeTokens = 512;
@@ -60,7 +66,7 @@ struct Layout {
 
 __host__ __device__ inline Layout layout(int n_seqs, int n_kv_heads, int group, int n_passes, int head_dim) {
   const size_t pre = (size_t)(n_passes ? kWorkgroups + n_kv_heads * n_passes : 0) * kRowsPass;
-  const size_t own = (size_t)(kWorkgroupsFew + n_kv_heads * n_seqs) * group;
+  const size_t own = (size_t)((group > kFewRows ? 1 : kWaves) * kWorkgroups + n_kv_heads * n_seqs) * group;
   Layout y;
   y.prefix_o = 0;
   y.own_o = y.prefix_o + pre * head_dim * 4;
@@ -81,14 +87,13 @@ struct DecodeCall {
   int pass_base[MES_MAX_EXPERTS];
 };
 
-constexpr bool has_codes(int source) { return source != KV_PAGED; }
-
 template <int D, int SRC>
 struct Raw {                                        // 32 tokens of keys and values on their way
   static constexpr bool FP8 = has_codes(SRC);
   static constexpr int VD = D / 16, KC = FP8 ? D / 64 : D / 32, VW = VD * (FP8 ? 1 : 2) / 4;
+  typedef uint32_t Words __attribute__((ext_vector_type(VW)));
   u32x4 k[2][KC];
-  uint32_t v[8][VW];
+  Words v[8];
 };
 
 // first dimension of the 8 that a lane holds in product c of K Q^T
@@ -102,61 +107,59 @@ struct Segment {                                    // a piece of the line
   int from, to, t0, t1;                             // tokens of [from, to) in the units [t0, t1), t0 a multiple of 64
 };
 
+template <int D>
+struct Merge {                                      // a workgroup's four wavefronts of one piece
+  float o[4][kFewRows][D + 4];
+  float2 ml[4][kFewRows];
+};
 struct Nothing {};
 template <int D, bool MANY>
 struct Shared {
-  union {
-    std::conditional_t<MANY, TileLds<D>, Nothing> tiles;
-    struct {
-      float merge[4][kFewRows][D + 4];
-      float2 ml[4][kFewRows];
-    };
-  };
-  int cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
+  [[no_unique_address]] std::conditional_t<MANY, TileLds<D>, Nothing> tiles;
+  uint32_t cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
   int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: fewer than two are
-  int part[4];
+  uint32_t part[4];
 };
 
 // The weighted sum over a piece with up to 16 query rows.  Pieces follow one another without a pause: a wavefront asks for the next piece's
-// first tokens where it would ask for more of this one's, and knows their pages by then.
-template <int D, int SRC>
+// first tokens where it would ask for more of this one's, and knows their pages by then.  TEAM: the workgroup's wavefronts take every fourth step
+// of a piece and add up their results; else a piece is a wavefront's, which waits for nobody.
+template <int D, int SRC, bool TEAM>
 struct Few {
   static constexpr bool FP8 = has_codes(SRC), SCALED = SRC == KV_PAGED_E4M3, BLOCKS = SRC == KV_PAGED_BLOCKS;
-  static constexpr int VD = D / 16, KS = D / 32;
+  static constexpr int VD = D / 16, KS = D / 32, kBatch = 32;   // kBatch: steps whose pages are looked up together
   typedef Raw<D, SRC> R;
   const DecodeArgs& a;
   int group, lane, wave, col, quad;
   u32x4 q[KS];                                      // Q^T operands
   R raw;                                            // the step that comes next
   int there[2];                                     // its pages
-  int pages[2];                                     // of 64 steps of the piece, one step per lane
-  int exponents[2][2];                              // blocks: of keys and values on these pages
+  int pages;                                        // of the halves of kBatch steps of the piece, one half per lane
+  int exponents[2];                                 // blocks: of keys and values on these pages
 
   __device__ Few(const DecodeArgs& args, int g) : a(args), group(g), lane(threadIdx.x & 63), wave(uniform(threadIdx.x >> 6)), col(lane & 15), quad(lane >> 4) {}
 
-  __device__ __forceinline__ int steps(const Segment& g) const { return ((g.t1 - g.t0 + 31) / 32 - wave + 3) / 4; }   // steps wave, wave + 4, ...
-  __device__ __forceinline__ void look_up(const Segment& g, int first, int (&pg)[2]) const {
-    const int32_t* table = a.page_table + (size_t)g.seq * a.table_pages;
-    const int mine = steps(g);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int t = g.t0 + (4 * (first + lane) + wave) * 32 + 16 * h;
-      pg[h] = first + lane < mine && t < g.to ? table[t >> a.page_shift] : -1;
-    }
+  __device__ __forceinline__ int token_of(const Segment& g, int step) const { return g.t0 + (TEAM ? 4 * step + wave : step) * kStep; }
+  __device__ __forceinline__ int steps(const Segment& g) const {
+    const int all = (g.t1 - g.t0 + kStep - 1) / kStep;
+    return TEAM ? (all - wave + 3) / 4 : all;
+  }
+  // the pages of steps first .. first + kBatch - 1
+  __device__ __forceinline__ int look_up(const Segment& g, int first) const {
+    const int t = token_of(g, first + lane / 2) + lane % 2 * 16;
+    return t < g.t1 ? (a.page_table + (size_t)g.seq * a.table_pages)[t >> a.page_shift] : -1;
   }
   // asked for with the tokens themselves: the pages have to be there
-  __device__ __forceinline__ void look_up_exponents(const Segment& g, int first, const int (&pg)[2]) {
+  __device__ __forceinline__ void look_up_exponents(const Segment& g, int first, int pg) {
     if constexpr (BLOCKS) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int t = g.t0 + (4 * (first + lane) + wave) * 32 + 16 * h;
-        const size_t at = block_at((unsigned)pg[h] < (unsigned)a.n_pages ? pg[h] : 0, g.kvh, a.n_kv_heads, a.page_shift, t & ((1 << a.page_shift) - 1));
-        exponents[h][0] = a.k_exponent[at];
-        exponents[h][1] = a.v_exponent[at];
-      }
+      const int t = token_of(g, first + lane / 2) + lane % 2 * 16;
+      const size_t at = block_at((unsigned)pg < (unsigned)a.n_pages ? pg : 0, g.kvh, a.n_kv_heads, a.page_shift, t & ((1 << a.page_shift) - 1));
+      exponents[0] = a.k_exponent[at];
+      exponents[1] = a.v_exponent[at];
     }
   }
-  __device__ __forceinline__ float power(int h, int kv, int i) const { return power_of(exponent_of(__builtin_amdgcn_readlane(exponents[h][kv], i & 63))); }
+  __device__ __forceinline__ static int lane_of(int step, int half) { return (step & (kBatch - 1)) * 2 + half; }
+  __device__ __forceinline__ float power(int h, int kv, int i) const { return power_of(exponent_of(__builtin_amdgcn_readlane(exponents[kv], lane_of(i, h)))); }
   __device__ __forceinline__ void load_q(const Segment& g) {
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
@@ -168,39 +171,30 @@ struct Few {
   __device__ __forceinline__ size_t row_of(const Segment& g, int t, int page) const {   // first element of token t's row
     return ((((size_t)((unsigned)page < (unsigned)a.n_pages ? page : 0) * a.n_kv_heads + g.kvh) << a.page_shift) + (t & ((1 << a.page_shift) - 1))) * D;
   }
-  __device__ __forceinline__ void request_k(const Segment& g, int i, const int (&pg)[2], int (&next)[2]) {
-    const int t = g.t0 + (4 * i + wave) * 32;
+  // The rows of 16 tokens are at a base that all lanes share, a lane's bytes at a distance that all of them share.
+  __device__ __forceinline__ void request_k(const Segment& g, int i, int pg, int (&next)[2]) {
+    constexpr int kItem = FP8 ? 1 : 2;
+    const uint32_t mine = col * D * kItem + 16 * quad;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      next[h] = __builtin_amdgcn_readlane(pg[h], i & 63);
-      const size_t at = row_of(g, t + 16 * h, next[h]) + col * D;
+      next[h] = __builtin_amdgcn_readlane(pg, lane_of(i, h));
+      const char* base = static_cast<const char*>(a.k) + row_of(g, token_of(g, i) + 16 * h, next[h]) * kItem;
 #pragma unroll
-      for (int c = 0; c < R::KC; ++c) {
-        if constexpr (FP8) raw.k[h][c] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.k) + at + 64 * c + 16 * quad);
-        else raw.k[h][c] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.k) + at + 32 * c + 8 * quad);
-      }
+      for (int c = 0; c < R::KC; ++c) raw.k[h][c] = *reinterpret_cast<const u32x4*>(base + (mine + 64 * c));
     }
   }
   __device__ __forceinline__ void request_v(const Segment& g, int i, const int (&next)[2]) {
-    const int t = g.t0 + (4 * i + wave) * 32;
-    typedef uint32_t words __attribute__((ext_vector_type(R::VW)));
+    constexpr int kItem = FP8 ? 1 : 2;
+    const uint32_t mine = (4 * quad * D + VD * col) * kItem;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const size_t at = row_of(g, t + 16 * h, next[h]) + 4 * quad * D + VD * col;
+      const char* base = static_cast<const char*>(a.v) + row_of(g, token_of(g, i) + 16 * h, next[h]) * kItem;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const void* p = FP8 ? (const void*)(static_cast<const uint8_t*>(a.v) + at + e * D) : (const void*)(static_cast<const uint16_t*>(a.v) + at + e * D);
-        if constexpr (R::VW == 1) raw.v[4 * h + e][0] = *reinterpret_cast<const uint32_t*>(p);
-        else {
-          const words w = *reinterpret_cast<const words*>(p);
-#pragma unroll
-          for (int x = 0; x < R::VW; ++x) raw.v[4 * h + e][x] = w[x];
-        }
-      }
+      for (int e = 0; e < 4; ++e) raw.v[4 * h + e] = *reinterpret_cast<const typename R::Words*>(base + (mine + e * D * kItem));
     }
   }
   __device__ __forceinline__ void start(const Segment& g) {   // a piece that nobody has asked for
-    look_up(g, 0, pages);
+    pages = look_up(g, 0);
     load_q(g);
     look_up_exponents(g, 0, pages);
     raw = R{};
@@ -210,8 +204,7 @@ struct Few {
   // The piece g, its first step asked for unless it is `fresh`; ahead: so is the first step of the piece `then` at the end.  Into o / ml_out, or
   // out where the piece is all that its rows see.  A fresh piece takes a step of nothing first, which asks for its first tokens: the code of
   // a step is then there before the loads of a whole chip are on their way, behind which it would be fetched (3 to 8 us).
-  template <class SH>
-  __device__ __forceinline__ void run(const Segment& g, bool fresh, bool ahead, const Segment& then, SH& sh, bool direct, float* o, float2* ml_out) {
+  __device__ __forceinline__ void run(const Segment& g, bool fresh, bool ahead, const Segment& then, Merge<D>* sh, bool direct, float* o, float2* ml_out) {
   const float factor = a.scale * kLog2e * (SCALED ? a.k_scale[g.kvh] : 1.0f), scale = SCALED ? factor_of_scores(factor) : factor;
   if constexpr (SCALED) factor_to_query(q, factor);
   f32x4 acc[VD];
@@ -219,16 +212,16 @@ struct Few {
 #pragma unroll
   for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
   const int mine = steps(g);
-  int pages_then[2] = {-1, -1};
-  if (ahead) look_up(then, 0, pages_then);
+  int pages_then = -1, pages_next = -1;             // of the next piece, of this one's next batch
+  if (ahead) pages_then = look_up(then, 0);
   ahead = ahead && steps(then) > 0;
   for (int i = fresh || mine == 0 ? -1 : 0; i < mine; ++i) {
-    const int t = g.t0 + (4 * i + wave) * 32;
+    const int t = token_of(g, i);
     const bool ok0 = (unsigned)there[0] < (unsigned)a.n_pages, ok1 = (unsigned)there[1] < (unsigned)a.n_pages;
-    const bool whole = ok0 && ok1 && t >= g.from && t + 32 <= g.to;
+    const bool whole = ok0 && ok1 && t >= g.from && t + kStep <= g.t1;
     auto seen = [&](int h, int e) {                 // token e of the lane's four in half h
       const int tok = t + 16 * h + 4 * quad + e;
-      return (h ? ok1 : ok0) && tok >= g.from && tok < g.to;
+      return (h ? ok1 : ok0) && tok >= g.from && tok < g.t1;
     };
     float power_k[2] = {1.0f, 1.0f}, power_v[2] = {1.0f, 1.0f};
     if constexpr (BLOCKS) {
@@ -281,8 +274,8 @@ struct Few {
     int next[2] = {-1, -1};
     const bool more = i + 1 < mine;
     if (more) {
-      if (((i + 1) & 63) == 0 && i > 0) {
-        look_up(g, i + 1, pages);
+      if (((i + 1) & (kBatch - 1)) == 0 && i > 0) {
+        pages = pages_next;
         look_up_exponents(g, i + 1, pages);
       }
       request_k(g, i + 1, pages, next);
@@ -293,9 +286,7 @@ struct Few {
     if (!whole) {                                   // what no row sees must not turn a weight of 0 into NaN
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int x = 0; x < R::VW; ++x)
-          if (!seen(e / 4, e % 4)) raw.v[e][x] = 0;
+        if (!seen(e / 4, e % 4)) raw.v[e] = typename R::Words(0);
     }
 #pragma unroll
     for (int jw = 0; jw < VD / 2; ++jw) {           // dimensions VD m + 2 jw and + 1
@@ -313,67 +304,75 @@ struct Few {
         acc[2 * jw + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p), acc[2 * jw + odd], 0, 0, 0);
       }
     }
-    if (more) request_v(g, i + 1, next);
-    else if (ahead) request_v(then, 0, next);
+    if (more) {
+      request_v(g, i + 1, next);
+      if (((i + 2) & (kBatch - 1)) == 0) pages_next = look_up(g, i + 2);
+    } else if (ahead) request_v(then, 0, next);
     there[0] = next[0];
     there[1] = next[1];
   }
   if (ahead) load_q(then);
-  pages[0] = pages_then[0];
-  pages[1] = pages_then[1];
-
-  // ---- the four wavefronts' results on one bound, added in their order
-  __syncthreads();                                  // the last piece's reads of LDS are over
+  pages = pages_then;
   l += other_row16(l);
   l += other_half(l);
-  if (lane < 16) sh.ml[wave][lane] = make_float2(m, l);
-  __syncthreads();
-  {
-    float top = -INFINITY;
+  if constexpr (!TEAM) {
+    // lane (col, quad) has row col, dimensions VD (4 quad + i) ..
+    if (col >= g.rows) return;
+    const float inv = l == 0.0f ? 0.0f : (SCALED ? a.v_scale[g.kvh] : 1.0f) / l;
+    uint16_t* dst = a.out + (size_t)(g.seq0 + col / group) * a.ld_out + (size_t)(g.kvh * group + col % group) * D;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, sh.ml[w][col].x);
-    const float shrink = exp2_fast(m - (top == -INFINITY ? 0.0f : top));
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float* to = &sh.merge[wave][col][VD * (4 * quad + i)];
-#pragma unroll
-      for (int j = 0; j < VD; j += 4)
-        *reinterpret_cast<f32x4*>(to + j) = f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]} * shrink;
-    }
-    __syncthreads();
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VD;
-    if (row < g.rows) {
-      float lr = 0.0f, mr = -INFINITY, x[VD];
-#pragma unroll
-      for (int w = 0; w < 4; ++w) mr = fmaxf(mr, sh.ml[w][row].x);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) lr += sh.ml[w][row].y * exp2_fast(sh.ml[w][row].x - (mr == -INFINITY ? 0.0f : mr));
-#pragma unroll
-      for (int j = 0; j < VD; ++j) x[j] = sh.merge[0][row][d0 + j] + sh.merge[1][row][d0 + j] + sh.merge[2][row][d0 + j] + sh.merge[3][row][d0 + j];
-      if (direct) {
-        const float inv = lr == 0.0f ? 0.0f : (SCALED ? a.v_scale[g.kvh] : 1.0f) / lr;
-        uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(g.kvh * group + row % group) * D + d0;
-#pragma unroll
-        for (int j = 0; j < VD; j += 4)
-          *reinterpret_cast<u32x2*>(dst + j) = u32x2{pack2(x[j] * inv, x[j + 1] * inv), pack2(x[j + 2] * inv, x[j + 3] * inv)};
-      } else {
-#pragma unroll
-        for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(o + (size_t)row * D + d0 + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
-        if (d0 == 0) ml_out[row] = make_float2(mr, lr);
+      for (int j = 0; j < VD; j += 4) {
+        const int d = VD * (4 * quad + i) + j;
+        if (direct) *reinterpret_cast<u32x2*>(dst + d) = u32x2{pack2(acc[j][i] * inv, acc[j + 1][i] * inv), pack2(acc[j + 2][i] * inv, acc[j + 3][i] * inv)};
+        else *reinterpret_cast<f32x4*>(o + (size_t)col * D + d) = f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
       }
-    }
+    if (!direct && quad == 0) ml_out[col] = make_float2(m, l);
+    return;
+  } else {
+
+  // ---- the four wavefronts' results on one bound, added in their order
+  if (lane < 16) sh->ml[wave][lane] = make_float2(m, l);
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, sh->ml[w][col].x);
+  const float shrink = exp2_fast(m - (top == -INFINITY ? 0.0f : top));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float* to = &sh->o[wave][col][VD * (4 * quad + i)];
+#pragma unroll
+    for (int j = 0; j < VD; j += 4)
+      *reinterpret_cast<f32x4*>(to + j) = f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]} * shrink;
+  }
+  __syncthreads();
+  const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * VD;
+  if (row >= g.rows) return;
+  float lr = 0.0f, mr = -INFINITY, x[VD];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mr = fmaxf(mr, sh->ml[w][row].x);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) lr += sh->ml[w][row].y * exp2_fast(sh->ml[w][row].x - (mr == -INFINITY ? 0.0f : mr));
+#pragma unroll
+  for (int j = 0; j < VD; ++j) x[j] = sh->o[0][row][d0 + j] + sh->o[1][row][d0 + j] + sh->o[2][row][d0 + j] + sh->o[3][row][d0 + j];
+  const float inv = lr == 0.0f ? 0.0f : (SCALED ? a.v_scale[g.kvh] : 1.0f) / lr;
+  uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(g.kvh * group + row % group) * D + d0;
+#pragma unroll
+  for (int j = 0; j < VD; j += 4)
+    *reinterpret_cast<u32x2*>(dst + j) = u32x2{pack2(x[j] * inv, x[j + 1] * inv), pack2(x[j + 2] * inv, x[j + 3] * inv)};
   }
   }
 };
 
 // The same for up to 128 rows: 32 per wavefront.
 template <int D, int SRC>
-__device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const Segment& g, Shared<D, true>& sh, bool direct, float* o, float2* ml_out) {
+__device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const Segment& g, TileLds<D>& tiles, bool direct, float* o, float2* ml_out) {
   constexpr int KS = D / 16, DT = D / 32;
   constexpr bool SCALED = SRC == KV_PAGED_E4M3;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), half = lane >> 5, row = kWaveRows * wave + (lane & 31);
   const int kvh = g.kvh;
-  Stage<D, SRC> stage(sh.tiles);
+  Stage<D, SRC> stage(tiles);
   stage.k = static_cast<const char*>(a.k);
   stage.v = static_cast<const char*>(a.v);
   stage.exponents[0] = a.k_exponent;
@@ -419,27 +418,36 @@ __device__ __forceinline__ void run_many(const DecodeArgs& a, int group, const S
   }
 }
 
-// MANY: prefixes are shared, or more than 16 query heads a key / value head: both bodies are there, also where no pass has more than 16 rows.  WHOLE: workgroup i does sequence i % n_seqs alone, and there is nothing to join.
-template <int D, int SRC, bool MANY, bool WHOLE>
-__global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCall c) {
+// Sequences of up to kWholeTokens: workgroup i does sequence i % n_seqs alone, and there is nothing to join.
+template <int D, int SRC>
+__global__ __launch_bounds__(kThreads, 3) void k_attn_decode_whole(DecodeCall c) {
+  __shared__ __align__(16) Merge<D> sh;
+  const DecodeArgs& a = c.a;
+  const int s = blockIdx.x % a.n_seqs, len = uniform(min(max(a.kv_len[s], 0), a.capacity));
+  const Segment g = {(int)blockIdx.x / a.n_seqs, s, s, c.sh.group, 0, len, 0, len};
+  Few<D, SRC, true> few(a, c.sh.group);
+  few.start(g);
+  few.run(g, true, false, g, &sh, true, nullptr, nullptr);
+}
+
+// MANY: prefixes are shared, or more than 16 query heads a key / value head.
+template <int D, int SRC, bool MANY>
+__global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
   __shared__ __align__(16) Shared<D, MANY> sh;
   const DecodeArgs& a = c.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int n_groups = MANY ? a.n_groups : 0, n_items = n_groups + a.n_seqs;
+  const bool wide = MANY && c.sh.group > kFewRows;  // sequences' own parts have too many rows for the small body, too
+  const int n_groups = MANY ? a.n_groups : 0, n_items = n_groups + a.n_seqs, n_many = wide ? n_items : n_groups;
   auto length = [&](int s) { return min(max(a.kv_len[s], 0), a.capacity); };
-  auto units = [](int from, int to) { return to > from ? (to - (from & ~63) + kUnit - 1) / kUnit : 0; };
+  auto tiles_of = [](int from, int to) { return to > from ? (to - (from & -kTile) + kTile - 1) / kTile : 0; };
+  auto steps_of = [](int from, int to) { return to > from ? (to - (from & -kStep) + kStep - 1) / kStep : 0; };
+  typedef Cost<SRC> C;
+  const uint32_t tile_cost = wide ? kWaves : C::kTile, begin_cost = wide ? 2 * kWaves : C::kBegin;   // (a workgroup's border at every tile)
+  auto many_cost = [&](int from, int to) { return to > from ? begin_cost + tiles_of(from, to) * tile_cost : 0u; };
+  auto own_cost = [&](int from, int to) { return wide ? many_cost(from, to) : to > from ? C::kOwn + steps_of(from, to) : 0u; };
 
-  if constexpr (WHOLE) {
-    Few<D, SRC> few(a, c.sh.group);
-    const int s = blockIdx.x % a.n_seqs;
-    const Segment g = {(int)blockIdx.x / a.n_seqs, s, s, c.sh.group, 0, uniform(length(s)), 0, uniform(length(s))};
-    few.start(g);
-    few.run(g, true, false, g, sh, true, nullptr, nullptr);
-    return;
-  }
-
-  // ---- units of every item, groups first
-  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[n_groups + s] = units(0, length(s));
+  // ---- cost of every item, groups first
+  for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[n_groups + s] = own_cost(0, length(s));
   __syncthreads();
   for (int g = wave; g < n_groups; g += 4) {
     const int first = a.first[g], behind = a.behind[g], prefix = a.prefix[g];
@@ -452,10 +460,10 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     const bool active = count >= 2;
     if (active)
       for (int s = first + lane; s < behind; s += 64)
-        if (length(s) >= prefix) sh.cum[n_groups + s] = units(prefix, length(s));
+        if (length(s) >= prefix) sh.cum[n_groups + s] = own_cost(prefix, length(s));
     if (lane == 0) {
       sh.group_src[g] = active ? src : -1;
-      sh.cum[g] = active ? (prefix + kUnit - 1) / kUnit * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
+      sh.cum[g] = active ? many_cost(0, prefix) * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
     }
   }
   __syncthreads();
@@ -467,114 +475,160 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     my_prefix = a.prefix[lane];
   }
   auto shared_by = [&](int s, int len) {            // the prefix that a sequence (the same in all lanes) shares with others
+    if (!MANY) return 0;
     const uint64_t who = __ballot(my_first <= s && s < my_behind && len >= my_prefix);
     return who ? __builtin_amdgcn_readlane(my_prefix, __builtin_ctzll(who)) : 0;
   };
   // ---- exclusive sums, in place
   {
     const int per = (n_items + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * per, n_items), hi = min(lo + per, n_items);
-    int sum = 0;
+    uint32_t sum = 0;
     for (int i = lo; i < hi; ++i) sum += sh.cum[i];
-    const int run = wave_scan(sum);
+    const uint32_t run = (uint32_t)wave_scan((int)sum);
     if (lane == 63) sh.part[wave] = run;
     __syncthreads();
-    int at = run - sum;
+    uint32_t at = run - sum;
     for (int w = 0; w < wave; ++w) at += sh.part[w];
     for (int i = lo; i < hi; ++i) {
-      const int v = sh.cum[i];
+      const uint32_t v = sh.cum[i];
       sh.cum[i] = at;
       at += v;
     }
     if (threadIdx.x == kThreads - 1) sh.cum[n_items] = sh.part[0] + sh.part[1] + sh.part[2] + sh.part[3];
     __syncthreads();
   }
-  const int per_head = uniform(sh.cum[n_items]), all = per_head * a.n_kv_heads;
-  const int chunk = max((all + (int)gridDim.x - 1) / (int)gridDim.x, 1);
+  // The line: what the larger body does, all heads, then, from a workgroup's border on, the rest, all heads.  Wavefront w has costs
+  // [w chunk, (w + 1) chunk); of the larger body's part the workgroup's wavefronts do theirs together.
+  const uint32_t many_head = uniform(sh.cum[n_many]), all_head = uniform(sh.cum[n_items]), few_head = all_head - many_head;
+  const uint32_t many_all = many_head * a.n_kv_heads, few_all = few_head * a.n_kv_heads;
+  const uint32_t shares = kWaves * (many_all && few_all && gridDim.x > 1 ? gridDim.x - 1 : gridDim.x);
+  // (at least a tile's cost each, so that none of the workgroups that a pass is cut over is without a tile)
+  const uint32_t chunk = max((uint32_t)(((uint64_t)many_all + few_all + shares - 1) / shares), MANY ? (tile_cost + kWaves - 1) / kWaves : 1u);
+  const uint32_t each = kWaves * chunk, few_from = (many_all + each - 1) / each * each, all = few_from + few_all;
+  auto end_of = [&](uint32_t number, uint32_t each, uint32_t most) { return (uint32_t)min((uint64_t)number * each, (uint64_t)most); };
 
   const Layout y = layout(a.n_seqs, a.n_kv_heads, c.sh.group, c.sh.n_passes, D);
   char* ws = static_cast<char*>(a.ws);
+  float* own_o = reinterpret_cast<float*>(ws + y.own_o);
+  float2* own_ml = reinterpret_cast<float2*>(ws + y.own_ml);
 
-  // ---- this workgroup's chunk, piece by piece
-  const int begin = (int)min((int64_t)blockIdx.x * chunk, (int64_t)all), end = min(begin + chunk, all);
-  struct Piece {
-    Segment g;
-    int units;
-    bool direct;
-    float* o;
-    float2* ml;
-  };
-  auto piece_at = [&](int u) {
-    Piece p;
-    Segment& g = p.g;
-    const int h = u / per_head, in_head = u % per_head;
-    int lo = 0, hi = n_items - 1;                   // last item that begins at or before the unit (those of no units come before it)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (sh.cum[mid] <= in_head) lo = mid; else hi = mid - 1;
-    }
-    const int it = uniform(lo), first = uniform(sh.cum[it]), n = uniform(sh.cum[it + 1]) - first;
-    int from_unit = in_head - first, to_unit = min(from_unit + end - u, n);
-    g.kvh = h;
-    p.direct = false;
-    if (it < n_groups) {
-      const int tiles = (a.prefix[it] + kUnit - 1) / kUnit, pass = from_unit / tiles;
-      from_unit -= pass * tiles;
-      to_unit = min(to_unit - pass * tiles, tiles);
-      g.seq = uniform(sh.group_src[it]);
-      g.seq0 = a.first[it] + pass * c.sh.per_pass;
-      g.rows = min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group;
-      g.from = 0;
-      g.to = a.prefix[it];
-      g.t0 = from_unit * kUnit;
-      g.t1 = min(to_unit * kUnit, g.to);
-      const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
-      p.o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
-      p.ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
-    } else {
-      const int s = it - n_groups;
-      g.seq = g.seq0 = s;
-      g.rows = c.sh.group;
-      g.to = uniform(length(s));
-      g.from = shared_by(s, g.to);
-      const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
-      p.direct = g.from == 0 && from_unit == 0 && to_unit == n;
-      p.o = reinterpret_cast<float*>(ws + y.own_o) + slot * c.sh.group * D;
-      p.ml = reinterpret_cast<float2*>(ws + y.own_ml) + slot * c.sh.group;
-      g.t0 = (g.from & ~63) + from_unit * kUnit;
-      g.t1 = min((g.from & ~63) + to_unit * kUnit, g.to);
-    }
-    g.t0 = uniform(g.t0);
-    g.t1 = uniform(g.t1);
-    g.rows = uniform(g.rows);
-    p.units = uniform(to_unit - from_unit);
-    return p;
-  };
-  // first the pieces of many rows, then the others: in one loop both bodies would keep registers for each other
+  // ---- the larger body's part: a tile is the workgroup's whose costs it begins in
   if constexpr (MANY) {
-    for (int u = begin; u < end;) {
-      const Piece p = piece_at(u);
-      u += p.units;
-      if (p.g.rows > kFewRows) run_many<D, SRC>(a, c.sh.group, p.g, sh, p.direct, p.o, p.ml);
+    const uint32_t end = end_of(blockIdx.x + 1, each, many_all);
+    auto tiles_before = [&](uint32_t cost) { return cost > begin_cost ? (cost - begin_cost + tile_cost - 1) / tile_cost : 0u; };   // that begin there
+    for (uint32_t u = end_of(blockIdx.x, each, many_all); u < end;) {
+      const int h = uniform(u / many_head);
+      const uint32_t in_head = u - h * many_head;
+      int lo = 0, hi = n_many - 1;                  // last item that begins at or before u (those of no cost come before it)
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (sh.cum[mid] <= in_head) lo = mid; else hi = mid - 1;
+      }
+      const int it = uniform(lo);
+      uint32_t first = h * many_head + uniform(sh.cum[it]), behind = h * many_head + uniform(sh.cum[it + 1]);
+      Segment g;
+      bool direct = false;
+      float* o;
+      float2* ml;
+      g.kvh = h;
+      if (it < n_groups) {
+        const uint32_t per_pass = many_cost(0, a.prefix[it]);
+        const int pass = uniform((u - first) / per_pass);
+        first += pass * per_pass;
+        behind = first + per_pass;
+        g.seq = uniform(sh.group_src[it]);
+        g.seq0 = a.first[it] + pass * c.sh.per_pass;
+        g.rows = uniform(min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group);
+        g.from = 0;
+        g.to = a.prefix[it];
+        const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
+        o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
+        ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
+      } else {
+        const int s = it - n_groups;
+        g.seq = g.seq0 = s;
+        g.rows = c.sh.group;
+        g.to = uniform(length(s));
+        g.from = shared_by(s, g.to);
+        const size_t slot = (size_t)blockIdx.x + (size_t)h * a.n_seqs + s;
+        o = own_o + slot * c.sh.group * D;
+        ml = own_ml + slot * c.sh.group;
+      }
+      const uint32_t stop = min(end, behind);
+      const int tile0 = uniform(tiles_before(u - first)), tile1 = uniform(tiles_before(stop - first));
+      u = stop;
+      if (tile0 == tile1) continue;
+      if (it >= n_groups) direct = g.from == 0 && tile0 == 0 && tile1 == (int)tiles_before(behind - first);
+      g.t0 = (g.from & -kTile) + tile0 * kTile;
+      g.t1 = min((g.from & -kTile) + tile1 * kTile, g.to);
+      run_many<D, SRC>(a, c.sh.group, g, sh.tiles, direct, o, ml);
     }
     asm volatile("" ::: "memory");
   }
-  int u = begin;
-  auto next_few = [&](Piece& p) {
-    while (u < end) {
-      p = piece_at(u);
-      u += p.units;
-      if (!MANY || p.g.rows <= kFewRows) return true;
+
+  // ---- the wavefront's own part, piece by piece
+  if (!wide) {
+    const uint32_t number = blockIdx.x * kWaves + wave;
+    uint32_t u = max(end_of(number, chunk, all), few_from) - few_from;
+    const uint32_t end = max(end_of(number + 1, chunk, all), few_from) - few_from;
+    struct Piece {
+      Segment g;
+      bool direct;
+      float* o;
+      float2* ml;
+    };
+    int h = 0, it = n_groups;
+    uint32_t first = 0;                             // cost before the item
+    if (u < end) {
+      h = uniform(u / few_head);
+      const uint32_t in_head = u - h * few_head + many_head;
+      int lo = n_groups, hi = n_items - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (sh.cum[mid] <= in_head) lo = mid; else hi = mid - 1;
+      }
+      it = uniform(lo);
     }
-    return false;
-  };
-  Piece p, then;
-  Few<D, SRC> few(a, c.sh.group);
-  for (int round = 0;; ++round) {
-    const bool more = next_few(then);               // while the first tokens of piece p are on their way
-    if (round) few.run(p.g, round == 1, more, then.g, sh, p.direct, p.o, p.ml);
-    else if (more) few.start(then.g);
-    if (!more) break;
-    p = then;
+    auto next = [&](Piece& p) {
+      while (u < end) {
+        const uint32_t before = uniform(sh.cum[it]), cost = uniform(sh.cum[it + 1]) - before;
+        first = h * few_head + before - many_head;
+        const uint32_t stop = min(end, first + cost);
+        if (cost && stop > first + C::kOwn) {
+          const int s = it - n_groups;
+          Segment& g = p.g;
+          g.kvh = h;
+          g.seq = g.seq0 = s;
+          g.rows = c.sh.group;
+          g.to = uniform(length(s));
+          g.from = uniform(shared_by(s, g.to));
+          const uint32_t from_step = u > first + C::kOwn ? u - first - C::kOwn : 0, to_step = stop - first - C::kOwn;
+          p.direct = g.from == 0 && from_step == 0 && stop == first + cost;
+          const size_t slot = (size_t)number + (size_t)h * a.n_seqs + s;
+          p.o = own_o + slot * c.sh.group * D;
+          p.ml = own_ml + slot * c.sh.group;
+          g.t0 = uniform((g.from & -kStep) + from_step * kStep);
+          g.t1 = uniform(min((int)((g.from & -kStep) + to_step * kStep), g.to));
+        }
+        const bool found = cost && stop > first + C::kOwn;
+        u = stop;
+        if (u == first + cost && ++it == n_items) {
+          it = n_groups;
+          ++h;
+        }
+        if (found) return true;
+      }
+      return false;
+    };
+    Piece p, then;
+    Few<D, SRC, false> few(a, c.sh.group);
+    for (int round = 0;; ++round) {
+      const bool more = next(then);                 // while the first tokens of piece p are on their way
+      if (round) few.run(p.g, round == 1, more, then.g, nullptr, p.direct, p.o, p.ml);
+      else if (more) few.start(then.g);
+      if (!more) break;
+      p = then;
+    }
   }
 
   // ---- where the join finds every row's pieces
@@ -585,16 +639,17 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
     for (int g = 0; g < n_groups; ++g) {
       if (s < a.first[g] || s >= a.behind[g]) continue;
       if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
-        const int n = (a.prefix[g] + kUnit - 1) / kUnit, pass = (s - a.first[g]) / c.sh.per_pass;
-        const int u0 = h * per_head + sh.cum[g] + pass * n, w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
+        const uint32_t n = many_cost(0, a.prefix[g]), pass = (s - a.first[g]) / c.sh.per_pass;
+        const uint32_t u0 = h * many_head + sh.cum[g] + pass * n, w0 = (u0 + begin_cost) / each, w1 = (u0 + n - tile_cost) / each;
         w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
         w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
       }
       break;
     }
-    const int u0 = h * per_head + sh.cum[it], n = sh.cum[it + 1] - sh.cum[it];
-    if (n > 0) {
-      const int w0 = u0 / chunk, w1 = (u0 + n - 1) / chunk;
+    const uint32_t cost = sh.cum[it + 1] - sh.cum[it];
+    if (cost) {
+      const uint32_t u0 = wide ? h * many_head + sh.cum[it] + begin_cost : few_from + h * few_head + sh.cum[it] - many_head + C::kOwn;
+      const uint32_t last = u0 + cost - (wide ? begin_cost + tile_cost : C::kOwn + 1), by = wide ? each : chunk, w0 = u0 / by, w1 = last / by;
       w.x = w0 + i;
       w.y = w0 == w1 && w.w == 0 ? -1 : w1 - w0 + 1;
     }
@@ -602,14 +657,14 @@ __global__ __launch_bounds__(kThreads, MANY ? 2 : 3) void k_attn_decode(DecodeCa
   }
 }
 
-// One wavefront (W = 4: four, sharing out the pieces) per query row: the pieces of its prefix and its own, on one bound.
+// One wavefront (W > 1: a workgroup of W, sharing out the pieces) per query row: the pieces of its prefix and its own, on one bound.
 template <int D, int W>
-__global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool scaled) {
+__global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void k_join(DecodeCall c, bool scaled) {
   constexpr int E = D / 64;                          // dimensions per lane
-  __shared__ float part[4][D];
+  __shared__ float part[W][D];
   const DecodeArgs& a = c.a;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), group = c.sh.group;
-  const int row = W == 4 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
+  const int row = W > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
   if (row >= a.n_seqs * a.n_heads) return;
   const int s = row / a.n_heads, head = row % a.n_heads, h = head / group, r = head % group;
   const Layout y = layout(a.n_seqs, a.n_kv_heads, group, c.sh.n_passes, D);
@@ -642,7 +697,7 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool scaled) {
     m = raised;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] *= shrink;
-    for (int k0 = W == 4 ? wave : 0; k0 < count; k0 += W * kBatch) {
+    for (int k0 = W > 1 ? wave : 0; k0 < count; k0 += W * kBatch) {
       float v[kBatch][E], f[kBatch];
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
@@ -658,13 +713,15 @@ __global__ __launch_bounds__(kThreads) void k_join(DecodeCall c, bool scaled) {
         for (int e = 0; e < E; ++e) x[e] = k0 + W * b < count ? fmaf(f[b], v[b][e], x[e]) : x[e];
     }
   }
-  if constexpr (W == 4) {                            // all four have the same bound and sum
+  if constexpr (W > 1) {                             // all of them have the same bound and sum
 #pragma unroll
     for (int e = 0; e < E; ++e) part[wave][E * lane + e] = x[e];
     __syncthreads();
     if (wave) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = part[0][E * lane + e] + part[1][E * lane + e] + part[2][E * lane + e] + part[3][E * lane + e];
+    for (int w = 1; w < W; ++w)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] += part[w][E * lane + e];
   }
   const float inv = l == 0.0f ? 0.0f : (scaled ? a.v_scale[h] : 1.0f) / l;
   uint16_t* dst = a.out + (size_t)s * a.ld_out + (size_t)head * D + E * lane;
@@ -676,17 +733,18 @@ template <int D, int SRC>
 hipError_t launch(const DecodeCall& c, hipStream_t s) {
   const bool many = c.sh.group > kFewRows || c.a.n_groups > 0;
   if (!many && c.a.capacity <= kWholeTokens) {
-    k_attn_decode<D, SRC, false, true><<<(unsigned)(c.a.n_kv_heads * c.a.n_seqs), kThreads, 0, s>>>(c);
+    k_attn_decode_whole<D, SRC><<<(unsigned)(c.a.n_kv_heads * c.a.n_seqs), kThreads, 0, s>>>(c);
     return hipGetLastError();
   }
-  // never more workgroups than units there can be
-  const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kUnit - 1) / kUnit + 1);
-  const unsigned grid = (unsigned)std::min<int64_t>(many ? kWorkgroups : kWorkgroupsFew, most);
-  if (many) k_attn_decode<D, SRC, true, false><<<grid, kThreads, 0, s>>>(c);
-  else k_attn_decode<D, SRC, false, false><<<grid, kThreads, 0, s>>>(c);
+  // never more workgroups than steps there can be
+  const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kStep - 1) / kStep + 1);
+  const unsigned grid = (unsigned)std::min<int64_t>(kWorkgroups, most);
+  if (many) k_attn_decode<D, SRC, true><<<grid, kThreads, 0, s>>>(c);
+  else k_attn_decode<D, SRC, false><<<grid, kThreads, 0, s>>>(c);
   if (hipError_t e = hipGetLastError()) return e;
   const int rows = c.a.n_seqs * c.a.n_heads;
-  if (rows <= 1024) k_join<D, 4><<<rows, kThreads, 0, s>>>(c, SRC == KV_PAGED_E4M3);
+  if (rows <= 64) k_join<D, 16><<<rows, 1024, 0, s>>>(c, SRC == KV_PAGED_E4M3);
+  else if (rows <= 1024) k_join<D, 4><<<rows, kThreads, 0, s>>>(c, SRC == KV_PAGED_E4M3);
   else k_join<D, 1><<<(rows + 3) / 4, kThreads, 0, s>>>(c, SRC == KV_PAGED_E4M3);
   return hipGetLastError();
 }
