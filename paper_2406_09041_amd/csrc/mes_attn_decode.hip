@@ -160,12 +160,12 @@ struct Few {
   }
   __device__ __forceinline__ static int lane_of(int step, int half) { return (step & (kBatch - 1)) * 2 + half; }
   __device__ __forceinline__ float power(int h, int kv, int i) const { return power_of(exponent_of(__builtin_amdgcn_readlane(exponents[kv], lane_of(i, h)))); }
-  __device__ __forceinline__ void load_q(const Segment& g) {
+  __device__ __forceinline__ void load_q(const Segment& g, u32x4 (&to)[KS]) const {
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
-      q[c] = u32x4{0, 0, 0, 0};
+      to[c] = u32x4{0, 0, 0, 0};
       if (col < g.rows)
-        q[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(g.kvh * group + col % group) * D + dim_of<D, SRC>(c, quad));
+        to[c] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(g.seq0 + col / group) * a.ld_q + (size_t)(g.kvh * group + col % group) * D + dim_of<D, SRC>(c, quad));
     }
   }
   __device__ __forceinline__ size_t row_of(const Segment& g, int t, int page) const {   // first element of token t's row
@@ -195,7 +195,7 @@ struct Few {
   }
   __device__ __forceinline__ void start(const Segment& g) {   // a piece that nobody has asked for
     pages = look_up(g, 0);
-    load_q(g);
+    load_q(g, q);
     look_up_exponents(g, 0, pages);
     raw = R{};
     there[0] = there[1] = -1;
@@ -213,7 +213,12 @@ struct Few {
   for (int j = 0; j < VD; ++j) acc[j] = f32x4{0, 0, 0, 0};
   const int mine = steps(g);
   int pages_then = -1, pages_next = -1;             // of the next piece, of this one's next batch
-  if (ahead) pages_then = look_up(then, 0);
+  u32x4 q_then[KS];                                 // asked for long before it is needed: a wavefront would wait for it between pieces
+  if (ahead) {
+    pages_then = look_up(then, 0);
+    load_q(then, q_then);
+  }
+  const bool another = ahead;
   ahead = ahead && steps(then) > 0;
   for (int i = fresh || mine == 0 ? -1 : 0; i < mine; ++i) {
     const int t = token_of(g, i);
@@ -311,7 +316,10 @@ struct Few {
     there[0] = next[0];
     there[1] = next[1];
   }
-  if (ahead) load_q(then);
+  if (another) {
+#pragma unroll
+    for (int c = 0; c < KS; ++c) q[c] = q_then[c];
+  }
   pages = pages_then;
   l += other_row16(l);
   l += other_half(l);
