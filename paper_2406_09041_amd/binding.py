@@ -721,16 +721,18 @@ def mes_rotary(angles: Angles, positions: torch.Tensor, q: torch.Tensor, k: Opti
     kv_heads = ld_k = ld_ko = 0
     fresh = q_out is None
     if fresh:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    n, h, d, ld_qo = _rows("q_out", q_out, index, kind)
-    assert (n, h, d) == (T, heads, dim)
+        q_out, ld_qo = torch.empty((T, heads, dim), dtype=kind, device=q.device), heads * dim
+    else:
+        n, h, d, ld_qo = _rows("q_out", q_out, index, kind)
+        assert (n, h, d) == (T, heads, dim)
     if k is not None:
         n, kv_heads, d, ld_k = _rows("k", k, index, kind)
         assert (n, d) == (T, dim), "k: as many rows as q"
         if fresh:
-            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        n, h, d, ld_ko = _rows("k_out", k_out, index, kind)
-        assert (n, h, d) == (T, kv_heads, dim)
+            k_out, ld_ko = torch.empty((T, kv_heads, dim), dtype=kind, device=q.device), kv_heads * dim
+        else:
+            n, h, d, ld_ko = _rows("k_out", k_out, index, kind)
+            assert (n, h, d) == (T, kv_heads, dim)
     _call_on(index, lib.mes_rotary, angles.ref, positions.data_ptr(), q.data_ptr(), None if k is None else k.data_ptr(), T, heads, kv_heads, dim, ld_q, ld_k,
              0 if kind is _BF16 else 1, int(transpose), q_out.data_ptr(), ld_qo, None if k is None else k_out.data_ptr(), ld_ko, int(fresh))
     return q_out if k is None else (q_out, k_out)
@@ -776,14 +778,15 @@ def mes_kv_read(cache: KvCache, layer: int, batch: SeqBatch, T: int, k_out: Opti
     sequence are left as they are in outputs that are given, and 0 where these are allocated."""
     index = cache.index
     assert batch.index == index
-    fresh = k_out is None and v_out is None
+    fresh, heads, dim = k_out is None and v_out is None, cache.n_kv_heads, cache.head_dim
+    ld = [heads * dim] * 2
     if fresh:
-        k_out, v_out = (torch.empty((max(T, 0), cache.n_kv_heads, cache.head_dim), dtype=_BF16, device=cache.device) for _ in range(2))
-    ld = [0, 0]
-    for i, t in enumerate((k_out, v_out)):
-        if t is not None:
-            *shape, ld[i] = _rows("k_out / v_out", t, index)
-            assert shape == [T, cache.n_kv_heads, cache.head_dim], "k_out, v_out: [T, n_kv_heads, head_dim] of the cache"
+        k_out, v_out = torch.empty((2, max(T, 0), heads, dim), dtype=_BF16, device=cache.device)
+    else:
+        for i, t in enumerate((k_out, v_out)):
+            if t is not None:
+                *shape, ld[i] = _rows("k_out / v_out", t, index)
+                assert shape == [T, heads, dim], "k_out, v_out: [T, n_kv_heads, head_dim] of the cache"
     _call_on(index, lib.mes_kv_read, cache.ref, layer, batch.ref, T, None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(),
              *ld, int(fresh))
     return k_out, v_out

@@ -57,26 +57,25 @@ struct Place {
   int seq, pos;                                            // -1: behind the last sequence; < 0 or past the capacity: none
   int from, to;                                            // positions [from, to) of the sequence's rows
 };
+// The first s with offsets[s + 1] > t, n where there is none; t is the same in all 64 lanes.  Two dependent loads (one up to 64 sequences), where
+// a search by halves would take one for each.
+__device__ __forceinline__ int sequence_of(const int32_t* offsets, int n, int t) {
+  if (n == 0) return 0;
+  const int lane = threadIdx.x & 63, step = (n + 63) >> 6;
+  const int first = __popcll(__ballot(offsets[min((lane + 1) * step, n)] <= t)) * step;
+  if (step == 1 || first >= n) return min(first, n);
+  return min(first + __popcll(__ballot(lane < step && offsets[min(first + lane + 1, n)] <= t)), n);
+}
+// s: the row's sequence, by sequence_of
 template <class A>
-__device__ __forceinline__ Place place_of(const A& a, int t) {
-  int s = t, begin = t, end = t + 1;                       // the sequence's rows
-  if (a.q_offsets) {
-    int lo = 0, hi = a.n_seqs;                             // first s with q_offsets[s + 1] > t
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (a.q_offsets[mid + 1] > t) hi = mid; else lo = mid + 1;
-    }
-    s = lo;
-    if (s < a.n_seqs) {
-      begin = a.q_offsets[s];
-      end = a.q_offsets[s + 1];
-    }
-    if (begin > t) s = a.n_seqs;
-  }
+__device__ __forceinline__ Place place_in(const A& a, int t, int s) {
   if (s >= a.n_seqs) return {-1, -1, 0, 0};
-  const int len = max(a.kv_len[s], 0);
+  const int begin = a.q_offsets ? a.q_offsets[s] : t, end = a.q_offsets ? a.q_offsets[s + 1] : t + 1, len = max(a.kv_len[s], 0);
+  if (begin > t) return {-1, -1, 0, 0};
   return {s, len - (end - t), max(len - (end - begin), 0), min(len, a.capacity)};
 }
+template <class A>
+__device__ __forceinline__ Place place_of(const A& a, int t) { return place_in(a, t, a.q_offsets ? sequence_of(a.q_offsets, a.n_seqs, t) : t); }
 
 // q's part of a row: turned, rounded once, to q_out; 0 where the row has no place and nothing is there yet
 __device__ __forceinline__ void append_queries(const AppendArgs& a, int t, const float* turn, bool real) {
@@ -221,45 +220,44 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_blocks(AppendArgs a) 
   }
 }
 
-// Reading back: a thread 16 dimensions of a token.  Workgroups take kReadRows rows; keys and values of a head are read in the order of the page.
-constexpr int kReadThreads = 256, kReadRows = 16;
+// Reading back: a thread 8 dimensions of a token, so that the stores of a wavefront are whole lines.  Workgroups take kReadRows rows; keys and
+// values of a head are read in the order of the page, kReadBatch units of a thread on their way before the first is written.
+constexpr int kReadThreads = 256, kReadRows = 8, kReadBatch = 8;
 
 template <int DTYPE>
-__device__ __forceinline__ void read16(const void* base, size_t element, float scale, uint16_t* to) {
-  if constexpr (DTYPE == MES_KV_BF16) {
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + element);
-    const uint4 x = p[0], y = p[1];
-    reinterpret_cast<uint4*>(to)[0] = x;
-    reinterpret_cast<uint4*>(to)[1] = y;
-  } else {
-    const uint4 c = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + element);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t v[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (DTYPE == MES_KV_E4M3_BLOCKS) {
-        v[2 * i] = widen2<false>(w[i], scale);
-        v[2 * i + 1] = widen2<true>(w[i], scale);
-      } else {
-        v[2 * i] = pack_bf16(code_at<0>(w[i]) * scale, code_at<1>(w[i]) * scale);
-        v[2 * i + 1] = pack_bf16(code_at<2>(w[i]) * scale, code_at<3>(w[i]) * scale);
-      }
-    }
-    reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+struct Codes8 {                                            // 8 dimensions as the cache holds them
+  std::conditional_t<DTYPE == MES_KV_BF16, uint4, uint2> w;
+  __device__ __forceinline__ void load(const void* base, size_t element) {
+    w = *reinterpret_cast<const decltype(w)*>(static_cast<const char*>(base) + element * (DTYPE == MES_KV_BF16 ? 2 : 1));
   }
-}
+  __device__ __forceinline__ void store(uint16_t* to, float scale) const {
+    uint4 v;
+    if constexpr (DTYPE == MES_KV_BF16) {
+      v = w;
+    } else if constexpr (DTYPE == MES_KV_E4M3_BLOCKS) {
+      v = make_uint4(widen2<false>(w.x, scale), widen2<true>(w.x, scale), widen2<false>(w.y, scale), widen2<true>(w.y, scale));
+    } else {
+      v = make_uint4(pack_bf16(code_at<0>(w.x) * scale, code_at<1>(w.x) * scale), pack_bf16(code_at<2>(w.x) * scale, code_at<3>(w.x) * scale),
+                     pack_bf16(code_at<0>(w.y) * scale, code_at<1>(w.y) * scale), pack_bf16(code_at<2>(w.y) * scale, code_at<3>(w.y) * scale));
+    }
+    *reinterpret_cast<uint4*>(to) = v;
+  }
+};
 
 template <int DTYPE, int D>
 __global__ __launch_bounds__(kReadThreads) void k_read(ReadArgs a) {
-  constexpr int kChunks = D / 16;
+  constexpr int kChunks = D / 8;
   __shared__ int pages[kReadRows], slots[kReadRows];       // page -1: absent, -2: no row of a sequence
   const int t0 = blockIdx.x * kReadRows;
-  if (threadIdx.x < kReadRows) {
+  if (threadIdx.x < 64) {
+    int seq = a.q_offsets ? sequence_of(a.q_offsets, a.n_seqs, t0) : t0;
     const int t = t0 + threadIdx.x;
     int page = -2, slot = 0;
-    if (t < a.T) {
-      const Place at = place_of(a, t);
+    if (threadIdx.x < kReadRows && t < a.T) {
+      if (a.q_offsets)
+        while (seq < a.n_seqs && a.q_offsets[seq + 1] <= t) ++seq;
+      else seq = t;
+      const Place at = place_in(a, t, seq);
       if (at.seq >= 0) {
         page = -1;
         if (at.pos >= 0 && at.pos < a.capacity) {
@@ -269,26 +267,37 @@ __global__ __launch_bounds__(kReadThreads) void k_read(ReadArgs a) {
         }
       }
     }
-    pages[threadIdx.x] = page;
-    slots[threadIdx.x] = slot;
+    if (threadIdx.x < kReadRows) {
+      pages[threadIdx.x] = page;
+      slots[threadIdx.x] = slot;
+    }
   }
   __syncthreads();
   const int half = a.n_kv_heads * kReadRows * kChunks;
-  for (int w = threadIdx.x; w < 2 * half; w += kReadThreads) {
-    const bool key = w < half;
-    const int z = key ? w : w - half, c = z % kChunks, r = z / kChunks % kReadRows, h = z / (kChunks * kReadRows), page = pages[r], slot = slots[r];
-    uint16_t* out = key ? a.k : a.v;
-    if (!out || t0 + r >= a.T || (page == -2 && !a.fresh)) continue;
-    out += (size_t)(t0 + r) * (key ? a.ld_k : a.ld_v) + (size_t)h * D + c * 16;
-    if (page < 0) {
-      reinterpret_cast<uint4*>(out)[0] = make_uint4(0, 0, 0, 0);
-      reinterpret_cast<uint4*>(out)[1] = make_uint4(0, 0, 0, 0);
-      continue;
+  for (int w0 = threadIdx.x; w0 < 2 * half; w0 += kReadBatch * kReadThreads) {
+    Codes8<DTYPE> codes[kReadBatch];
+    float scale[kReadBatch];
+    uint16_t* out[kReadBatch];
+#pragma unroll
+    for (int b = 0; b < kReadBatch; ++b) {
+      const int w = w0 + b * kReadThreads;
+      const bool key = w < half;
+      const int z = key ? w : w - half, c = z % kChunks, r = z / kChunks % kReadRows, h = z / (kChunks * kReadRows);
+      out[b] = key ? a.k : a.v;
+      scale[b] = 1.0f;
+      codes[b] = {};
+      const int page = w < 2 * half ? pages[r] : -2, slot = slots[r];
+      if (page == -2 && !(a.fresh && w < 2 * half && t0 + r < a.T)) out[b] = nullptr;
+      if (!out[b]) continue;
+      out[b] += (size_t)(t0 + r) * (key ? a.ld_k : a.ld_v) + (size_t)h * D + c * 8;
+      if (page < 0) continue;                              // 0
+      if constexpr (DTYPE == MES_KV_E4M3) scale[b] = (key ? a.k_scale : a.v_scale)[h];
+      if constexpr (DTYPE == MES_KV_E4M3_BLOCKS) scale[b] = power_of(exponent_of((key ? a.k_exponent : a.v_exponent)[block_at(page, h, a.n_kv_heads, a.page_shift, slot)]));
+      codes[b].load(key ? a.k_cache : a.v_cache, (((((size_t)page * a.n_kv_heads + h) << a.page_shift) + slot) * D) + c * 8);
     }
-    float scale = 1.0f;
-    if constexpr (DTYPE == MES_KV_E4M3) scale = (key ? a.k_scale : a.v_scale)[h];
-    if constexpr (DTYPE == MES_KV_E4M3_BLOCKS) scale = power_of(exponent_of((key ? a.k_exponent : a.v_exponent)[block_at(page, h, a.n_kv_heads, a.page_shift, slot)]));
-    read16<DTYPE>(key ? a.k_cache : a.v_cache, (((((size_t)page * a.n_kv_heads + h) << a.page_shift) + slot) * D) + c * 16, scale, out);
+#pragma unroll
+    for (int b = 0; b < kReadBatch; ++b)
+      if (out[b]) codes[b].store(out[b], scale[b]);
   }
 }
 
