@@ -364,7 +364,8 @@ typedef struct {
  * MES_KV_E4M3_BLOCKS: a block gets the least exponent under which the finite ones of its new values are at most 448 codes; where it holds
  * tokens of the sequence before the call's first, their exponent, if that is larger, and where it is smaller their codes
  * are rounded to the new one (exactly, but for codes that become subnormal).  What is infinite becomes the largest code
- * (240 under the largest exponent, so that its value is finite), NaN stays NaN.  What a block held behind the new tokens is lost.
+ * (240 under the largest exponent, so that its value is finite), NaN stays NaN.  What a block held behind the new tokens is lost, and no
+ * two sequences of a call write to one block (pages that mes_pages_grow has seen to are one sequence's).
  * Rows without a place (see mes_seqs) are left out: nothing is written for rows before position 0, past the table's room
  * or behind the last sequence; on a page outside the cache only q_out is.  Two rows of one call must not share a place. */
 mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,
@@ -404,7 +405,8 @@ mes_status mes_rotary_table(float* table, int n_positions, int dims, double base
 /* Turns rows outside a cache (what mes_attn_prompt takes): q [T][n_heads][head_dim] to q_out and, where k is not NULL, k
  * [T][n_kv_heads][head_dim] to k_out, row t by the angles of positions[t] (DEVICE int32 [T]).  Every product and sum is rounded to fp32, the result
  * once to the rows' type: MES_ROWS_BF16 or MES_ROWS_FP32.  transpose: 1 turns back by the same cosines and sines, (a c + b s, b c - a s): the
- * gradient of the rows where `q` and `k` are those of the turned rows.  q_out may be q, k_out k (rows as far apart).
+ * gradient of the rows where `q` and `k` are those of the turned rows.  q_out may be q, k_out k (rows as far apart); else outputs
+ * overlap no input.
  * head_dim: a multiple of 16 up to 512.  Rows ld_* elements apart, 16-byte aligned, as for the attention calls.
  * Rows whose position is outside the table (-1: one that pads the batch) are left as they are in q_out / k_out, with fresh = 1 (outputs that
  * are not the inputs and whose memory holds nothing yet) set to 0. */

@@ -749,26 +749,27 @@ def mes_kv_append(cache: KvCache, layer: int, batch: SeqBatch, q: Optional[torch
     assert batch.index == index and rows_v[:3] == (T, kv_heads, dim) == (T, cache.n_kv_heads, cache.head_dim), "k, v: [T, n_kv_heads, head_dim] of the cache"
     heads = ld_q = ld_o = n_pos = 0
     rot = src = dst = None
-    fresh = False
-    if isinstance(rotary, Angles):
+    fresh, turned = q is not None and q_out is None, type(rotary) is Angles
+    if turned:
         assert rotary.index == index, f"angles on device {index}"
-        rot = rotary.ref
     elif rotary is not None:
         assert rotary.dtype is torch.float32 and rotary.is_contiguous() and rotary.get_device() == index and rotary.shape[1:] == (2, dim // 2)
         n_pos, rot = rotary.shape[0], rotary.data_ptr()
     if q is not None:
         n, heads, d, ld_q = _rows("q", q, index)
         assert n == T and d == dim
-        if q_out is None:
-            q_out, fresh = torch.empty_like(q, memory_format=torch.contiguous_format), True
-        n, h, d, ld_o = _rows("q_out", q_out, index)
-        assert (n, h, d) == (T, heads, dim)
+        if fresh:
+            q_out, ld_o = torch.empty_like(q, memory_format=torch.contiguous_format), heads * dim
+        else:
+            n, h, d, ld_o = _rows("q_out", q_out, index)
+            assert (n, h, d) == (T, heads, dim)
         src, dst = q.data_ptr(), q_out.data_ptr()
-    rows = (cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3])
-    if isinstance(rotary, Angles):
-        _call_on(index, lib.mes_kv_append_angles, *rows, rot, dst, ld_o, int(fresh))
+    if turned:
+        _call_on(index, lib.mes_kv_append_angles, cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q, ld_k, rows_v[3], rotary.ref,
+                 dst, ld_o, fresh)
     else:
-        _call_on(index, lib.mes_kv_append_fresh if fresh else lib.mes_kv_append, *rows, rot, n_pos, dst, ld_o)
+        _call_on(index, lib.mes_kv_append_fresh if fresh else lib.mes_kv_append, cache.ref, layer, batch.ref, src, k.data_ptr(), v.data_ptr(), T, heads, ld_q,
+                 ld_k, rows_v[3], rot, n_pos, dst, ld_o)
     return q_out if q is not None else None
 
 

@@ -53,7 +53,7 @@ constexpr int kMostTurned = 512;       // dimensions
 struct TableArgs {
   float* table;
   int64_t n_positions;
-  int dims, run;
+  int dims;
   double magnitude, frequency[kMostTurned / 2];
 };
 hipError_t launch_rotary_table(const TableArgs& a, hipStream_t s);

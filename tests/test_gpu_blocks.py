@@ -349,7 +349,8 @@ def test_extend_with_lengths_and_pages_that_do_not_fit():
 DECODES = [  # lens, heads, kvh, dim, page, (segments, prefixes)
     ([1], 4, 2, 64, 16, None), ([0], 2, 2, 128, 16, None), ([200], 32, 8, 128, 16, None), ([127, 33, 0, 400, 512], 8, 2, 128, 32, None),
     ([127, 128, 0, 1000, 1, 31, 32, 33], 4, 2, 64, 64, None), ([2100, 5, 300], 16, 1, 128, 16, None), ([8300, 17], 4, 4, 64, 128, None),
-    ([90, 300], 34, 2, 128, 16, None), ([700] * 3, 64, 1, 64, 256, None),
+    ([90, 300], 34, 2, 128, 16, None), ([700] * 3, 64, 1, 64, 256, None), ([150, 33, 400, 290], 4, 2, 64, 16, None), ([500, 129], 12, 4, 64, 32, None),
+    ([400, 200, 300, 250, 10], 40, 2, 128, 32, ([0, 5], [190])),                # own parts and the prefix in the larger body
     ([300, 170, 151, 150, 149, 3, 0], 8, 2, 128, 16, ([0, 7], [150])), ([100] * 20 + [60, 9], 8, 2, 64, 32, ([0, 20, 22], [64, 5])),
     ([350, 400, 330, 90, 80, 70, 1], 32, 8, 128, 64, ([0, 3, 3, 6, 7], [321, 9, 17, 1])), ([1300, 1290], 4, 1, 128, 16, ([0, 2], [1281])),
 ]
@@ -370,6 +371,55 @@ def test_decode(lens, heads, kvh, dim, page, shared):
     for s, m in enumerate(lens):
         want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [m - 1], dim ** -0.5)
         _check(out[s:s + 1], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+def test_a_large_batch_by_sampled_rows(kind):
+    """Lengths over two powers of ten, experts of many and few sequences, with and without prefixes, ended sequences: rows whose pieces are cut over
+    many wavefronts, that are one wavefront's, that end with their prefix."""
+    from test_gpu_attn import Paged
+    rng = random.Random(5)
+    segs, prefix = [60, 31, 9, 3, 2, 1, 0, 54], [700, 333, 512, 1600, 64, 900, 9, 0]
+    bounds, lens, share = _offsets(segs), [], {}
+    for e, n in enumerate(segs):
+        for i in range(n):
+            own = rng.choice([0, 1, 31, 32, rng.randint(1, 60), rng.randint(1, 400), rng.randint(1, 2500)])
+            lens.append(rng.choice([0, prefix[e] // 2] + [prefix[e] + own] * 8))
+        mine = [s for s in range(bounds[e], bounds[e + 1]) if lens[s] >= prefix[e]]
+        share.update({s: (mine[0], prefix[e]) for s in mine if prefix[e]})
+    heads, kvh, dim, n = 8, 2, 128, len(lens)
+    lens[130] = 9000
+    if kind == "blocks":
+        c = Random(3, lens, kvh, dim, 16, layers=1, layer=0, share=share)
+    else:
+        c = Paged(3, lens, kvh, dim, 16, kind == "e4m3", layers=1, layer=0, share=[share.get(s, (s, 0)) for s in range(n)])
+    q = _rows(torch.Generator().manual_seed(24), n, heads, dim, 2.0)
+    call = mes.AttnDecode(c.cache, heads, n)
+    call.ws.fill_(255)
+    out = call(0, c.batch(), q.to(DEV), bounds, prefix)
+    alone = call(0, c.batch(), q.to(DEV))                        # nothing shared
+    for s in sorted({0, 1, 59, 60, 75, 95, 100, 101, 103, 105, 106, 130, n - 1} | set(rng.sample(range(n), 30))):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [lens[s] - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s} of {lens[s]}")
+        _check(alone[s:s + 1], want, tol, f"sequence {s} of {lens[s]}, nothing shared")
+    assert torch.isfinite(out).all() and torch.isfinite(alone).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+def test_rows_behind_contexts_of_many_lengths_by_sampled_rows(kind):
+    """More items than compute units, the longest several times the mean: the call is cut, and its parts added up."""
+    from test_gpu_attn import Paged
+    contexts, news = [1024, 1024, 2040, 0, 1024, 77, 4096, 1024], [64, 700, 130, 333, 1, 17, 512, 250]
+    lens, off, heads, kvh, dim = [a + b for a, b in zip(contexts, news)], _offsets(news), 16, 4, 64
+    c = Random(4, lens, kvh, dim, 16) if kind == "blocks" else Paged(4, lens, kvh, dim, 16, kind == "e4m3")
+    q = _rows(torch.Generator().manual_seed(2), off[-1], heads, dim, 2.0)
+    out = mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q.to(DEV))
+    assert torch.isfinite(out).all()
+    for s, n in enumerate(news):
+        rows = sorted({0, n // 3, n // 2, n - 1})
+        pick = [off[s] + r for r in rows]
+        want, tol = O.attend(q[pick], c.k[s], c.v[s], [contexts[s] + r for r in rows], dim ** -0.5)
+        _check(out[pick], want, tol, f"sequence {s}")
 
 
 def test_decode_with_pages_that_are_not_there():
