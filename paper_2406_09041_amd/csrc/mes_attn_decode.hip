@@ -25,10 +25,11 @@
 // with weights in fp32).
 //
 // Measured (head_dim 128, 32 heads over 8 key / value heads): 256 sequences of 0 to 8192 tokens 160 us, 5.0 TB/s of the 5.96 that a
-// pass that only reads reaches; the same at e4m3 99 us, 4.0 TB/s; 64 sequences of 512 tokens 26.5 us (5.1 TB/s); 64 of 16 experts with prompts of 512 to
-// 1600 tokens 42 us, 106 MB; 96 behind 8200 shared tokens of an e4m3 cache 54 us, of which 10 us are products at the library's rate; one sequence of
-// 200 tokens 8.3 us.  Own pieces cost 4 to 5 us each beside the larger body; in a launch of their own it was worse: 43 -> 51 us for the 64
-// sequences, 59 -> 68 for the shared prefix.
+// pass that only reads reaches; the same over e4m3 codes 91 us, 4.4 TB/s (the wavefronts end within 81 us, half of them within 74, and the join
+// takes 7); 256 of 735 tokens over blocks 76 us, 5.1 TB/s; 256 of 9 experts with prompts of 64 to 4000 tokens over blocks 109 us; 64 of 16 experts with
+// prompts of 512 to 1600 tokens 33 us; 96 behind 8200 shared tokens of an e4m3 cache 49 us, of which 10 us are products at the library's
+// rate; one sequence of 200 tokens 8.3 us.  Two steps of a wavefront on their way instead of one: no faster over codes, and spilled over bf16; the heads
+// of a sequence one behind the other on the line, instead of the sequences of a head: the same.
 #include "mes_attn_tiles.h"
 
 namespace mes {
@@ -38,12 +39,15 @@ constexpr bool has_codes(int source) { return source != KV_PAGED; }
 
 constexpr int kThreads = 256, kWaves = kThreads / 64, kStep = 32, kRowsPass = 128, kFewRows = 16;
 // Costs on the line, in steps of a wavefront: of a tile of the larger body, of beginning and ending what a pass or a sequence does there, and
-// the same of a sequence's own part in the smaller one.
+// the same of a sequence's own part in the smaller one.  As measured under load over codes: a step 1.8 us, a piece 4.4 to 5.7 us more, a
+// workgroup's tile 3.2 us and a pass 5.5 to 6.5 us more, which is four wavefronts' time; steps over bf16 take about twice as long.  (Tiles at 3 steps and passes at
+// nothing: 162 us instead of 109 for the 256 sequences of 9 experts, and 300 instead of 100 for 128 sequences that share one token.)
 template <int SRC>
 struct Cost {
   static constexpr uint32_t kTile = has_codes(SRC) ? 7 : 4, kBegin = has_codes(SRC) ? 12 : 7, kOwn = has_codes(SRC) ? 3 : 2;
 };
-// Workgroups of a launch: what the chip holds.
+// Workgroups of a launch: two per compute unit, which is what the chip holds with the larger body; without it three fit, and were as fast
+// or slower (256 sequences of 735 tokens 92 us instead of 76).
 constexpr int kWorkgroups = 512;
 // Up to this many tokens a sequence is one workgroup's, where nothing is shared: no second launch to add up pieces (one
 // sequence of 200 tokens, when it was made: 9.2 us, 12.4 with it).

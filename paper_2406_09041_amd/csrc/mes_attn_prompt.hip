@@ -12,7 +12,7 @@
 //
 // Measured (head_dim 128, 32 heads over 8 key / value heads unless stated): one prompt of 77 rows 8.8 us, of which 7 is the time of a launch
 // that does next to nothing; four of 1024 rows 53 us; 1 to 6001 rows of 40 heads with keys of their own 411 us, 961 TFLOP/s; 8
-// prompts of 1 to 700 rows behind 0 to 4096 cached tokens 126 us, at e4m3 147.
+// prompts of 1 to 700 rows behind 0 to 4096 cached tokens 105 us, at e4m3 or over blocks 118 (widening the codes and writing them to LDS).
 #include "mes_attn_tiles.h"
 
 namespace mes {

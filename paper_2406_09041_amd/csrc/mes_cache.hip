@@ -141,7 +141,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
 // The same to a cache of blocks.  A block of a head's keys or values is one wavefront's work, from the largest of its values to its codes: it
 // holds all of them in registers, or, where the call has few tokens for the block, several heads of it.  One workgroup per row turns the row's queries
 // and takes its share of the heads of the block that the row is in, so that nothing has to be counted beforehand and a block's wavefronts are
-// on different compute units.
+// on different compute units.  Four prompts of about 1024 tokens (32 query, 8 key / value heads of 128): 93 MB in 21.5 us, 4.3 TB/s; 256 single tokens
+// as long as a launch.
 template <int D>
 __global__ __launch_bounds__(kAppendThreads) void k_append_blocks(AppendArgs a) {
   constexpr int kUnits = D / 16, kRowsPass = 64 / kUnits, kPasses = MES_KV_BLOCK / kRowsPass;
@@ -222,6 +223,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_blocks(AppendArgs a) 
 
 // Reading back: a thread 8 dimensions of a token, so that the stores of a wavefront are whole lines.  Workgroups take kReadRows rows; keys and
 // values of a head are read in the order of the page, kReadBatch units of a thread on their way before the first is written.
+// 64 contexts, 68 thousand tokens of 8 heads of 128: 407 MB in 91 us, 4.5 TB/s (4.88 is what a copy of 2 GiB reaches); workgroups of 16 and 32 rows, whose
+// threads do more one after the other: 93 and 106.
 constexpr int kReadThreads = 256, kReadRows = 8, kReadBatch = 8;
 
 template <int DTYPE>
