@@ -406,6 +406,45 @@ def test_a_large_batch_by_sampled_rows(kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+@pytest.mark.parametrize("heads,kvh,dim", [(4, 2, 64), (12, 3, 128), (16, 1, 64), (2, 2, 128)])
+def test_short_sequences_without_a_join(kind, heads, kvh, dim):
+    """Up to 512 tokens: one workgroup per sequence and key / value head, one to four steps of each of its wavefronts."""
+    from test_gpu_attn import Paged
+    lens = [512, 150, 33, 400, 290, 0, 1, 129, 257]
+    c = Random(6, lens, kvh, dim, 32) if kind == "blocks" else Paged(6, lens, kvh, dim, 32, kind == "e4m3")
+    q = _rows(torch.Generator().manual_seed(7), len(lens), heads, dim, 2.0)
+    out = mes.AttnDecode(c.cache, heads, len(lens))(c.layer, c.batch(), q.to(DEV))
+    for s, n in enumerate(lens):
+        want, tol = O.attend(q[s:s + 1], c.k[s], c.v[s], [n - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"{n} tokens")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "blocks"])
+def test_long_pieces_of_wavefronts(kind):
+    """So many long sequences that a wavefront takes more than the 32 steps whose pages it looks up together; exponents of blocks far apart."""
+    n, tokens, heads, kvh, dim, page = 64, 10000, 8, 4, 64, 128
+    width = -(-tokens // page)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    shape = (1, n * width, kvh, page, dim)
+    if kind == "blocks":
+        code = [(torch.randn(shape, generator=g, device=DEV) * 90).clamp(-448, 448).to(torch.float8_e4m3fn) for _ in range(2)]
+        e = [torch.randint(117, 123, (*shape[:3], page // 16), generator=g, device=DEV, dtype=torch.uint8).view(torch.float8_e8m0fnu) for _ in range(2)]
+        cache = mes.KvCache.over(*code, *e)
+    else:
+        cache = mes.KvCache.over(*[torch.randn(shape, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2)])
+    table = torch.randperm(n * width, generator=g, device=DEV).to(torch.int32).reshape(n, width)
+    kv_len = _ints([tokens - 37 * (s % 5) for s in range(n)])
+    q = _rows(torch.Generator().manual_seed(6), n, heads, dim)
+    out = mes.AttnDecode(cache, heads, n)(0, mes.SeqBatch(kv_len, table), q.to(DEV))
+    assert torch.isfinite(out).all()
+    for s in (0, 1, 17, 33, 63):
+        m = int(kv_len[s])
+        k, v = mes.mes_kv_read(cache, 0, mes.SeqBatch(kv_len[s:s + 1], table[s:s + 1], _ints([0, m])), m)
+        want, tol = O.attend(q[s:s + 1], k.cpu(), v.cpu(), [m - 1], dim ** -0.5)
+        _check(out[s:s + 1], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
 def test_rows_behind_contexts_of_many_lengths_by_sampled_rows(kind):
     """More items than compute units, the longest several times the mean: the call is cut, and its parts added up."""
     from test_gpu_attn import Paged
