@@ -9,16 +9,16 @@
 // the device (every workgroup adds them up for itself).  A piece of the line that does not cover a sequence alone leaves (bound, sum,
 // weighted values) in the workspace, and k_join adds the pieces of a row in their order.
 //
-// Up to 16 query rows (one sequence of a group of up to 16 heads, or few sequences' shared prefix): a wavefront takes 32 tokens at a
-// time.  Scores are formed transposed, S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K's operand is 16 tokens x 8 dimensions per lane
-// straight from memory, and the result holds one query row (lane & 15) and tokens 4 g + (0..3) per lane (g = lane / 16), which rounded
-// to bf16 IS the operand P^T of O^T = V^T P^T over the 32 tokens in the order (4 g + i, 16 + 4 g + i).  V is read by rows, 16 lanes a
-// row, lane r the dimensions VD r .. VD r + VD - 1 of its 8 tokens: product j of VD then yields the dimensions VD m + j, and its operand
+// A sequence's own tokens, up to 16 heads per key / value head: a wavefront takes 32 tokens at a time.  Scores are formed transposed,
+// S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K's operand is 16 tokens x 8 dimensions per lane straight from memory, and the result
+// holds one query row (lane & 15) and tokens 4 g + (0..3) per lane (g = lane / 16), which rounded to bf16 IS the operand P^T of
+// O^T = V^T P^T over the 32 tokens in the order (4 g + i, 16 + 4 g + i).  V is read by rows, 16 lanes a row, lane r the dimensions
+// VD r .. VD r + VD - 1 of its 8 tokens: product j of VD then yields the dimensions VD m + j, and its operand
 // is pairs of 16-bit halves put together, one v_perm each.  So neither keys nor values pass through LDS.  Of the 16 columns of a
 // tile 4 (n_heads / n_kv_heads) are used where nothing is shared: the matrix cores are idle most of the time anyway.
 //
-// More rows: up to 128 of them share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from about 100 rows on; also those of a
-// sequence alone where more than 16 query heads share a key / value head.
+// Prefixes, however few rows share them: up to 128 rows share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from
+// about 100 rows on; also those of a sequence alone where more than 16 query heads share a key / value head.
 //
 // Weights are rounded to bf16 for the product with V, as the matrix cores take both operands alike, and summed as rounded: they still add up
 // to 1, and a row's error grows by at most 2^-8 of its weighted values' size (measured against 64 bits: 0.0020 of the rows' norm, 0.0017
@@ -58,12 +58,7 @@ struct Shape {                       // what host and device derive alike
   int group, per_pass, n_passes;     // query heads per key / value head, sequences per pass, passes of all groups
 };
 
-// partial results: [slot][rows][D] floats, then [slot][rows] (bound, sum)
-struct Partials {
-  float* o;
-  float2* ml;
-};
-
+// Of the workspace: partial results [slot][rows][D] floats and [slot][rows] (bound, sum), of passes and of sequences' own parts.
 struct Layout {
   size_t prefix_o, prefix_ml, own_o, own_ml, meta, total;
 };
@@ -92,7 +87,7 @@ struct DecodeCall {
 };
 
 template <int D, int SRC>
-struct Raw {                                        // 32 tokens of keys and values on their way
+struct Raw {                                        // 32 tokens of keys and values on their way, as the loads bring them
   static constexpr bool FP8 = has_codes(SRC);
   static constexpr int VD = D / 16, KC = FP8 ? D / 64 : D / 32, VW = VD * (FP8 ? 1 : 2) / 4;
   typedef uint32_t Words __attribute__((ext_vector_type(VW)));
@@ -108,7 +103,7 @@ __device__ __forceinline__ int dim_of(int c, int g) {
 
 struct Segment {                                    // a piece of the line
   int kvh, seq, seq0, rows;                         // key / value head; page table; sequence of row 0; query rows
-  int from, to, t0, t1;                             // tokens of [from, to) in the units [t0, t1), t0 a multiple of 64
+  int from, to, t0, t1;                             // tokens of [from, to) in [t0, t1), t0 a multiple of a tile or a step
 };
 
 template <int D>
