@@ -444,7 +444,8 @@ mes_status mes_attn_extend(const mes_kv* kv, int layer, const mes_seqs* seqs, co
  * with o[n_experts] = n_seqs, and those sequences of expert e that have prefix_len[e] tokens or more hold the same
  * tokens in their first prefix_len[e] positions (HOST [n_experts], >= 0; for instance the expert's system prompt).  These are
  * read once for all of them, through the page table of the first such sequence; they need not be shared pages.  A
- * shorter sequence (a row that only pads the batch: kv_len 0) is read by itself.
+ * shorter sequence (a row that only pads the batch: kv_len 0) is read by itself.  MES_KV_E4M3_BLOCKS: whole blocks of the prefix are read once; the block
+ * that it ends in is every sequence's own, as the exponent there, and with it the prefix's codes, depends on the tokens that follow.
  * seg_offsets and prefix_len NULL (n_experts ignored): nothing is shared.  1 <= n_experts <= MES_MAX_EXPERTS.
  * workspace: >= mes_attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim), 16-byte aligned, contents
  * irrelevant; calls sharing a workspace must be stream-ordered.  Results do not depend on other calls, and are the same

@@ -98,6 +98,9 @@ struct DecodeArgs {
   int n_groups;                        // of sequences that share a prefix (two of them at least): rows first .. behind
   int32_t first[MES_MAX_EXPERTS], behind[MES_MAX_EXPERTS], prefix[MES_MAX_EXPERTS];
 };
+// Of the first `prefix` tokens, which an expert's sequences share, those that one sequence's pages give for all of them.  Over blocks whole blocks: the one
+// that the prefix ends in also holds tokens of the sequence's own, which have a part in its exponent and so in the prefix's codes.
+__host__ __device__ inline int shared_tokens(bool blocks, int prefix) { return blocks ? prefix & -MES_KV_BLOCK : prefix; }
 size_t attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim);
 hipError_t launch_attn_decode(const DecodeArgs& a, int source, hipStream_t s);
 

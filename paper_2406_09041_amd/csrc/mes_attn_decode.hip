@@ -452,6 +452,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
   const uint32_t tile_cost = wide ? kWaves : C::kTile, begin_cost = wide ? 2 * kWaves : C::kBegin;   // (a workgroup's border at every tile)
   auto many_cost = [&](int from, int to) { return to > from ? begin_cost + tiles_of(from, to) * tile_cost : 0u; };
   auto own_cost = [&](int from, int to) { return wide ? many_cost(from, to) : to > from ? C::kOwn + steps_of(from, to) : 0u; };
+  // the tokens that are read once, of those that an expert's sequences share
+  auto read_once = [](int prefix) { return shared_tokens(SRC == KV_PAGED_BLOCKS, prefix); };
 
   // ---- cost of every item, groups first
   for (int s = threadIdx.x; s < a.n_seqs; s += kThreads) sh.cum[n_groups + s] = own_cost(0, length(s));
@@ -467,10 +469,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     const bool active = count >= 2;
     if (active)
       for (int s = first + lane; s < behind; s += 64)
-        if (length(s) >= prefix) sh.cum[n_groups + s] = own_cost(prefix, length(s));
+        if (length(s) >= prefix) sh.cum[n_groups + s] = own_cost(read_once(prefix), length(s));
     if (lane == 0) {
       sh.group_src[g] = active ? src : -1;
-      sh.cum[g] = active ? many_cost(0, prefix) * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
+      sh.cum[g] = active ? many_cost(0, read_once(prefix)) * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
     }
   }
   __syncthreads();
@@ -481,10 +483,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     my_behind = a.behind[lane];
     my_prefix = a.prefix[lane];
   }
-  auto shared_by = [&](int s, int len) {            // the prefix that a sequence (the same in all lanes) shares with others
+  auto shared_by = [&](int s, int len) {            // the tokens of a sequence (the same in all lanes) that a pass reads for it
     if (!MANY) return 0;
     const uint64_t who = __ballot(my_first <= s && s < my_behind && len >= my_prefix);
-    return who ? __builtin_amdgcn_readlane(my_prefix, __builtin_ctzll(who)) : 0;
+    return who ? read_once(__builtin_amdgcn_readlane(my_prefix, __builtin_ctzll(who))) : 0;
   };
   // ---- exclusive sums, in place
   {
@@ -539,7 +541,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       float2* ml;
       g.kvh = h;
       if (it < n_groups) {
-        const uint32_t per_pass = many_cost(0, a.prefix[it]);
+        const uint32_t per_pass = many_cost(0, read_once(a.prefix[it]));
         const int pass = uniform((u - first) / per_pass);
         first += pass * per_pass;
         behind = first + per_pass;
@@ -547,7 +549,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
         g.seq0 = a.first[it] + pass * c.sh.per_pass;
         g.rows = uniform(min(c.sh.per_pass, a.behind[it] - g.seq0) * c.sh.group);
         g.from = 0;
-        g.to = a.prefix[it];
+        g.to = read_once(a.prefix[it]);
         const size_t slot = (size_t)blockIdx.x + h * c.sh.n_passes + c.pass_base[it] + pass;
         o = reinterpret_cast<float*>(ws + y.prefix_o) + slot * kRowsPass * D;
         ml = reinterpret_cast<float2*>(ws + y.prefix_ml) + slot * kRowsPass;
@@ -646,7 +648,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     for (int g = 0; g < n_groups; ++g) {
       if (s < a.first[g] || s >= a.behind[g]) continue;
       if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
-        const uint32_t n = many_cost(0, a.prefix[g]), pass = (s - a.first[g]) / c.sh.per_pass;
+        const uint32_t n = many_cost(0, read_once(a.prefix[g])), pass = (s - a.first[g]) / c.sh.per_pass;
         const uint32_t u0 = h * many_head + sh.cum[g] + pass * n, w0 = (u0 + begin_cost) / each, w1 = (u0 + n - tile_cost) / each;
         w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
         w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
