@@ -347,7 +347,8 @@ typedef struct {           /* HOST struct; pointers DEVICE, caller-owned */
  * (q_offsets NULL: one row per sequence, row s).  0 <= n_seqs <= MES_MAX_SEQS; calls of no
  * sequences or no rows return MES_OK without touching anything.
  * Values that the host cannot see are checked where they are used: a token past the table's room or on a page outside
- * [0, n_pages) counts as absent (never read or written), a negative kv_len as 0. */
+ * [0, n_pages) counts as absent (never read or written), a negative kv_len as 0; where the offsets reach past the call's T rows, the
+ * rows that it has are the first of their sequence's, at the positions that they would have with the others. */
 typedef struct {
   int32_t n_seqs, table_pages;
   const int32_t* q_offsets;    /* [n_seqs + 1], 0 = o[0] <= o[1] <= ...; rows behind o[n_seqs] are left as they are */

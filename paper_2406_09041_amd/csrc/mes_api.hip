@@ -390,11 +390,11 @@ static mes_status append(const char* who, bool fresh, const mes_kv* kv, int laye
   if (kv->dtype == MES_KV_E4M3) { a.k_scale = kv->k_scale; a.v_scale = kv->v_scale; }
   if (kv->dtype == MES_KV_E4M3_BLOCKS) { a.k_exponent = layer_exponents(*kv, kv->k_exponent, layer); a.v_exponent = layer_exponents(*kv, kv->v_exponent, layer); }
   a.q_offsets = seqs->q_offsets; a.kv_len = seqs->kv_len; a.page_table = seqs->page_table;
-  a.layer = layer; a.n_pages = kv->n_pages; a.page_shift = log2_of(kv->page_tokens); a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads;
+  a.T = T; a.layer = layer; a.n_pages = kv->n_pages; a.page_shift = log2_of(kv->page_tokens); a.n_heads = n_heads; a.n_kv_heads = kv->n_kv_heads;
   a.head_dim = kv->head_dim; a.n_seqs = seqs->n_seqs; a.table_pages = seqs->table_pages; a.capacity = capacity;
   a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_q_out = ld_q_out;
   a.fresh = fresh;
-  return check_hip(launch_append(a, T, kv->dtype, (hipStream_t)stream), who);
+  return check_hip(launch_append(a, kv->dtype, (hipStream_t)stream), who);
 }
 
 mes_status mes_kv_append(const mes_kv* kv, int layer, const mes_seqs* seqs, const void* q, const void* k, const void* v, int T,

@@ -29,13 +29,13 @@ struct AppendArgs {
   const float *k_scale, *v_scale;      // e4m3
   uint8_t *k_exponent, *v_exponent;    // blocks; of the layer
   const int32_t *q_offsets, *kv_len, *page_table;
-  int layer, n_pages, page_shift, n_heads, n_kv_heads, head_dim, n_seqs, table_pages, capacity;
+  int T, layer, n_pages, page_shift, n_heads, n_kv_heads, head_dim, n_seqs, table_pages, capacity;
   int ld_q, ld_k, ld_v, ld_q_out;
   int dims;                            // that are turned
   bool pairs;                          // of neighbours
   bool fresh;                          // rows of q_out that get nothing are set to 0
 };
-hipError_t launch_append(const AppendArgs& a, int T, int dtype, hipStream_t s);
+hipError_t launch_append(const AppendArgs& a, int dtype, hipStream_t s);
 struct ReadArgs {
   const void *k_cache, *v_cache;       // the cache's layer
   const float *k_scale, *v_scale;      // of the layer, e4m3

@@ -1,6 +1,7 @@
 // Writing to the paged cache (rotary embedding of new queries and keys, keys and values to their pages) and copying its
 // pages.  Both move bytes and are bound by HBM where there are many, by a launch where there are few.
 #include "mes_attn.h"
+#include "mes_place.h"
 #include "mes_rows.h"
 
 namespace mes {
@@ -52,11 +53,6 @@ __device__ inline void put8(void* base, size_t element, const float v[8], float 
 
 // Four prompts of 1024 tokens (32 query, 8 key / value heads of 128, bf16): 101 MB in 19.7 us, 5.1 TB/s; 256 single tokens 6 MB, as long as a launch.
 //
-// Which token a row of the call is.
-struct Place {
-  int seq, pos;                                            // -1: behind the last sequence; < 0 or past the capacity: none
-  int from, to;                                            // positions [from, to) of the sequence's rows
-};
 // The first s with offsets[s + 1] > t, n where there is none; t is the same in all 64 lanes.  Two dependent loads (one up to 64 sequences), where
 // a search by halves would take one for each.
 __device__ __forceinline__ int sequence_of(const int32_t* offsets, int n, int t) {
@@ -69,10 +65,8 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int n, int t)
 // s: the row's sequence, by sequence_of
 template <class A>
 __device__ __forceinline__ Place place_in(const A& a, int t, int s) {
-  if (s >= a.n_seqs) return {-1, -1, 0, 0};
-  const int begin = a.q_offsets ? a.q_offsets[s] : t, end = a.q_offsets ? a.q_offsets[s + 1] : t + 1, len = max(a.kv_len[s], 0);
-  if (begin > t) return {-1, -1, 0, 0};
-  return {s, len - (end - t), max(len - (end - begin), 0), min(len, a.capacity)};
+  if (s >= a.n_seqs) return kNoPlace;
+  return place_of_row(s, a.q_offsets ? a.q_offsets[s] : t, a.q_offsets ? a.q_offsets[s + 1] : t + 1, a.kv_len[s], a.capacity, t, a.T);
 }
 template <class A>
 __device__ __forceinline__ Place place_of(const A& a, int t) { return place_in(a, t, a.q_offsets ? sequence_of(a.q_offsets, a.n_seqs, t) : t); }
@@ -155,8 +149,8 @@ __global__ __launch_bounds__(kAppendThreads) void k_append_blocks(AppendArgs a) 
   if (!real) return;
   const int page = a.page_table[(size_t)at.seq * a.table_pages + (pos >> a.page_shift)];
   if ((unsigned)page >= (unsigned)a.n_pages) return;
-  // the block's rows in this call: positions [from, to), rows of the call from row0
-  const int begin = pos & -MES_KV_BLOCK, from = max(begin, at.from), rows = min(begin + MES_KV_BLOCK, at.to) - from, row0 = t - (pos - from);
+  const BlockRows in_call = block_rows(at, t, MES_KV_BLOCK);
+  const int begin = in_call.begin, from = in_call.from, rows = in_call.rows, row0 = in_call.row0;
   const int older = from - begin, slot = begin & ((1 << a.page_shift) - 1);
   // lanes of a (head, keys or values), and how many of these a wavefront does at a time
   int lanes = kUnits;
@@ -344,7 +338,8 @@ __global__ __launch_bounds__(kCopyThreads) void k_copy_pages(CopyArgs a) {
 
 }  // namespace
 
-hipError_t launch_append(const AppendArgs& a, int T, int dtype, hipStream_t s) {
+hipError_t launch_append(const AppendArgs& a, int dtype, hipStream_t s) {
+  const int T = a.T;
   if (dtype == MES_KV_BF16) k_append<false><<<T, kAppendThreads, 0, s>>>(a);
   else if (dtype == MES_KV_E4M3) k_append<true><<<T, kAppendThreads, 0, s>>>(a);
   else if (a.head_dim == 128) k_append_blocks<128><<<T, kAppendThreads, 0, s>>>(a);

@@ -1,4 +1,4 @@
-"""The cache in blocks where its sequences differ: prefixes that end inside a block.  References: oracle/attn_oracle.py over what
+"""The cache in blocks where its sequences differ, calls with fewer rows than their offsets name.  References: oracle/attn_oracle.py over what
 mes_kv_read gives of a sequence's own pages."""
 import pytest
 import torch
@@ -51,3 +51,61 @@ def test_a_shared_prefix_is_what_every_sequence_holds(heads, kvh, dim, page, pre
         want, tol = O.attend(q[s:s + 1], *held[s], [kv_len[s] - 1], dim ** -0.5)
         _check(alone[s:s + 1], want, tol, f"sequence {s}, nothing shared")
         _check(shared[s:s + 1], want, tol, f"sequence {s}")
+
+
+CUT = [  # rows, offsets, lengths: the offsets reach past the call's rows
+    (5, [0, 20], [20]), (5, [0, 20], [33]), (1, [0, 16], [40]), (10, [0, 3, 40], [19, 45]), (33, [0, 0, 30, 49], [4, 35, 19]), (7, [0, 9, 12], [9, 90]), (12, [0, 30], [9]),
+]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+@pytest.mark.parametrize("kvh,dim", [(8, 128), (2, 64)])
+@pytest.mark.parametrize("T,offsets,kv_len", CUT)
+def test_append_of_fewer_rows_than_the_offsets_name(T, offsets, kv_len, kvh, dim, kind):
+    """The rows that are there get their places, all heads of them; what lies behind them in memory goes nowhere."""
+    page, heads, n = 32, 2 * kvh, len(kv_len)
+    g = torch.Generator().manual_seed(T + kvh)
+    scale = [torch.full((1, kvh), x, device=DEV) for x in (0.25, 0.0625)]
+    kinds = {"bf16": mes.KV_BF16, "e4m3": mes.KV_E4M3, "blocks": mes.KV_E4M3_BLOCKS}
+    make = lambda: mes.KvCache(1, 4 * n, page, kvh, dim, kinds[kind], *(scale if kind == "e4m3" else (None, None)))  # noqa: E731
+    table = torch.randperm(4 * n, generator=g).reshape(n, 4)
+    angles = mes.Angles(mes.mes_rotary_table(4 * page, dim))
+    wide = [torch.cat([_rows(g, T, h, dim), 1e4 * _rows(g, 40, h, dim)]).to(DEV) for h in (heads, kvh, kvh)]
+    q, k, v = (x[:T] for x in wide)
+    got, want = make(), make()
+    for c in (got, want):                                        # older tokens, in the blocks that follow too
+        old = [_rows(g, 4 * page, kvh, dim) for _ in range(2)] if c is got else old
+        for s in range(n):
+            mes.mes_kv_append(c, 0, mes.SeqBatch(_ints([4 * page]), _ints(table[s:s + 1].tolist()), _ints([0, 4 * page])), None, *(x.to(DEV) for x in old))
+    out = mes.mes_kv_append(got, 0, mes.SeqBatch(_ints(kv_len), _ints(table.tolist()), _ints(offsets)), q, k, v, angles)
+    # one call for each sequence, of the rows that are there
+    turned = torch.zeros_like(out)
+    for s in range(n):
+        a, b = offsets[s], min(offsets[s + 1], T)
+        if b > a:
+            batch = mes.SeqBatch(_ints([kv_len[s] - (offsets[s + 1] - b)]), _ints(table[s:s + 1].tolist()), _ints([0, b - a]))
+            turned[a:b] = mes.mes_kv_append(want, 0, batch, q[a:b], k[a:b], v[a:b], angles)
+    assert torch.equal(out, turned)
+    parts = ["k", "v"] + ["k_scale", "v_scale"] * (kind == "blocks")
+    for x in parts:
+        a, b = (getattr(c, x).view(torch.uint8) for c in (got, want))
+        assert torch.equal(a, b), x
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "blocks"])
+@pytest.mark.parametrize("offsets", [[0, 8, 3, 12], [0, 20, -5, 12], [4, 2, 1, 0], [0, -1, 40, 5]])
+def test_append_with_offsets_out_of_order(offsets, kind):
+    """Which row is whose is anyone's guess: the call ends, and pages that are none of the sequences' are left as they are."""
+    page, kvh, dim, T = 16, 2, 64, 12
+    g = torch.Generator().manual_seed(3)
+    scale = [torch.ones(1, kvh, device=DEV) for _ in range(2)] if kind == "e4m3" else [None, None]
+    cache = mes.KvCache(1, 20, page, kvh, dim, {"bf16": mes.KV_BF16, "e4m3": mes.KV_E4M3, "blocks": mes.KV_E4M3_BLOCKS}[kind], *scale)
+    table = [[1, 3], [5, 7], [9, 11]]
+    q, k, v = (_rows(g, T, h, dim).to(DEV) for h in (4, kvh, kvh))
+    batch = mes.SeqBatch(_ints([30, 17, 12]), _ints(table), _ints(offsets))
+    out = mes.mes_kv_append(cache, 0, batch, q, k, v, mes.Angles(mes.mes_rotary_table(2 * page, dim)))
+    assert torch.isfinite(out).all()
+    rest = torch.tensor([p for p in range(20) if p not in sum(table, [])], device=DEV)
+    assert not cache.k.view(torch.uint8)[0, rest].any() and not cache.v.view(torch.uint8)[0, rest].any()
+    for x in mes.mes_kv_read(cache, 0, batch, T):
+        assert torch.isfinite(x).all()
