@@ -52,6 +52,12 @@ constexpr int kWorkgroups = 512;
 // Up to this many tokens a sequence is one workgroup's, where nothing is shared: no second launch to add up pieces (one
 // sequence of 200 tokens, when it was made: 9.2 us, 12.4 with it).
 constexpr int kWholeTokens = 512;
+// Few sequences and heads are not put on the line: with up to a wavefront's work each, a row's pieces are so many that adding them up takes longer than
+// they do (one sequence of 60000 tokens, 8 heads over one key / value head: 52 us, 20 as in few_items; of 8000, 32 over 8: 18.0 and 12.4; 32
+// of 700, 28 over 4: 19.4 and 15.5).  From about 200 items on the line is as fast or faster, and where a part would be longer than
+// kMostUnits, as parts of one length leave compute units idle (one of 60000, 40 heads of their own: 219 us and 256).
+constexpr int kFewItems = 192, kFewSeqs = 256, kMostUnits = 8;
+static_assert(kFewItems <= kWorkgroups && kFewSeqs >= kFewItems && kFewSeqs % 64 == 0, "an item has a workgroup, a lane as many sequences as another");
 static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
 
 struct Shape {                       // what host and device derive alike
@@ -112,9 +118,10 @@ struct Merge {                                      // a workgroup's four wavefr
   float2 ml[4][kFewRows];
 };
 struct Nothing {};
-template <int D, bool MANY>
+template <int D, bool MANY, bool FEW>
 struct Shared {
   [[no_unique_address]] std::conditional_t<MANY, TileLds<D>, Nothing> tiles;
+  [[no_unique_address]] std::conditional_t<FEW, Merge<D>, Nothing> merge;
   uint32_t cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
   int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: fewer than two are
   uint32_t part[4];
@@ -363,6 +370,12 @@ struct Few {
   for (int w = 0; w < 4; ++w) lr += sh->ml[w][row].y * exp2_fast(sh->ml[w][row].x - (mr == -INFINITY ? 0.0f : mr));
 #pragma unroll
   for (int j = 0; j < VD; ++j) x[j] = sh->o[0][row][d0 + j] + sh->o[1][row][d0 + j] + sh->o[2][row][d0 + j] + sh->o[3][row][d0 + j];
+  if (!direct) {
+#pragma unroll
+    for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(o + (size_t)row * D + d0 + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+    if (d0 == 0) ml_out[row] = make_float2(mr, lr);
+    return;
+  }
   const float inv = lr == 0.0f ? 0.0f : (SCALED ? a.v_scale[g.kvh] : 1.0f) / lr;
   uint16_t* dst = a.out + (size_t)(g.seq0 + row / group) * a.ld_out + (size_t)(g.kvh * group + row % group) * D + d0;
 #pragma unroll
@@ -437,11 +450,81 @@ __global__ __launch_bounds__(kThreads, 3) void k_attn_decode_whole(DecodeCall c)
   few.run(g, true, false, g, &sh, true, nullptr, nullptr);
 }
 
-// MANY: prefixes are shared, or more than 16 query heads a key / value head.
-template <int D, int SRC, bool MANY>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
-  __shared__ __align__(16) Shared<D, MANY> sh;
+// Few items (sequence, key / value head): each in parts of up to kMostUnits units of 128 tokens, the shortest that there are workgroups for.  A part is a
+// workgroup's, whose wavefronts take every fourth step and add up in LDS: a quarter of the pieces for the join, and none that ends one sequence and
+// begins another.  Lane i of a wavefront looks after sequences kEach i .. kEach i + kEach - 1.  False: parts would be longer, and nothing has been done.
+template <int D, int SRC>
+__device__ __forceinline__ bool few_items(const DecodeCall& c, Merge<D>& sh) {
   const DecodeArgs& a = c.a;
+  constexpr int kUnit = kWaves * kStep, kEach = kFewSeqs / 64;
+  const int lane = threadIdx.x & 63;
+  int len[kEach], units[kEach], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int s = kEach * lane + i;
+    len[i] = s < a.n_seqs ? min(max(a.kv_len[s], 0), a.capacity) : 0;
+    sum += units[i] = (len[i] + kUnit - 1) / kUnit;
+  }
+  // units of a part; a call's units are below 2^29
+  int share = max((wave_sum(sum) * a.n_kv_heads + kWorkgroups - 1) / kWorkgroups, 1), upto = 0;
+  for (;; ++share) {
+    if (share > kMostUnits) return false;
+    sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += (units[i] + share - 1) / share;
+    upto = wave_scan(sum);
+    if (__builtin_amdgcn_readlane(upto, 63) * a.n_kv_heads <= kWorkgroups) break;
+  }
+  const int all = __builtin_amdgcn_readlane(upto, 63);      // parts of a head
+  int first[kEach], parts[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    parts[i] = (units[i] + share - 1) / share;
+    first[i] = i ? first[i ? i - 1 : 0] + parts[i ? i - 1 : 0] : upto - sum;
+  }
+  const Layout y = layout(a.n_seqs, a.n_kv_heads, c.sh.group, c.sh.n_passes, D);
+  char* ws = static_cast<char*>(a.ws);
+  // where the join finds every row's pieces
+  if (threadIdx.x < 64)
+    for (int h = blockIdx.x; h < a.n_kv_heads; h += gridDim.x)
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (kEach * lane + i < a.n_seqs)
+          reinterpret_cast<Meta*>(ws + y.meta)[h * a.n_seqs + kEach * lane + i] = make_int4(h * all + first[i], parts[i] == 1 ? -1 : parts[i], 0, 0);
+  for (int number = blockIdx.x; number < all * a.n_kv_heads; number += gridDim.x) {
+    const int h = number / all, at = number % all;
+    int seq = 0, part = 0, n = 0, tokens = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (first[i] <= at && at < first[i] + parts[i]) {
+        seq = kEach * lane + i;
+        part = at - first[i];
+        n = parts[i];
+        tokens = len[i];
+      }
+    const int who = __builtin_ctzll(__ballot(n > 0));
+    seq = __builtin_amdgcn_readlane(seq, who);
+    part = __builtin_amdgcn_readlane(part, who);
+    n = __builtin_amdgcn_readlane(n, who);
+    tokens = __builtin_amdgcn_readlane(tokens, who);
+    const Segment g = {h, seq, seq, c.sh.group, 0, tokens, part * share * kUnit, min((part + 1) * share * kUnit, tokens)};
+    if (number >= (int)gridDim.x) __syncthreads();           // the last part's sums have been read
+    Few<D, SRC, true> few(a, c.sh.group);
+    few.start(g);
+    few.run(g, true, false, g, &sh, n == 1, reinterpret_cast<float*>(ws + y.own_o) + (size_t)number * c.sh.group * D,
+            reinterpret_cast<float2*>(ws + y.own_ml) + (size_t)number * c.sh.group);
+  }
+  return true;
+}
+
+// MANY: prefixes are shared, or more than 16 query heads a key / value head.
+// FEW: few items, see few_items (a kernel of its own: with that code beside it the line's ran up to 3% slower).
+template <int D, int SRC, bool MANY, bool FEW>
+__global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
+  __shared__ __align__(16) Shared<D, MANY, FEW> sh;
+  const DecodeArgs& a = c.a;
+  if constexpr (FEW)
+    if (few_items<D, SRC>(c, sh.merge)) return;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const bool wide = MANY && c.sh.group > kFewRows;  // sequences' own parts have too many rows for the small body, too
   const int n_groups = MANY ? a.n_groups : 0, n_items = n_groups + a.n_seqs, n_many = wide ? n_items : n_groups;
@@ -748,8 +831,10 @@ hipError_t launch(const DecodeCall& c, hipStream_t s) {
   // never more workgroups than steps there can be
   const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kStep - 1) / kStep + 1);
   const unsigned grid = (unsigned)std::min<int64_t>(kWorkgroups, most);
-  if (many) k_attn_decode<D, SRC, true><<<grid, kThreads, 0, s>>>(c);
-  else k_attn_decode<D, SRC, false><<<grid, kThreads, 0, s>>>(c);
+  const bool few = c.a.n_seqs * c.a.n_kv_heads <= kFewItems;
+  if (many) k_attn_decode<D, SRC, true, false><<<grid, kThreads, 0, s>>>(c);
+  else if (few) k_attn_decode<D, SRC, false, true><<<grid, kThreads, 0, s>>>(c);
+  else k_attn_decode<D, SRC, false, false><<<grid, kThreads, 0, s>>>(c);
   if (hipError_t e = hipGetLastError()) return e;
   const int rows = c.a.n_seqs * c.a.n_heads;
   if (rows <= 64) k_join<D, 16><<<rows, 1024, 0, s>>>(c, SRC == KV_PAGED_E4M3);
