@@ -447,7 +447,15 @@ __global__ __launch_bounds__(kThreads, 3) void k_attn_decode_whole(DecodeCall c)
   const Segment g = {(int)blockIdx.x / a.n_seqs, s, s, c.sh.group, 0, len, 0, len};
   Few<D, SRC, true> few(a, c.sh.group);
   few.start(g);
-  few.run(g, true, false, g, &sh, true, nullptr, nullptr);
+  // (so short a piece does not wait for a step of nothing: over codes 0.4 to 1 us of 7 to 20)
+  if (few.steps(g) > 0) {
+    int next[2];
+    few.request_k(g, 0, few.pages, next);
+    few.request_v(g, 0, next);
+    few.there[0] = next[0];
+    few.there[1] = next[1];
+  }
+  few.run(g, false, false, g, &sh, true, nullptr, nullptr);
 }
 
 // Few items (sequence, key / value head): each in parts of up to kMostUnits units of 128 tokens, the shortest that there are workgroups for.  A part is a
