@@ -100,7 +100,11 @@ struct DecodeArgs {
 };
 // Of the first `prefix` tokens, which an expert's sequences share, those that one sequence's pages give for all of them.  Over blocks whole blocks: the one
 // that the prefix ends in also holds tokens of the sequence's own, which have a part in its exponent and so in the prefix's codes.
-__host__ __device__ inline int shared_tokens(bool blocks, int prefix) { return blocks ? prefix & -MES_KV_BLOCK : prefix; }
+__host__ __device__ constexpr int shared_tokens(bool blocks, int prefix) { return blocks ? prefix & -MES_KV_BLOCK : prefix; }
+// The fewest sequences whose common tokens are read once.  Over codes a pass takes longer than two wavefronts that read the tokens for a sequence each, as half of
+// the bytes are not what it waits for (prefixes of 500 to 4000 tokens, 64 experts of two sequences: 121 us shared, 96 apart; 16 of
+// three 38 and 43).  Over bf16 it does not (64 of two: 156 and 184).
+__host__ __device__ constexpr int least_sharing(bool codes) { return codes ? 3 : 2; }
 size_t attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim);
 hipError_t launch_attn_decode(const DecodeArgs& a, int source, hipStream_t s);
 
