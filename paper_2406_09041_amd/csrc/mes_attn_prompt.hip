@@ -68,9 +68,12 @@ __device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
   // A tile of keys takes a workgroup 1.1 us alone on its compute unit and 2.3 us beside another; writing and adding up parts about as long
   // as 11 tiles (measured: 512 rows behind 4096 tokens 70 us cut and 87 whole; a prompt of 1024 tokens 38 us cut and 24 whole).  The longest item
   // either has its compute unit to itself, or, where there are more items than compute units, it has company until the others' share of the work
-  // is done (8 prompts behind 0 to 4096 tokens, 528 items, longest 72 tiles: 142 us whole, 124 cut).
+  // is done (8 prompts behind 0 to 4096 tokens of an e4m3 cache, 528 items, longest 72 tiles: 148 us whole, 118 cut).  Packed prompts alone have
+  // items of every length up to the longest, so that it is alone sooner: there it has to be longer by a quarter (16 heads over 2, one prompt of
+  // 4000 rows 90 us whole, 101 cut; 8 over 1, of 5800 112 and 102, of 8500 180 and 180, of 10000 228 and 239).
   const bool beside = y.all_items * columns > kHeld / 2;
-  if (y.longest <= 21 * share / 8 + 11 * kTile / R && !(beside && y.longest > 21 * share / 16 + 18 * kTile / R)) return y;
+  constexpr int kShares = SRC == KV_PACKED ? 27 : 21, kTiles = SRC == KV_PACKED ? 24 : 18;
+  if (y.longest <= 21 * share / 8 + 11 * kTile / R && !(beside && y.longest > kShares * share / 16 + kTiles * kTile / R)) return y;
   // parts longer than a share: the workspace has room for no more, and they fit the chip at once; whole tiles (R is 32, 64 or 128)
   int block = max(share + share / 8 + 1, kLeastPart / R);
   block += R < kTile ? block & 1 : 0;
@@ -422,7 +425,7 @@ bool packed_may_cut(int T, int n_seqs, int R, int columns) {
   for (double l = rows / n_seqs; l < 1.2 * rows; l *= 1.1) {
     const double longest = std::min(l + 1, rows + 1), rest = std::max(rows - longest, 0.0);
     const double work = 0.5 * (longest * longest + (n_seqs > 1 ? rest * rest / (n_seqs - 1) : 0.0));
-    if (longest > 2.5 * work * columns / kHeld + 11 * kTile / R || longest > 1.25 * work * columns / kHeld + 18 * kTile / R) return true;
+    if (longest > 2.5 * work * columns / kHeld + 11 * kTile / R || longest > 1.6 * work * columns / kHeld + 24 * kTile / R) return true;
   }
   return false;
 }
