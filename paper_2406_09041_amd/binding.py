@@ -707,12 +707,35 @@ class Angles:
         self.ref = ctypes.byref(self.desc)
 
 
+class _Turned(torch.autograd.Function):
+    """mes_rotary with a graph behind it: the gradients of the rows are those of the turned rows, turned back."""
+
+    @staticmethod
+    def forward(ctx, angles, positions, transpose, *rows):
+        ctx.angles, ctx.transpose = angles, transpose
+        ctx.save_for_backward(positions, angles.table)       # neither may be written to until the gradients are there
+        ctx.set_materialize_grads(False)
+        return mes_rotary(angles, positions, *rows, transpose=transpose)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        positions, _ = ctx.saved_tensors
+        there = [g.contiguous() for g in grads if g is not None]
+        back = mes_rotary(ctx.angles, positions, *there, transpose=not ctx.transpose) if there else ()
+        back = iter(back if len(there) == 2 else (back,))
+        return (None, None, None, *(None if g is None else next(back) for g in grads))
+
+
 def mes_rotary(angles: Angles, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                k_out: Optional[torch.Tensor] = None, transpose: bool = False):
     """Turns rows q [T, heads, d] and k [T, kv heads, d], bf16 or fp32, by the angles of positions int32 [T]; returns (q_out, k_out), or q_out
     where there is no k (q_out may be q, k_out k).  transpose: turns back, which takes gradients of turned rows to those of the rows.
-    Rows whose position is outside the table (-1) are left as they are in outputs that are given, and 0 where these are allocated."""
+    Rows whose position is outside the table (-1) are left as they are in outputs that are given, and 0 where these are allocated.
+    Rows that require gradients: outputs that are allocated are part of the graph, and none can be given."""
     index, kind = q.get_device(), q.dtype
+    if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
+        assert q_out is None and k_out is None, "q_out, k_out: rows that require gradients are turned into outputs that are allocated"
+        return _Turned.apply(angles, positions, transpose, *((q,) if k is None else (q, k)))
     assert kind in (_BF16, torch.float32) and q.is_cuda and angles.index == index, "rows are bf16 or fp32, on the angles' device"
     T, heads, dim, ld_q = _rows("q", q, index, kind)
     _int32_on("positions", positions, index)
