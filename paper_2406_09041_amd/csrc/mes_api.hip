@@ -620,8 +620,7 @@ mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, co
   }
   if ((int64_t)seqs->n_seqs * n_heads > kMaxRows)
     return fail(MES_ERR_SHAPE, "%s: %d sequences of %d heads are more than one call takes", who, seqs->n_seqs, n_heads);
-  // units of work are numbered in 32 bits (an expert's shared prefix has at most two passes per sequence)
-  if ((int64_t)3 * seqs->n_seqs * kv->n_kv_heads * (seqs->table_pages * kv->page_tokens / 128 + 2) > 0x40000000)
+  if (!decode_fits(seqs->n_seqs, kv->n_kv_heads, seqs->table_pages * kv->page_tokens))
     return fail(MES_ERR_SHAPE, "%s: %d page tables of %d pages are more than one call takes", who, seqs->n_seqs, seqs->table_pages);
   const size_t need = attn_decode_workspace_bytes(seqs->n_seqs, n_heads, kv->n_kv_heads, kv->head_dim);
   if (!workspace || workspace_bytes < need) return fail(MES_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, need);

@@ -101,6 +101,10 @@ struct DecodeArgs {
 // Of the first `prefix` tokens, which an expert's sequences share, those that one sequence's pages give for all of them.  Over blocks whole blocks: the one
 // that the prefix ends in also holds tokens of the sequence's own, which have a part in its exponent and so in the prefix's codes.
 __host__ __device__ constexpr int shared_tokens(bool blocks, int prefix) { return blocks ? prefix & -MES_KV_BLOCK : prefix; }
+// Work of a decode call is numbered in 32 bits, in costs: of a sequence and key / value head there are at most kMostCosts (u + 2), u = page table's tokens / 128
+// (mes_attn_decode.hip has the proof), and calls that could have 2^32 are refused.
+constexpr int64_t kMostCosts = 12;
+inline bool decode_fits(int n_seqs, int n_kv_heads, int capacity) { return kMostCosts * n_seqs * n_kv_heads * (capacity / 128 + 2) <= (int64_t)1 << 32; }
 // The fewest sequences whose common tokens are read once.  Over codes a pass takes longer than two wavefronts that read the tokens for a sequence each, as half of
 // the bytes are not what it waits for (prefixes of 500 to 4000 tokens, 64 experts of two sequences: 121 us shared, 96 apart; 16 of
 // three 38 and 43).  Over bf16 it does not (64 of two: 156 and 184).

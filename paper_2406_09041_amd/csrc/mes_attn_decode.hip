@@ -46,6 +46,17 @@ template <int SRC>
 struct Cost {
   static constexpr uint32_t kTile = has_codes(SRC) ? 7 : 4, kBegin = has_codes(SRC) ? 12 : 7, kOwn = has_codes(SRC) ? 3 : 2;
 };
+// Costs of a sequence and head never pass kMostCosts (u + 2), u = capacity / 128 (4 u + 4 steps, 2 u + 2 tiles at most), so that those of a call, and what they
+// are rounded up by, fit 32 bits (see decode_fits).  Sequences that share pay for the tokens behind the prefix, those shorter than it for their own alone, and there are
+// passes for half as many as both at most, but for groups of an odd number in passes of two, one more, of which the two that share pay for.
+// Narrow: the own part and half a pass; wide: the same, from tiles.  What is rounded up: a 512th, which narrow groups have room for; wide ones are not.
+template <int SRC>
+constexpr bool costs_fit() {
+  typedef Cost<SRC> C;
+  return 4 + C::kTile < kMostCosts && C::kOwn + 5 + (C::kBegin + 2 * C::kTile + 1) / 2 < 2 * kMostCosts &&   // 4 u + 5 steps, 2 u + 2 tiles
+         3 * kWaves <= kMostCosts && 6 * kWaves <= 2 * kMostCosts;                                            // (2 u + 2 tiles and a beginning) 3 / 2
+}
+static_assert(costs_fit<KV_PAGED>() && costs_fit<KV_PAGED_E4M3>() && costs_fit<KV_PAGED_BLOCKS>(), "work numbers of 32 bits");
 // Workgroups of a launch: two per compute unit, which is what the chip holds with the larger body; without it three fit, and were as fast
 // or slower (256 sequences of 735 tokens 92 us instead of 76).
 constexpr int kWorkgroups = 512;
@@ -540,7 +551,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
   auto tiles_of = [](int from, int to) { return to > from ? (to - (from & -kTile) + kTile - 1) / kTile : 0; };
   auto steps_of = [](int from, int to) { return to > from ? (to - (from & -kStep) + kStep - 1) / kStep : 0; };
   typedef Cost<SRC> C;
-  const uint32_t tile_cost = wide ? kWaves : C::kTile, begin_cost = wide ? 2 * kWaves : C::kBegin;   // (a workgroup's border at every tile)
+  const uint32_t tile_cost = wide ? kWaves : C::kTile, begin_cost = wide ? 2 * kWaves : C::kBegin;   // (a workgroup's border at every tile); see costs_fit
   auto many_cost = [&](int from, int to) { return to > from ? begin_cost + tiles_of(from, to) * tile_cost : 0u; };
   auto own_cost = [&](int from, int to) { return wide ? many_cost(from, to) : to > from ? C::kOwn + steps_of(from, to) : 0u; };
   // the tokens that are read once, of those that an expert's sequences share
