@@ -13,14 +13,13 @@
 // Measured (head_dim 128, 32 heads over 8 key / value heads unless stated): one prompt of 77 rows 8.8 us, of which 7 is the time of a launch
 // that does next to nothing; four of 1024 rows 53 us; 1 to 6001 rows of 40 heads with keys of their own 411 us, 961 TFLOP/s; 8
 // prompts of 1 to 700 rows behind 0 to 4096 cached tokens 105 us, at e4m3 or over blocks 118 (widening the codes and writing them to LDS).
+#include "mes_attn_cut.h"
 #include "mes_attn_tiles.h"
 
 namespace mes {
 namespace {
 
-constexpr int kHeld = 512;             // workgroups that the chip holds, two per compute unit
-constexpr int kMostCut = 1024;         // items of a call that is cut: with more, no compute unit is without work for long
-constexpr int kLeastPart = 256;        // keys of a block
+static_assert(kTile == kCutTile, "tiles of keys");
 
 // The part of the call a workgroup works on
 struct Item {
@@ -43,15 +42,9 @@ struct Lanes {
   int block, parts, ahead, all_parts;  // units of a block (0: the call is not cut); parts of the sequence, and before it
 };
 
-// Parts of the blocks below block b of a sequence: block i is seen by the items whose keys reach past its beginning.
-__device__ __forceinline__ int parts_below(int b, int block, int base, int tiles) {
-  const int full = min(b, base / block + 1);             // blocks that begin at or before base: all items
-  return full * tiles + (b - full) * (tiles + base) - block * ((b - full) * (full + b - 1) / 2);
-}
-__device__ __forceinline__ int first_item(int b, int block, int base) { return max(b * block - base, 0); }
-
+// cut_slots: what the workspace has room for, 0: the call is not cut
 template <int SRC>
-__device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
+__device__ Lanes look(const PromptArgs& a, int R, int columns, int cut_slots) {
   const int lane = threadIdx.x & 63;
   Lanes y = {};
   if (lane < a.n_seqs) {
@@ -62,22 +55,9 @@ __device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
   y.base = (max(y.before, 0) + R - 1) / R;
   y.all_items = wave_sum(y.tiles);
   y.longest = wave_max(y.tiles ? y.base + y.tiles : 0);
-  if (!may_cut || y.all_items * columns > kMostCut) return y;
-  const int units = wave_sum(y.tiles * y.base + y.tiles * (y.tiles + 1) / 2);
-  const int share = units / max(kHeld / columns, 1) + 1;  // of a workgroup, if all had the same
-  // A tile of keys takes a workgroup 1.1 us alone on its compute unit and 2.3 us beside another; writing and adding up parts about as long
-  // as 11 tiles (measured: 512 rows behind 4096 tokens 70 us cut and 87 whole; a prompt of 1024 tokens 38 us cut and 24 whole).  The longest item
-  // either has its compute unit to itself, or, where there are more items than compute units, it has company until the others' share of the work
-  // is done (8 prompts behind 0 to 4096 tokens of an e4m3 cache, 528 items, longest 72 tiles: 148 us whole, 118 cut).  Packed prompts alone have
-  // items of every length up to the longest, so that it is alone sooner: there it has to be longer by a quarter (16 heads over 2, one prompt of
-  // 4000 rows 90 us whole, 101 cut; 8 over 1, of 5800 112 and 102, of 8500 180 and 180, of 10000 228 and 239).
-  const bool beside = y.all_items * columns > kHeld / 2;
-  constexpr int kShares = SRC == KV_PACKED ? 27 : 21, kTiles = SRC == KV_PACKED ? 24 : 18;
-  if (y.longest <= 21 * share / 8 + 11 * kTile / R && !(beside && y.longest > kShares * share / 16 + kTiles * kTile / R)) return y;
-  // parts longer than a share: the workspace has room for no more, and they fit the chip at once; whole tiles (R is 32, 64 or 128)
-  int block = max(share + share / 8 + 1, kLeastPart / R);
-  block += R < kTile ? block & 1 : 0;
-  y.block = block;
+  if (cut_slots == 0 || y.all_items * columns > kMostCut) return y;
+  const int block = cut_block(SRC == KV_PACKED, R, columns, y.all_items, y.longest, wave_sum(y.tiles * y.base + y.tiles * (y.tiles + 1) / 2));
+  if (!block) return y;
   y.parts = y.tiles ? parts_below((y.base + y.tiles + block - 1) / block, block, y.base, y.tiles) : 0;
   // sequences in order of their longest rows
   for (int k = 0; k < a.n_seqs; ++k) {
@@ -85,6 +65,7 @@ __device__ Lanes look(const PromptArgs& a, int R, int columns, bool may_cut) {
     if (reach > y.base + y.tiles || (reach == y.base + y.tiles && k < lane)) y.ahead += count;
     y.all_parts += count;
   }
+  y.block = y.all_parts * columns <= cut_slots ? block : 0;   // (offsets out of order can name more rows than the call has)
   return y;
 }
 
@@ -239,7 +220,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_attn_prompt(PromptArgs a, i
   bool found;
   {
     Lanes y = {};
-    if (a.n_seqs <= 64) y = look<SRC>(a, R, columns, cut_slots > 0);
+    if (a.n_seqs <= 64) y = look<SRC>(a, R, columns, cut_slots);
     if (uniform(y.block)) {
       found = part_number(y, blockIdx.x / columns, it, block);
       block = uniform(block);
@@ -356,7 +337,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_prompt(PromptArgs a, int 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int R = kTileWaves * kWaveRows / heads, columns = a.n_heads / heads, hx = blockIdx.x % columns, kvh = hx % a.n_kv_heads;
   const int item = blockIdx.x / columns;
-  const Lanes y = look<SRC>(a, R, columns, true);
+  const Lanes y = look<SRC>(a, R, columns, cut_slots);
   const int block = uniform(y.block);
   if (!block || item >= y.all_items) return;
   const int upto = wave_scan(y.tiles);                               // items up to and with the lane's
@@ -415,9 +396,6 @@ __global__ __launch_bounds__(kJoinThreads) void k_join_prompt(PromptArgs a, int 
 inline int heads_of(int group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
 // enough items for every way T rows can be shared out over the sequences
 inline int64_t slots_of(int T, int n_seqs, int heads) { return (int64_t)T / (kTileWaves * kWaveRows / heads) + n_seqs; }
-// parts of a call: one per item, and one per block, which is longer than a share
-inline int cut_slots_of(int64_t workgroups) { return (int)std::min<int64_t>(workgroups, kMostCut) + kHeld; }
-
 // Whether look() could cut a call of packed prompts whose sequences take up all T rows: for some length of the longest, the others
 // sharing the rest evenly, which is the least work there can be beside it.
 bool packed_may_cut(int T, int n_seqs, int R, int columns) {
