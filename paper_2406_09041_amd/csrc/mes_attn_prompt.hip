@@ -397,15 +397,16 @@ inline int heads_of(int group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 
 // enough items for every way T rows can be shared out over the sequences
 inline int64_t slots_of(int T, int n_seqs, int heads) { return (int64_t)T / (kTileWaves * kWaveRows / heads) + n_seqs; }
 // Whether look() could cut a call of packed prompts whose sequences take up all T rows: for some length of the longest, the others
-// sharing the rest evenly, which is the least work there can be beside it.
+// sharing the rest evenly, which is the least work there can be beside it.  (Where it could not, there is no launch that finds nothing to join.)
 bool packed_may_cut(int T, int n_seqs, int R, int columns) {
-  const double rows = (double)T / R;
-  for (double l = rows / n_seqs; l < 1.2 * rows; l *= 1.1) {
-    const double longest = std::min(l + 1, rows + 1), rest = std::max(rows - longest, 0.0);
-    const double work = 0.5 * (longest * longest + (n_seqs > 1 ? rest * rest / (n_seqs - 1) : 0.0));
-    if (longest > 2.5 * work * columns / kHeld + 11 * kTile / R || longest > 1.6 * work * columns / kHeld + 24 * kTile / R) return true;
+  const int rows = (T + R - 1) / R;
+  for (int longest = (rows + n_seqs - 1) / n_seqs;; longest += longest / 10 + 1) {
+    longest = std::min(longest, rows);
+    const int others = n_seqs - 1, rest = rows - longest, each = others ? (rest + others - 1) / others : 0;
+    const int64_t units = ((int64_t)longest * (longest + 1) + (others ? (int64_t)rest * rest / others + rest : 0)) / 2;
+    if (cut_block(true, R, columns, std::max(longest, rows), std::max(longest, each), (int)std::min<int64_t>(units, 1 << 28))) return true;
+    if (longest == rows) return false;
   }
-  return false;
 }
 
 template <int D>
