@@ -610,9 +610,9 @@ mes_status mes_attn_decode(const mes_kv* kv, int layer, const mes_seqs* seqs, co
     }
     if (seg_offsets[n_experts] != seqs->n_seqs)
       return fail(MES_ERR_SEGMENTS, "%s: seg_offsets[%d] = %d, expected n_seqs = %d", who, n_experts, seg_offsets[n_experts], seqs->n_seqs);
-    // an expert with too few sequences or without tokens that are read once shares nothing: only the others are handed on
+    // an expert with one sequence or without tokens that are read once shares nothing: only the others are handed on
     for (int e = 0; e < n_experts; ++e) {
-      if (seg_offsets[e + 1] - seg_offsets[e] < least_sharing(kv->dtype != MES_KV_BF16) || shared_tokens(kv->dtype == MES_KV_E4M3_BLOCKS, prefix_len[e]) == 0) continue;
+      if (seg_offsets[e + 1] - seg_offsets[e] < 2 || shared_tokens(kv->dtype == MES_KV_E4M3_BLOCKS, prefix_len[e]) == 0) continue;
       a.first[a.n_groups] = seg_offsets[e];
       a.behind[a.n_groups] = seg_offsets[e + 1];
       a.prefix[a.n_groups++] = prefix_len[e];

@@ -105,10 +105,6 @@ __host__ __device__ constexpr int shared_tokens(bool blocks, int prefix) { retur
 // (mes_attn_decode.hip has the proof), and calls that could have 2^32 are refused.
 constexpr int64_t kMostCosts = 12;
 inline bool decode_fits(int n_seqs, int n_kv_heads, int capacity) { return kMostCosts * n_seqs * n_kv_heads * (capacity / 128 + 2) <= (int64_t)1 << 32; }
-// The fewest sequences whose common tokens are read once.  Over codes a pass takes longer than two wavefronts that read the tokens for a sequence each, as half of
-// the bytes are not what it waits for (prefixes of 500 to 4000 tokens, 64 experts of two sequences: 121 us shared, 96 apart; 16 of
-// three 38 and 43).  Over bf16 it does not (64 of two: 156 and 184).
-__host__ __device__ constexpr int least_sharing(bool codes) { return codes ? 3 : 2; }
 size_t attn_decode_workspace_bytes(int n_seqs, int n_heads, int n_kv_heads, int head_dim);
 hipError_t launch_attn_decode(const DecodeArgs& a, int source, hipStream_t s);
 

@@ -134,7 +134,7 @@ struct Shared {
   [[no_unique_address]] std::conditional_t<MANY, TileLds<D>, Nothing> tiles;
   [[no_unique_address]] std::conditional_t<FEW, Merge<D>, Nothing> merge;
   uint32_t cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
-  int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: too few are (least_sharing)
+  int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: fewer than two are
   uint32_t part[4];
 };
 
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       if (src < 0 && who) src = s0 + __builtin_ctzll(who);
       count += __popcll(who);
     }
-    const bool active = count >= least_sharing(has_codes(SRC));
+    const bool active = count >= 2;
     if (active)
       for (int s = first + lane; s < behind; s += 64)
         if (length(s) >= prefix) sh.cum[n_groups + s] = own_cost(read_once(prefix), length(s));

@@ -29,7 +29,7 @@ def _line(lens, prefix, group, codes):
     tile, begin = (4, 8) if wide else (7, 12) if codes else (4, 7)
     many = lambda a, b: begin + tile * -(-(b - a // 64 * 64) // 64) if b > a else 0  # noqa: E731
     own = lambda a, b: many(a, b) if wide else (3 if codes else 2) + -(-(b - a // 32 * 32) // 32) if b > a else 0  # noqa: E731
-    shares = sum(n >= prefix > 0 for n in lens) >= (3 if codes else 2)
+    shares = sum(n >= prefix > 0 for n in lens) >= 2
     total = sum(own(prefix if shares and n >= prefix else 0, n) for n in lens)
     return total + (math.ceil(len(lens) / per_pass) * many(0, prefix) if shares else 0)
 

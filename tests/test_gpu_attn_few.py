@@ -89,3 +89,20 @@ def test_lengths_grow_in_a_captured_graph(kind):
             pick = slice(2 * h, 2 * h + 2)
             want, tol = O.attend(q[s:s + 1, pick], k[:, h:h + 1], v[:, h:h + 1], [n - 1], dim ** -0.5)
             _check(out[s:s + 1, pick], want, tol, f"sequence {s} of {n}")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,heads,kvh,dim,prefix", [(2, 8, 2, 128, 96), (2, 2, 2, 64, 640), (3, 4, 1, 64, 160), (16, 4, 4, 128, 2048), (4, 8, 2, 64, 1312)])
+def test_a_shared_prefix_is_read_through_the_first_sequences_pages(n, heads, kvh, dim, prefix, kind):
+    """However few share it: the others need not hold it."""
+    lens = [prefix + 10 + 7 * s for s in range(n)]
+    share = {s: (0, prefix) for s in range(n)} if kind == "blocks" else [(0, prefix)] * n
+    c = _cache(kind, n + prefix, lens, kvh, dim, 32, share=share)
+    for s in range(1, n):
+        for x in (c.cache.k, c.cache.v):
+            pages = torch.tensor(c.table[s][:prefix // 32], device=DEV)
+            x.view(torch.uint8)[0, pages] = 0x7f                 # e4m3: NaN; bf16: 3.4e38
+    q = _rows(torch.Generator().manual_seed(5), n, heads, dim)
+    call = mes.AttnDecode(c.cache, heads, n)
+    call.ws.fill_(255)
+    _right(c, lens, call(0, c.batch(), q.to(DEV), [0, n], [prefix]), q)
