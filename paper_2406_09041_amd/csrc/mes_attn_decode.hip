@@ -45,6 +45,7 @@ constexpr int kThreads = 256, kWaves = kThreads / 64, kStep = 32, kRowsPass = 12
 template <int SRC>
 struct Cost {
   static constexpr uint32_t kTile = has_codes(SRC) ? 7 : 4, kBegin = has_codes(SRC) ? 12 : 7, kOwn = has_codes(SRC) ? 3 : 2;
+  static constexpr uint32_t kTileStreamed = 64 / kStep, kBeginStreamed = kWaves * kOwn;   // of a pass whose tokens are streamed
 };
 // Costs of a sequence and head never pass kMostCosts (u + 2), u = capacity / 128 (4 u + 4 steps, 2 u + 2 tiles at most), so that those of a call, and what they
 // are rounded up by, fit 32 bits (see decode_fits).  Sequences that share pay for the tokens behind the prefix, those shorter than it for their own alone, and there are
@@ -67,6 +68,7 @@ constexpr int kWholeTokens = 512;
 // they do (one sequence of 60000 tokens, 8 heads over one key / value head: 52 us, 20 as in few_items; of 8000, 32 over 8: 18.0 and 12.4; 32
 // of 700, 28 over 4: 19.4 and 15.5).  From about 200 items on the line is as fast or faster, and where a part would be longer than
 // kMostUnits, as parts of one length leave compute units idle (one of 60000, 40 heads of their own: 219 us and 256).
+constexpr int kLeastStreamed = 256;   // tokens
 constexpr int kFewItems = 192, kFewSeqs = 256, kMostUnits = 8;
 static_assert(kFewItems <= kWorkgroups && kFewSeqs >= kFewItems && kFewSeqs % 64 == 0, "an item has a workgroup, a lane as many sequences as another");
 static_assert(kThreads == kTileThreads && kRowsPass == kTileWaves * kWaveRows, "the workgroups of both bodies are the same");
@@ -129,10 +131,14 @@ struct Merge {                                      // a workgroup's four wavefr
   float2 ml[4][kFewRows];
 };
 struct Nothing {};
-template <int D, bool MANY, bool FEW>
+// What a decode kernel is made for: the line of sequences' own parts alone; few items before it; prefixes that are shared, or more than 16 query heads a key /
+// value head; prefixes of few rows.  What a call does not need costs its kernel registers, so each has its own (few_items beside the line: up to 3%,
+// passes that are streamed beside those that are not: 5%).
+enum Mode { LINE, FEW_ITEMS, MANY_ROWS, STREAMED };
+template <int D, int MODE>
 struct Shared {
-  [[no_unique_address]] std::conditional_t<MANY, TileLds<D>, Nothing> tiles;
-  [[no_unique_address]] std::conditional_t<FEW, Merge<D>, Nothing> merge;
+  [[no_unique_address]] std::conditional_t<(MODE >= MANY_ROWS), TileLds<D>, Nothing> tiles;
+  [[no_unique_address]] std::conditional_t<MODE == FEW_ITEMS, Merge<D>, Nothing> merge;
   uint32_t cum[MES_MAX_SEQS + MES_MAX_EXPERTS + 1];
   int group_src[MES_MAX_EXPERTS];                   // first sequence as long as the prefix, -1: fewer than two are
   uint32_t part[4];
@@ -536,13 +542,12 @@ __device__ __forceinline__ bool few_items(const DecodeCall& c, Merge<D>& sh) {
   return true;
 }
 
-// MANY: prefixes are shared, or more than 16 query heads a key / value head.
-// FEW: few items, see few_items (a kernel of its own: with that code beside it the line's ran up to 3% slower).
-template <int D, int SRC, bool MANY, bool FEW>
+template <int D, int SRC, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
-  __shared__ __align__(16) Shared<D, MANY, FEW> sh;
+  constexpr bool MANY = MODE >= MANY_ROWS, STREAM = MODE == STREAMED;
+  __shared__ __align__(16) Shared<D, MODE> sh;
   const DecodeArgs& a = c.a;
-  if constexpr (FEW)
+  if constexpr (MODE == FEW_ITEMS)
     if (few_items<D, SRC>(c, sh.merge)) return;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const bool wide = MANY && c.sh.group > kFewRows;  // sequences' own parts have too many rows for the small body, too
@@ -552,8 +557,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
   auto steps_of = [](int from, int to) { return to > from ? (to - (from & -kStep) + kStep - 1) / kStep : 0; };
   typedef Cost<SRC> C;
   const uint32_t tile_cost = wide ? kWaves : C::kTile, begin_cost = wide ? 2 * kWaves : C::kBegin;   // (a workgroup's border at every tile); see costs_fit
-  auto many_cost = [&](int from, int to) { return to > from ? begin_cost + tiles_of(from, to) * tile_cost : 0u; };
-  auto own_cost = [&](int from, int to) { return wide ? many_cost(from, to) : to > from ? C::kOwn + steps_of(from, to) : 0u; };
+  // of a group's pass, or (wide) of a sequence's own part
+  auto streamed = [&](int it) { return STREAM && it < n_groups && (a.behind[it] - a.first[it]) * c.sh.group <= kFewRows; };
+  auto tile_cost_of = [&](int it) { return streamed(it) ? C::kTileStreamed : tile_cost; };
+  auto begin_cost_of = [&](int it) { return streamed(it) ? C::kBeginStreamed : begin_cost; };
+  auto many_cost = [&](int it, int from, int to) { return to > from ? begin_cost_of(it) + tiles_of(from, to) * tile_cost_of(it) : 0u; };
+  auto own_cost = [&](int from, int to) { return wide ? many_cost(n_groups, from, to) : to > from ? C::kOwn + steps_of(from, to) : 0u; };
   // the tokens that are read once, of those that an expert's sequences share
   auto read_once = [](int prefix) { return shared_tokens(SRC == KV_PAGED_BLOCKS, prefix); };
 
@@ -574,7 +583,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
         if (length(s) >= prefix) sh.cum[n_groups + s] = own_cost(read_once(prefix), length(s));
     if (lane == 0) {
       sh.group_src[g] = active ? src : -1;
-      sh.cum[g] = active ? many_cost(0, read_once(prefix)) * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
+      sh.cum[g] = active ? many_cost(g, 0, read_once(prefix)) * ((behind - first + c.sh.per_pass - 1) / c.sh.per_pass) : 0;
     }
   }
   __syncthreads();
@@ -626,7 +635,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
   // ---- the larger body's part: a tile is the workgroup's whose costs it begins in
   if constexpr (MANY) {
     const uint32_t end = end_of(blockIdx.x + 1, each, many_all);
-    auto tiles_before = [&](uint32_t cost) { return cost > begin_cost ? (cost - begin_cost + tile_cost - 1) / tile_cost : 0u; };   // that begin there
     for (uint32_t u = end_of(blockIdx.x, each, many_all); u < end;) {
       const int h = uniform(u / many_head);
       const uint32_t in_head = u - h * many_head;
@@ -636,6 +644,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
         if (sh.cum[mid] <= in_head) lo = mid; else hi = mid - 1;
       }
       const int it = uniform(lo);
+      const uint32_t per_tile = uniform(tile_cost_of(it)), begin = uniform(begin_cost_of(it));
+      auto tiles_before = [&](uint32_t cost) { return cost > begin ? (cost - begin + per_tile - 1) / per_tile : 0u; };   // that begin there
       uint32_t first = h * many_head + uniform(sh.cum[it]), behind = h * many_head + uniform(sh.cum[it + 1]);
       Segment g;
       bool direct = false;
@@ -643,7 +653,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       float2* ml;
       g.kvh = h;
       if (it < n_groups) {
-        const uint32_t per_pass = many_cost(0, read_once(a.prefix[it]));
+        const uint32_t per_pass = many_cost(it, 0, read_once(a.prefix[it]));
         const int pass = uniform((u - first) / per_pass);
         first += pass * per_pass;
         behind = first + per_pass;
@@ -672,6 +682,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
       if (it >= n_groups) direct = g.from == 0 && tile0 == 0 && tile1 == (int)tiles_before(behind - first);
       g.t0 = (g.from & -kTile) + tile0 * kTile;
       g.t1 = min((g.from & -kTile) + tile1 * kTile, g.to);
+      if constexpr (STREAM)
+        if (streamed(it)) {
+          static_assert(sizeof(Merge<D>) <= sizeof(sh.tiles), "LDS of both bodies");
+          __syncthreads();                          // the last piece's reads of LDS are over
+          Few<D, SRC, true> few(a, c.sh.group);
+          few.start(g);
+          few.run(g, true, false, g, &reinterpret_cast<Merge<D>&>(sh.tiles), false, o, ml);
+          continue;
+        }
       run_many<D, SRC>(a, c.sh.group, g, sh.tiles, direct, o, ml);
     }
     asm volatile("" ::: "memory");
@@ -750,8 +769,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_decode(DecodeCall c) {
     for (int g = 0; g < n_groups; ++g) {
       if (s < a.first[g] || s >= a.behind[g]) continue;
       if (sh.group_src[g] >= 0 && length(s) >= a.prefix[g]) {
-        const uint32_t n = many_cost(0, read_once(a.prefix[g])), pass = (s - a.first[g]) / c.sh.per_pass;
-        const uint32_t u0 = h * many_head + sh.cum[g] + pass * n, w0 = (u0 + begin_cost) / each, w1 = (u0 + n - tile_cost) / each;
+        const uint32_t n = many_cost(g, 0, read_once(a.prefix[g])), pass = (s - a.first[g]) / c.sh.per_pass;
+        const uint32_t u0 = h * many_head + sh.cum[g] + pass * n, w0 = (u0 + begin_cost_of(g)) / each, w1 = (u0 + n - tile_cost_of(g)) / each;
         w.z = w0 + h * c.sh.n_passes + c.pass_base[g] + pass;
         w.w = (w1 - w0 + 1) | ((s - a.first[g]) % c.sh.per_pass * c.sh.group) << 16;
       }
@@ -840,6 +859,22 @@ __global__ __launch_bounds__(W == 1 ? kThreads : 64 * W) void k_join(DecodeCall 
   else *dst = (uint16_t)pack2(x[0] * inv, 0.0f);
 }
 
+// Whether passes of up to kFewRows rows stream their tokens, as sequences' own parts do, instead of bringing them to LDS for rows that are not there: where most
+// tokens that a call shares are of such passes and, unless it is small, are more than a few tiles.  Prefixes of 2048 tokens, e4m3: 64 experts of two sequences, 40 heads of their
+// own, 360 us (514 through LDS), 32 of 3, 32 heads over 8, 43 (50); bf16 with 16 heads of 64, 64 of two, 148 (172), but with 128
+// dimensions as fast or slower (8 of 3, 40 heads: 82 and 75).
+bool streaming_pays(const DecodeCall& c, int head_dim, int source) {
+  if (c.sh.group > kFewRows || !(has_codes(source) || head_dim == 64)) return false;
+  const bool small = c.a.n_seqs * c.a.n_kv_heads <= kFewItems;
+  int64_t few = 0, more = 0;                        // tokens of such passes, of others
+  for (int g = 0; g < c.a.n_groups; ++g) {
+    const int n = c.a.behind[g] - c.a.first[g], prefix = c.a.prefix[g];
+    if (n * c.sh.group <= kFewRows && (prefix >= kLeastStreamed || small)) few += prefix;
+    else more += (int64_t)((n + c.sh.per_pass - 1) / c.sh.per_pass) * prefix;
+  }
+  return few > more;
+}
+
 template <int D, int SRC>
 hipError_t launch(const DecodeCall& c, hipStream_t s) {
   const bool many = c.sh.group > kFewRows || c.a.n_groups > 0;
@@ -850,10 +885,12 @@ hipError_t launch(const DecodeCall& c, hipStream_t s) {
   // never more workgroups than steps there can be
   const int64_t most = (int64_t)c.a.n_kv_heads * (c.a.n_seqs + c.sh.n_passes) * ((c.a.capacity + kStep - 1) / kStep + 1);
   const unsigned grid = (unsigned)std::min<int64_t>(kWorkgroups, most);
-  const bool few = c.a.n_seqs * c.a.n_kv_heads <= kFewItems;
-  if (many) k_attn_decode<D, SRC, true, false><<<grid, kThreads, 0, s>>>(c);
-  else if (few) k_attn_decode<D, SRC, false, true><<<grid, kThreads, 0, s>>>(c);
-  else k_attn_decode<D, SRC, false, false><<<grid, kThreads, 0, s>>>(c);
+  auto go = [&](auto mode) { k_attn_decode<D, SRC, decltype(mode)::value><<<grid, kThreads, 0, s>>>(c); };
+  constexpr int kStreamed = has_codes(SRC) || D == 64 ? STREAMED : MANY_ROWS;
+  if (many && streaming_pays(c, D, SRC)) go(std::integral_constant<int, kStreamed>{});
+  else if (many) go(std::integral_constant<int, MANY_ROWS>{});
+  else if (c.a.n_seqs * c.a.n_kv_heads <= kFewItems) go(std::integral_constant<int, FEW_ITEMS>{});
+  else go(std::integral_constant<int, LINE>{});
   if (hipError_t e = hipGetLastError()) return e;
   const int rows = c.a.n_seqs * c.a.n_heads;
   if (rows <= 64) k_join<D, 16><<<rows, 1024, 0, s>>>(c, SRC == KV_PAGED_E4M3);

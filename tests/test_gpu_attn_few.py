@@ -106,3 +106,31 @@ def test_a_shared_prefix_is_read_through_the_first_sequences_pages(n, heads, kvh
     call = mes.AttnDecode(c.cache, heads, n)
     call.ws.fill_(255)
     _right(c, lens, call(0, c.batch(), q.to(DEV), [0, n], [prefix]), q)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads,kvh,dim", [(8, 2, 64), (4, 4, 128), (14, 2, 128)])
+def test_passes_of_few_and_of_many_rows(heads, kvh, dim, kind):
+    """In one call: experts of two and three sequences, of twenty, of one; sequences shorter than their prefix, as long as it, ended ones."""
+    segs, prefix = [3, 20, 2, 1, 2, 2], [3000, 100, 1500, 9, 700, 333]
+    bounds, rng, lens, share = [0], random.Random(4), [], {}
+    for e, n in enumerate(segs):
+        bounds.append(bounds[-1] + n)
+        mine = [prefix[e] + rng.choice([0, 1, 31, 400, 1300]) for _ in range(n)]
+        if e == 1:
+            mine[3], mine[4] = 0, 99
+        if e == 4:
+            mine[0] = 699                                        # one as long as the prefix: nothing is shared
+        first = next((s for s, m in enumerate(mine) if m >= prefix[e]), None)
+        share.update({len(lens) + s: (len(lens) + first, prefix[e]) for s, m in enumerate(mine) if m >= prefix[e]})
+        lens += mine
+    n = len(lens)
+    c = _cache(kind, 9, lens, kvh, dim, 16, share=share if kind == "blocks" else [share.get(s, (s, 0)) for s in range(n)])
+    q = _rows(torch.Generator().manual_seed(24), n, heads, dim, 2.0)
+    call = mes.AttnDecode(c.cache, heads, n)
+    out = []
+    for fill in (0, 255):
+        call.ws.fill_(fill)
+        out.append(call(0, c.batch(), q.to(DEV), bounds, prefix))
+    assert torch.equal(*out)
+    _right(c, lens, out[0], q)
