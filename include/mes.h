@@ -377,7 +377,7 @@ mes_status mes_kv_append_fresh(const mes_kv* kv, int layer, const mes_seqs* seqs
                                int n_heads, int ld_q, int ld_k, int ld_v, const float* rotary, int n_positions, void* q_out,
                                int ld_q_out, void* stream);
 
-/* Rotary positions in their other forms.  Position p turns pair i of the first `dims` dimensions of a head by the angle that row p of the table
+/* Rotary positions in other forms.  Position p turns pair i of the first `dims` dimensions of a head by the angle that row p of the table
  * has the cosine and sine of: (a c - b s, b c + a s); the dimensions behind are left as they are.  MES_ROTARY_HALVES: pair i is
  * (i, i + dims / 2), as in mes_kv_append; MES_ROTARY_PAIRS: neighbours, (2 i, 2 i + 1).  dims: a multiple of 16, at most head_dim. */
 enum { MES_ROTARY_HALVES = 0, MES_ROTARY_PAIRS = 1 };
@@ -417,7 +417,7 @@ mes_status mes_rotary(const mes_angles* angles, const int32_t* positions, const 
                       int fresh, void* stream);
 
 /* Reads tokens back: row t of sequence s, numbered as in mes_kv_append, gets the keys and values of its position in bf16
- * (e4m3: code times scale, rounded once; blocks: the value itself) in k, v [T][n_kv_heads][head_dim], rows ld_* apart, which overlap
+ * (e4m3: code times scale, rounded to fp32 and that to bf16; blocks: the value itself) in k, v [T][n_kv_heads][head_dim], rows ld_* apart, which overlap
  * neither each other nor the cache.  Either may be NULL.  Rows of a sequence whose token is absent (see mes_seqs) or before position 0 are set
  * to 0; rows behind the last sequence are left as they are, with fresh = 1 set to 0. */
 mes_status mes_kv_read(const mes_kv* kv, int layer, const mes_seqs* seqs, int T, void* k, void* v, int ld_k, int ld_v, int fresh,

@@ -5,8 +5,8 @@
 // prefix, in tiles of 64 tokens, which a workgroup's four wavefronts do together.  Then what every sequence has of its own, in steps of 32 tokens,
 // which a wavefront does alone and waits for nobody (in teams of four with their sums added up in LDS, sequences of 16 to 4096 tokens
 // took 104 us instead of 91, as beginning and ending a piece cost 4 us each).  The line is cut into equal chunks, wherever that falls: all wavefronts are
-// equally busy however the lengths are spread, also for one long sequence, and the launch does not depend on the lengths, which stay on
-// the device (every workgroup adds them up for itself).  A piece of the line that does not cover a sequence alone leaves (bound, sum,
+// equally busy however the lengths are spread, and the launch does not depend on the lengths, which stay on
+// the device (every workgroup adds them up for itself).  Where there are few sequences and heads, they are cut in equal parts instead (few_items).  A piece of the line that does not cover a sequence alone leaves (bound, sum,
 // weighted values) in the workspace, and k_join adds the pieces of a row in their order.
 //
 // A sequence's own tokens, up to 16 heads per key / value head: a wavefront takes 32 tokens at a time.  Scores are formed transposed,
@@ -17,8 +17,9 @@
 // is pairs of 16-bit halves put together, one v_perm each.  So neither keys nor values pass through LDS.  Of the 16 columns of a
 // tile 4 (n_heads / n_kv_heads) are used where nothing is shared: the matrix cores are idle most of the time anyway.
 //
-// Prefixes, however few rows share them: up to 128 rows share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from
-// about 100 rows on; also those of a sequence alone where more than 16 query heads share a key / value head.
+// Prefixes: up to 128 rows share keys and values in LDS (mes_attn_tiles.h), bound by the matrix cores from about 100 rows on; also those of a
+// sequence alone where more than 16 query heads share a key / value head.  Passes of up to 16 rows stream their tokens as above where that pays
+// (streaming_pays).
 //
 // Weights are rounded to bf16 for the product with V, as the matrix cores take both operands alike, and summed as rounded: they still add up
 // to 1, and a row's error grows by at most 2^-8 of its weighted values' size (measured against 64 bits: 0.0020 of the rows' norm, 0.0017
@@ -27,8 +28,8 @@
 // Measured (head_dim 128, 32 heads over 8 key / value heads): 256 sequences of 0 to 8192 tokens 160 us, 5.0 TB/s of the 5.96 that a
 // pass that only reads reaches; the same over e4m3 codes 91 us, 4.4 TB/s (the wavefronts end within 81 us, half of them within 74, and the join
 // takes 7); 256 of 735 tokens over blocks 76 us, 5.1 TB/s; 256 of 9 experts with prompts of 64 to 4000 tokens over blocks 109 us; 64 of 16 experts with
-// prompts of 512 to 1600 tokens 33 us; 96 behind 8200 shared tokens of an e4m3 cache 49 us, of which 10 us are products at the library's
-// rate; one sequence of 200 tokens 8.3 us.  Two steps of a wavefront on their way instead of one: no faster over codes, and spilled over bf16; the heads
+// prompts of 512 to 1600 tokens 33 to 36 us; 96 behind 8200 shared tokens of an e4m3 cache 50 us, of which 10 us are products at the library's
+// rate; one sequence of 200 tokens 8.3 us, of 8000 12.4.  Two steps of a wavefront on their way instead of one: no faster over codes, and spilled over bf16; the heads
 // of a sequence one behind the other on the line, instead of the sequences of a head: the same.
 #include "mes_attn_tiles.h"
 
@@ -39,9 +40,9 @@ constexpr bool has_codes(int source) { return source != KV_PAGED; }
 
 constexpr int kThreads = 256, kWaves = kThreads / 64, kStep = 32, kRowsPass = 128, kFewRows = 16;
 // Costs on the line, in steps of a wavefront: of a tile of the larger body, of beginning and ending what a pass or a sequence does there, and
-// the same of a sequence's own part in the smaller one.  As measured under load over codes: a step 1.8 us, a piece 4.4 to 5.7 us more, a
-// workgroup's tile 3.2 us and a pass 5.5 to 6.5 us more, which is four wavefronts' time; steps over bf16 take about twice as long.  (Tiles at 3 steps and passes at
-// nothing: 162 us instead of 109 for the 256 sequences of 9 experts, and 300 instead of 100 for 128 sequences that share one token.)
+// the same of a sequence's own part in the smaller one.  Under load, heads of 128: a step takes 2.7 us over codes and 5.4 over bf16, a piece 5 us more, a workgroup's
+// tile 2.3 to 2.6 us over codes and 3.1 over bf16 (four wavefronts' time).  Tiles and passes are set higher than that: they come first on the line, and what is late there
+// ends last (256 sequences of 9 experts over blocks: 162 us with tiles at 3 and passes at nothing, 109 with these).
 template <int SRC>
 struct Cost {
   static constexpr uint32_t kTile = has_codes(SRC) ? 7 : 4, kBegin = has_codes(SRC) ? 12 : 7, kOwn = has_codes(SRC) ? 3 : 2;

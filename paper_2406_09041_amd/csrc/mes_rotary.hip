@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void k_rotary_table(TableArgs a) {
 }
 
 // One workgroup per row (rows blockIdx, blockIdx + gridDim, ... where there are more than a launch has workgroups), a unit per thread.
-// Gradients of 8192 tokens' rows (40 heads of 128, bf16): 172 MB in 31.6 us, 5.4 TB/s; 21 tokens as long as a launch.
+// Gradients of 8192 tokens' rows (40 heads of 128, bf16): 172 MB in 33 to 35 us, 4.9 to 5.2 TB/s; 21 tokens as long as a launch.
 template <class E>
 __global__ __launch_bounds__(1024) void k_rotary(RotaryArgs a) {
   const int d = a.head_dim, per = d >> 4, units = (a.n_heads + a.n_kv_heads) * per, turned = a.dims >> 4;
