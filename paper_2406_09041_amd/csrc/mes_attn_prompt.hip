@@ -32,8 +32,9 @@ __device__ __forceinline__ int rows_of(const PromptArgs& a, int s, int& lo) {
   return max(min(a.q_offsets[s + 1], a.T) - lo, 0);
 }
 
-// More than the table has room for makes no difference to any row.
-__device__ __forceinline__ int tokens_before(const PromptArgs& a, int s, int rows) { return min(max(a.kv_len[s], 0) - rows, a.capacity); }
+// Tokens before the sequence's row `lo`, its first: all that the offsets name count, also those that the call does not have.  More than the table has room for makes no
+// difference to any row.
+__device__ __forceinline__ int tokens_before(const PromptArgs& a, int s, int lo) { return min(max(a.kv_len[s], 0) - max(a.q_offsets[s + 1] - lo, 0), a.capacity); }
 
 // Up to 64 sequences: lane s looks after sequence s.  Keys are counted in units of R: item t of a sequence sees about base + t + 1.
 struct Lanes {
@@ -49,7 +50,7 @@ __device__ Lanes look(const PromptArgs& a, int R, int columns, int cut_slots) {
   Lanes y = {};
   if (lane < a.n_seqs) {
     y.n = rows_of<SRC>(a, lane, y.lo);
-    if (SRC != KV_PACKED) y.before = tokens_before(a, lane, y.n);
+    if (SRC != KV_PACKED) y.before = tokens_before(a, lane, y.lo);
   }
   y.tiles = (y.n + R - 1) / R;
   y.base = (max(y.before, 0) + R - 1) / R;
@@ -125,7 +126,7 @@ __device__ bool item_number(const PromptArgs& a, const Lanes& y, int R, int j, i
   it.seq = lo;
   it.rows = rows_of<SRC>(a, lo, it.row0);
   it.tile = j - max(a.q_offsets[lo], 0) / R - lo;
-  it.before = SRC != KV_PACKED ? tokens_before(a, lo, it.rows) : 0;
+  it.before = SRC != KV_PACKED ? tokens_before(a, lo, it.row0) : 0;
   return it.tile >= 0 && it.tile < (it.rows + R - 1) / R;
 }
 

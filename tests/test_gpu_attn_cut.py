@@ -82,3 +82,21 @@ def test_offsets_out_of_order(kind):
     rows = [0, 1, 3000, 5100, T - 1]
     want, tol = O.attend(q[rows], k, v, rows, dim ** -0.5)
     _check(out[rows], want, tol)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("many", [0, 70])
+def test_fewer_rows_than_the_offsets_name(kind, many):
+    """The rows that are there are the first of their sequence's, with and without more than 64 sequences beside it: those of the whole call."""
+    lens, news = [5] * many + [40, 900], [2] * many + [33, 300]
+    heads, kvh, dim, T = 4, 2, 64, 2 * many + 33 + 130
+    c, off = _cache(kind, 3, lens, kvh, dim, 16), _offsets(news)
+    q = _rows(torch.Generator().manual_seed(3), off[-1], heads, dim, 2.0).to(DEV)
+    whole = mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q)
+    some = mes.mes_attn_extend(c.cache, c.layer, c.batch(off), q[:T])
+    for s in range(len(lens)):
+        rows = [r for r in (0, 1, news[s] // 3, news[s] - 1) if off[s] + r < T]
+        pick = [off[s] + r for r in rows]
+        want, tol = O.attend(q[pick].cpu(), c.k[s], c.v[s], [lens[s] - news[s] + r for r in rows], dim ** -0.5)
+        _check(whole[pick], want, tol, f"all rows, sequence {s}")
+        _check(some[pick], want, tol, f"some rows, sequence {s}")
