@@ -720,6 +720,7 @@ class _Turned(torch.autograd.Function):
     @staticmethod
     def backward(ctx, *grads):
         positions, _ = ctx.saved_tensors
+        grads = [g if need else None for g, need in zip(grads, ctx.needs_input_grad[3:])]
         there = [g.contiguous() for g in grads if g is not None]
         back = mes_rotary(ctx.angles, positions, *there, transpose=not ctx.transpose) if there else ()
         back = iter(back if len(there) == 2 else (back,))
